@@ -330,6 +330,170 @@ int fcp_noalloc_device_status(int32_t* status);
 int fcp_plan_set_profiling(fcp_plan* plan, int32_t enable);
 int fcp_plan_kernel_ms(const fcp_plan* plan, int32_t kind, int32_t* launches, float* mean_ms);
 
+/* ------------------------------------------------------------------------------------------
+ * Rotary positions.  Pair i of the first rotary_dim columns of every head is turned by the angle
+ * p * f_i, p the token's position, and stretched by a magnitude m:
+ *     (x, y) -> m * (x cos - y sin, y cos + x sin)
+ * pair i = columns (i, i + rotary_dim/2) in the layout HALF, (2i, 2i + 1) in INTERLEAVED; columns from rotary_dim
+ * on are copied.  With b = base, r = rotary_dim, s = factor, o = original_length, f_i = b^(-2i/r) is scaled to
+ *   LINEAR      f_i / s
+ *   NTK         the frequencies of the base b * s^(r/(r-2))                                   (r > 2)
+ *   YARN        f_i / s * t + f_i * (1 - t), t = clamp((i - lo) / (hi - lo), 0, 1), lo = floor(d(high)) and
+ *               hi = ceil(d(low)) clamped to [0, r-1], d(n) = r ln(o / (2 pi n)) / (2 ln b); high, low = 32, 1
+ *               turns within the original length unless given; m = 0.1 ln s + 1
+ *   WAVELENGTH  f_i * u + f_i / s * (1 - u), u = clamp((o f_i / (2 pi) - low) / (high - low), 0, 1);
+ *               high, low = 4, 1 turns unless given
+ * m = 1 unless YARN; magnitude > 0 sets it.
+ *
+ * fcp_rope_init — host only.  Fills the table (a plain value: copy it, keep it, no release).  Frequencies are
+ * held as fractions of a turn in 64 bits, turn[i] = 2^64 f_i / (2 pi), so that the angle of any position, as a
+ * fraction of a turn, is the integer product modulo 2^64: exact to 2^-33 turns at position 2^31.
+ * Errors: INVALID_ARG (NULL, unknown layout or scaling, odd rotary_dim or outside [2, head_dim], base <= 1,
+ * factor < 1, original_length <= 0 where it is used, low >= high, not finite), UNSUPPORTED (head_dim).
+ */
+#define FCP_ROPE_HALF         0
+#define FCP_ROPE_INTERLEAVED  1
+#define FCP_ROPE_NONE         0
+#define FCP_ROPE_LINEAR       1
+#define FCP_ROPE_NTK          2
+#define FCP_ROPE_YARN         3
+#define FCP_ROPE_WAVELENGTH   4
+
+typedef struct fcp_rope_config {
+  int32_t head_dim;          /* 64 or 128                                              */
+  int32_t rotary_dim;        /* even, 2 .. head_dim                                     */
+  int32_t layout;            /* FCP_ROPE_HALF or FCP_ROPE_INTERLEAVED                   */
+  int32_t scaling;           /* FCP_ROPE_NONE ... FCP_ROPE_WAVELENGTH                   */
+  double  base, factor, original_length;
+  double  low, high;         /* <= 0: the defaults above                                */
+  double  magnitude;         /* <= 0: the default above                                 */
+} fcp_rope_config;
+
+typedef struct fcp_rope_table {
+  int32_t  head_dim, rotary_dim, layout;
+  float    magnitude;
+  uint64_t turn[64];
+} fcp_rope_table;
+
+int fcp_rope_init(const fcp_rope_config* config, fcp_rope_table* table);
+
+/* fcp_rope_fwd / fcp_rope_bwd — device.  Turns q [T][hq][D] and k [T][hkv][D] (bf16) into q_out, k_out; the backward
+ * call takes the gradients of the outputs and gives those of the inputs (the transposed rotation).  *_stride: elements
+ * from one token's heads to the next one's (>= heads * D; 0 means heads * D), so that q and k may be slices of one
+ * projection; heads of a token are contiguous.  An output may be its input (same pointer and stride); otherwise they
+ * must not overlap.  q or k may be NULL with its head count 0.
+ * Positions: `positions` [T] (device), or, if NULL, from row_offset [B+1] (device), the packed batch's offsets: token t
+ * of sequence b stands at t - row_offset[b], with length [B] (device; NULL: not used) at
+ * length[b] - (row_offset[b+1] - row_offset[b]) + t - row_offset[b], i.e. the rows are the last ones of sequences of those
+ * lengths, as in the calls on a cache below.  Rows outside [row_offset[0], row_offset[B]) are left as they were.
+ * Arithmetic in fp32, one rounding to bf16.  Asynchronous on `stream`; no workspace.
+ * Errors: INVALID_ARG (NULL, T < 0 or >= 2^31, B < 0, a stride below heads * D, head counts < 0).
+ */
+int fcp_rope_fwd(const fcp_rope_table* table, int64_t T, const void* q, int64_t q_stride, int32_t hq, const void* k,
+                 int64_t k_stride, int32_t hkv, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                 const int32_t* positions, const int32_t* row_offset, const int32_t* length, int32_t B, void* stream);
+int fcp_rope_bwd(const fcp_rope_table* table, int64_t T, const void* dq, int64_t dq_stride, int32_t hq, const void* dk,
+                 int64_t dk_stride, int32_t hkv, void* dq_in, int64_t dq_in_stride, void* dk_in, int64_t dk_in_stride,
+                 const int32_t* positions, const int32_t* row_offset, const int32_t* length, int32_t B, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A cache of keys and values in 8 bits, for answering token by token with the attention of this library.
+ *
+ * The cache is a pool of pages that the caller owns (device memory):
+ *     k, v              [n_pages][hkv][page_tokens][D]   one byte per value: e4m3 (no infinities) or int8
+ *     k_scale, v_scale  [n_pages][hkv] fp32              value = code * scale
+ *     weight            [n_pages][hkv][page_tokens] fp32 attention weight that a token has drawn so far; may be NULL
+ *     status            [4] int32, zeroed by the caller  see below
+ * Token t of sequence b lies in page page_table[b][t / page_tokens] at t % page_tokens.  fcp_cache_create checks the
+ * description and makes a handle of it (host only, no device memory); the memory must live as long as the handle is used.
+ *
+ * A call works on a batch of sequences.  The rows of its tensors are the newest tokens of each sequence, packed: rows
+ * row_offset[b] .. row_offset[b+1]-1 are the last tokens of sequence b, whose length includes them.  row_offset, length
+ * and page_table are read on the device, so a captured call can be replayed with new contents; rows, max_new and
+ * table_width bound them on the host.  Rows behind row_offset[B] are neither read nor written.
+ *
+ * What the kernels check: a sequence with a length outside [0, table_width * page_tokens], or with row offsets that
+ * fall, leave [0, rows] or span more than max_new rows, counts as absent (its rows are not written); tokens on a page
+ * outside [0, n_pages) or, in fcp_cache_attn and fcp_cache_evict, on a page whose scale is not in
+ * [FCP_CACHE_MIN_SCALE, FCP_CACHE_MAX_SCALE], count as absent.  status then holds FCP_ERR_INVALID_ARG, one of the
+ * FCP_CACHE_BAD_* codes and the sequence (first failure, sticky); FCP_ERR_TIMEOUT as everywhere.
+ * The calls write nothing but what is listed, wherever pages and offsets point inside their buffers.
+ * Two calls on one cache must be stream-ordered if one of them writes what the other uses.
+ */
+#define FCP_CACHE_E4M3 0
+#define FCP_CACHE_INT8 1
+#define FCP_CACHE_MIN_SCALE 0x1p-100f
+#define FCP_CACHE_MAX_SCALE 0x1p+122f
+#define FCP_CACHE_BAD_LENGTH 1001
+#define FCP_CACHE_BAD_ROWS   1002
+#define FCP_CACHE_BAD_PAGE   1003
+#define FCP_CACHE_BAD_SCALE  1004
+
+typedef struct fcp_cache fcp_cache;
+typedef struct fcp_cache_config {
+  void    *k, *v;                    /* 16-byte aligned                                        */
+  float   *k_scale, *v_scale, *weight;
+  int32_t *status;
+  int32_t n_pages;                   /* n_pages * hkv * page_tokens < 2^31                     */
+  int32_t page_tokens;               /* 16, 32, 64 or 128                                      */
+  int32_t hkv, head_dim;             /* head_dim 64 or 128                                     */
+  int32_t kind;                      /* FCP_CACHE_E4M3 or FCP_CACHE_INT8                       */
+} fcp_cache_config;
+
+typedef struct fcp_cache_batch {
+  int32_t B;                         /* sequences                                              */
+  int32_t rows;                      /* rows of the call's tensors                             */
+  int32_t max_new;                   /* no sequence has more new tokens than this              */
+  int32_t table_width;               /* columns of page_table                                  */
+  const int32_t* page_table;         /* device [B][table_width]                                */
+  const int32_t* length;             /* device [B]                                             */
+  const int32_t* row_offset;         /* device [B+1]                                           */
+} fcp_cache_batch;
+
+int fcp_cache_create(const fcp_cache_config* config, fcp_cache** cache);
+int fcp_cache_destroy(fcp_cache* cache);
+/* The four status words (synchronises the device). */
+int fcp_cache_device_status(const fcp_cache* cache, int32_t* status);
+
+/* fcp_cache_append — device.  Writes the new tokens' k and v (bf16 [rows][hkv][D], *_stride as in fcp_rope_fwd) into their
+ * places.  Per page, head and tensor, with a = max |x| over the page's new tokens (infinities count as the largest finite
+ * value, NaN as 0):  fresh = the smallest power of two >= FCP_CACHE_MIN_SCALE with a / fresh <= 448 (e4m3) or 127 (int8);
+ * scale = max(old scale, fresh) if the page holds earlier tokens of the sequence, else fresh; new codes are
+ * x / scale rounded to the nearest (ties to even), infinities the largest code, NaN the NaN code (int8: 0); where the scale
+ * grew, the earlier codes are code * (old / scale), rounded.  Powers of two keep a floating code exact through that, as
+ * long as it is not subnormal.  weight, if there is one, is set to 0 at the new tokens.
+ * A page that takes new tokens must belong to one sequence only.  Calling again with the same arguments changes nothing.
+ */
+int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const void* k, int64_t k_stride, const void* v,
+                     int64_t v_stride, void* stream);
+
+/* fcp_cache_attn — device.  Attention of the new tokens, whose keys and values are in the cache already: new token j of n of
+ * a sequence of length L sees the keys at positions <= L - n + j,
+ *     o = softmax(q k^T * scale) v,   lse = natural log of the sum of exp(scaled scores)
+ * q bf16 [rows][hq][D] with q_stride, o bf16 [rows][hq][D], lse fp32 [rows][hq]; hq % hkv == 0; scale <= 0 means
+ * 1/sqrt(D).  A row that sees nothing gets o = 0 and lse = -infinity.  Pages may be shared by sequences.
+ * accumulate != 0: weight of every cached token += its attention weight, summed over the sequence's new tokens and the
+ * query heads of its KV head (what fcp_cache_evict goes by); then no page may appear twice among the call's tokens.
+ * workspace: device, 256-byte aligned, of at least fcp_cache_attn_workspace_bytes; its contents need not be initialised; two calls
+ * that may overlap on the GPU, also two captured ones, need one each.
+ * Results do not depend on the order in which blocks run.
+ */
+int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t hq, int64_t* bytes);
+int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const void* q, int64_t q_stride, int32_t hq,
+                   float scale, void* o, float* lse, int32_t accumulate, void* workspace, int64_t workspace_bytes,
+                   void* stream);
+
+/* fcp_cache_evict — device.  Cuts sequences to n_sink + n_heavy + n_recent tokens per KV head: the first n_sink, the last
+ * n_recent, and of those between the n_heavy of largest weight (equal ones: the earlier; NaN: last); a sequence that has no more
+ * is kept whole.  The kept tokens go, in their order, to the pages dst_table [B][dst_width] (device), which must not be
+ * among the batch's source pages: codes, weights, and per page and head the largest scale among the pages its tokens came
+ * from (codes are rounded again where their own was smaller).  new_length [B], kept [B][hkv][n_sink+n_heavy+n_recent] (position
+ * of each kept token, -1 behind the last) are written.  The cache needs weights.  row_offset, rows and max_new of the batch
+ * are not used.  new_length is 0 for an absent sequence.  A token on an absent source page is kept as zeros.
+ */
+int fcp_cache_evict(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t n_sink, int32_t n_heavy, int32_t n_recent,
+                    const int32_t* dst_table, int32_t dst_width, int32_t* new_length, int32_t* kept, void* stream);
+
 /* fcp_selftest_bounded_wait — device.  Every wait inside the persistent kernels (on an mbarrier fed
  * by TMA, the tensor core or another warp) is bounded: after 2 s without progress the waiter gives
  * up, the CTA unwinds, and FCP_ERR_TIMEOUT appears in the status words instead of a hung GPU.  This

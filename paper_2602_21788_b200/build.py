@@ -9,8 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfcp.so")
-SOURCES = ["fcp_plan.cpp", "fcp_kernels.cu"]
-HEADERS = ["fcp_plan.hpp", "sm100_ptx.cuh", "fcp_fwd.cuh", "fcp_bwd.cuh"]
+SOURCES = ["fcp_plan.cpp", "fcp_kernels.cu", "fcp_rope.cu", "fcp_cache.cu"]
+HEADERS = ["fcp_plan.hpp", "sm100_ptx.cuh", "fcp_launch.cuh", "fcp_fwd.cuh", "fcp_bwd.cuh", "fcp_cache_index.hpp", "fcp_cache.cuh"]
 
 
 def _stale() -> bool:

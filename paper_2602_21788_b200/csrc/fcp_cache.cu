@@ -1,0 +1,394 @@
+// The calls on a paged 8-bit cache: handle, checks, launches.
+#include <algorithm>
+#include <cstdint>
+#include <mutex>
+#include <new>
+
+#include "fcp_cache.cuh"
+#include "fcp_launch.cuh"
+
+using namespace fcp;
+
+// Whatever a call needs of the device is looked up at the handle's first compute call, so that a handle can be made, and its
+// calls refused, on a machine without a GPU.
+struct fcp_cache {
+  fcp_cache_config config;
+  mutable std::mutex mu;
+  mutable int device = -1;
+  mutable int sm_count = 0;
+  mutable CUtensorMap k_map, v_map;
+};
+
+namespace {
+
+inline int rows_per_tile(int wr) { return 16 * wr; }
+// Row tiles of 16, 32, 64 or 128 rows: the smallest that holds a KV head's rows, because the warps that stand side by side
+// for more rows all convert the same codes.
+int tile_warps(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
+int box_keys(const fcp_cache_config& c) { return std::min(c.page_tokens, CT_KEYS); }
+
+CacheView view(const fcp_cache_config& c) {
+  CacheView v;
+  v.k = (uint8_t*)c.k;
+  v.v = (uint8_t*)c.v;
+  v.k_scale = c.k_scale;
+  v.v_scale = c.v_scale;
+  v.weight = c.weight;
+  v.status = c.status;
+  v.n_pages = c.n_pages;
+  v.page_tokens = c.page_tokens;
+  v.hkv = c.hkv;
+  return v;
+}
+BatchView view(const fcp_cache_config& c, const fcp_cache_batch& b) {
+  BatchView v;
+  v.B = b.B;
+  v.rows = b.rows;
+  v.max_new = b.max_new;
+  v.table_width = b.table_width;
+  v.capacity = b.table_width * c.page_tokens;
+  v.page_table = b.page_table;
+  v.length = b.length;
+  v.row_offset = b.row_offset;
+  return v;
+}
+
+// One row of [hkv or hq][D] after the other: 16-byte pieces need aligned rows.
+int check_rows(const char* call, const char* name, const void* p, int64_t& stride, int64_t width) {
+  if (stride == 0) stride = width;
+  if (!p || ((uintptr_t)p & 15) != 0 || stride < width || stride % 8 != 0) {
+    fcp_set_error("%s: %s is NULL or not 16-byte aligned, or its stride %lld is below heads * head_dim = %lld or no multiple of 8",
+                  call, name, (long long)stride, (long long)width);
+    return FCP_ERR_INVALID_ARG;
+  }
+  return FCP_OK;
+}
+
+// `rows_used`: whether the call reads row_offset.
+int check_batch(const char* call, const fcp_cache* cache, const fcp_cache_batch* b, bool rows_used) {
+  if (!cache || !b) {
+    fcp_set_error("%s: NULL cache or batch", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (b->B < 0 || b->table_width < 1 || (int64_t)b->table_width * cache->config.page_tokens >= int64_t(1) << 31 ||
+      (b->B > 0 && (!b->page_table || !b->length))) {
+    fcp_set_error("%s: B %d, table_width %d, or a NULL page_table or length", call, b->B, b->table_width);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (rows_used && (b->rows < 0 || b->max_new < 0 || b->max_new > b->rows || (b->B > 0 && !b->row_offset) ||
+                    (int64_t)b->rows + 2 * (int64_t)b->B >= int64_t(1) << 31)) {
+    fcp_set_error("%s: rows %d, max_new %d, or a NULL row_offset", call, b->rows, b->max_new);
+    return FCP_ERR_INVALID_ARG;
+  }
+  return FCP_OK;
+}
+
+int cache_map(CUtensorMap* m, const fcp_cache_config& c, void* base) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) {
+    fcp_set_error("cuTensorMapEncodeTiled is not available from the driver");
+    return FCP_ERR_CUDA;
+  }
+  const cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.n_pages * c.hkv * c.page_tokens};
+  const cuuint64_t strides[1] = {(cuuint64_t)c.head_dim};
+  const cuuint32_t box[2] = {(cuuint32_t)c.head_dim, (cuuint32_t)box_keys(c)};
+  const cuuint32_t estr[2] = {1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  c.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    fcp_set_error("cuTensorMapEncodeTiled failed with %d", (int)r);
+    return FCP_ERR_CUDA;
+  }
+  return FCP_OK;
+}
+
+typedef void (*AttnKernel)(const CUtensorMap, const CUtensorMap, const AttnArgs);
+template <int D, int KIND>
+AttnKernel attn_kernel(int wr) {
+  return wr == 0 ? cache_attn_kernel<D, KIND, 0> : wr == 1 ? cache_attn_kernel<D, KIND, 1> : wr == 2 ? cache_attn_kernel<D, KIND, 2>
+         : wr == 4 ? cache_attn_kernel<D, KIND, 4> : cache_attn_kernel<D, KIND, 8>;
+}
+AttnKernel attn_kernel(const fcp_cache_config& c, int wr) {
+  if (c.head_dim == 128) return c.kind == FCP_CACHE_E4M3 ? attn_kernel<128, FCP_CACHE_E4M3>(wr) : attn_kernel<128, FCP_CACHE_INT8>(wr);
+  return c.kind == FCP_CACHE_E4M3 ? attn_kernel<64, FCP_CACHE_E4M3>(wr) : attn_kernel<64, FCP_CACHE_INT8>(wr);
+}
+int attn_smem(const fcp_cache_config& c) { return c.head_dim == 128 ? AttnSmem<128>::DYN_BYTES : AttnSmem<64>::DYN_BYTES; }
+
+// The first compute call of a handle: device, kernel attributes, tensor maps.  Later ones: the device is still the current one.
+int ready(const char* call, const fcp_cache* cache) {
+  int device = 0;
+  FCP_CUDA_CHECK(cudaGetDevice(&device));
+  std::lock_guard<std::mutex> lock(cache->mu);
+  if (cache->device == device) return FCP_OK;
+  if (cache->device >= 0) {
+    fcp_set_error("%s: the cache lies on device %d, the current device is %d", call, cache->device, device);
+    return FCP_ERR_INVALID_ARG;
+  }
+  cudaPointerAttributes where;
+  FCP_CUDA_CHECK(cudaPointerGetAttributes(&where, cache->config.k));
+  if (where.type != cudaMemoryTypeDevice && where.type != cudaMemoryTypeManaged) {
+    fcp_set_error("%s: the cache is not in device memory", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (where.device != device) {
+    fcp_set_error("%s: the cache lies on device %d, the current device is %d", call, where.device, device);
+    return FCP_ERR_INVALID_ARG;
+  }
+  int major = 0, sms = 0;
+  FCP_CUDA_CHECK(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device));
+  FCP_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+  if (major != 10) {
+    fcp_set_error("device %d is not sm_100: this library is built for sm_100a only", device);
+    return FCP_ERR_CUDA;
+  }
+  const fcp_cache_config& c = cache->config;
+  for (int wr : {0, 1, 2, 4, 8})
+    FCP_CUDA_CHECK(cudaFuncSetAttribute(attn_kernel(c, wr), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(c)));
+  FCP_CUDA_CHECK(cudaFuncSetAttribute(cache_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_BYTES));
+  int rc = cache_map(&cache->k_map, c, c.k);
+  if (rc == FCP_OK) rc = cache_map(&cache->v_map, c, c.v);
+  if (rc != FCP_OK) return rc;
+  cache->sm_count = std::min(sms, FCP_PLAN_SMS);
+  cache->device = device;
+  return FCP_OK;
+}
+
+// Workspace of fcp_cache_attn: partial outputs and log-sum-exps of two groups per CTA, and what each CTA shares.
+struct AttnSpace {
+  int64_t o, lse, split, bytes;
+};
+AttnSpace attn_space(int wr, int D) {
+  const int64_t parts = 2 * (int64_t)FCP_PLAN_SMS * rows_per_tile(wr);
+  AttnSpace s;
+  s.o = 0;
+  s.lse = parts * D * 4;
+  s.split = s.lse + (parts * 4 + 255) / 256 * 256;
+  s.bytes = s.split + (FCP_PLAN_SMS * SP_W * 4 + 255) / 256 * 256;
+  return s;
+}
+
+int check_heads(const char* call, const fcp_cache_config& c, int32_t hq) {
+  if (hq <= 0 || hq % c.hkv != 0 || hq > 65536) {
+    fcp_set_error("%s: %d query heads over %d KV heads", call, hq, c.hkv);
+    return hq > 0 && hq <= 65536 ? FCP_ERR_UNSUPPORTED : FCP_ERR_INVALID_ARG;
+  }
+  return FCP_OK;
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------------------------
+// Handle
+// ---------------------------------------------------------------------------------------------
+extern "C" int fcp_cache_create(const fcp_cache_config* c, fcp_cache** cache) {
+  if (!c || !cache) {
+    fcp_set_error("fcp_cache_create: NULL argument");
+    return FCP_ERR_INVALID_ARG;
+  }
+  *cache = nullptr;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->status || (((uintptr_t)c->k | (uintptr_t)c->v) & 15) != 0 ||
+      (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale | (uintptr_t)c->weight | (uintptr_t)c->status) & 3) != 0) {
+    fcp_set_error("fcp_cache_create: a buffer is NULL or not aligned");
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (c->head_dim != 64 && c->head_dim != 128) {
+    fcp_set_error("fcp_cache_create: head_dim %d is not 64 or 128", c->head_dim);
+    return FCP_ERR_UNSUPPORTED;
+  }
+  if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) {
+    fcp_set_error("fcp_cache_create: page_tokens %d is not 16, 32, 64 or 128", c->page_tokens);
+    return FCP_ERR_UNSUPPORTED;
+  }
+  if (c->kind != FCP_CACHE_E4M3 && c->kind != FCP_CACHE_INT8) {
+    fcp_set_error("fcp_cache_create: unknown kind %d", c->kind);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (c->n_pages <= 0 || c->hkv <= 0 || c->hkv > 32767 ||
+      (int64_t)c->n_pages * c->hkv >= ((int64_t(1) << 31) + c->page_tokens - 1) / c->page_tokens) {
+    fcp_set_error("fcp_cache_create: %d pages of %d heads and %d tokens: not positive, or 2^31 rows and more", c->n_pages, c->hkv, c->page_tokens);
+    return FCP_ERR_INVALID_ARG;
+  }
+  fcp_cache* h = new (std::nothrow) fcp_cache();
+  if (!h) {
+    fcp_set_error("fcp_cache_create: no host memory");
+    return FCP_ERR_NO_MEMORY;
+  }
+  h->config = *c;
+  *cache = h;
+  return FCP_OK;
+}
+
+extern "C" int fcp_cache_destroy(fcp_cache* cache) {
+  delete cache;
+  return FCP_OK;
+}
+
+extern "C" int fcp_cache_device_status(const fcp_cache* cache, int32_t* status) {
+  if (!cache || !status) {
+    fcp_set_error("fcp_cache_device_status: NULL argument");
+    return FCP_ERR_INVALID_ARG;
+  }
+  FCP_CUDA_CHECK(cudaDeviceSynchronize());
+  FCP_CUDA_CHECK(cudaMemcpy(status, cache->config.status, 4 * sizeof(int32_t), cudaMemcpyDeviceToHost));
+  return FCP_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Compute calls
+// ---------------------------------------------------------------------------------------------
+namespace {
+typedef void (*AppendKernel)(const AppendArgs);
+template <int D, int KIND>
+AppendKernel append_kernel(int page_tokens) {
+  const int n = page_tokens * D / (16 * APPEND_THREADS);
+  return n <= 1 ? cache_append_kernel<D, KIND, 1> : n == 2 ? cache_append_kernel<D, KIND, 2>
+         : n == 4 ? cache_append_kernel<D, KIND, 4> : cache_append_kernel<D, KIND, 8>;
+}
+}  // namespace
+
+extern "C" int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const void* k, int64_t k_stride,
+                                const void* v, int64_t v_stride, void* stream) {
+  const char* call = "fcp_cache_append";
+  int rc = check_batch(call, cache, batch, true);
+  if (rc != FCP_OK) return rc;
+  const fcp_cache_config& c = cache->config;
+  if (batch->B == 0 || batch->rows == 0 || batch->max_new == 0) return FCP_OK;
+  if ((rc = check_rows(call, "k", k, k_stride, (int64_t)c.hkv * c.head_dim)) != FCP_OK) return rc;
+  if ((rc = check_rows(call, "v", v, v_stride, (int64_t)c.hkv * c.head_dim)) != FCP_OK) return rc;
+  if ((rc = ready(call, cache)) != FCP_OK) return rc;
+  AppendArgs a;
+  a.c = view(c);
+  a.s = view(c, *batch);
+  a.k = (const __nv_bfloat16*)k;
+  a.v = (const __nv_bfloat16*)v;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.slots = batch->max_new == 1 ? batch->B : append_slot(batch->rows, batch->B, c.page_tokens);
+  AppendKernel kernel = c.head_dim == 128 ? (c.kind == FCP_CACHE_E4M3 ? append_kernel<128, FCP_CACHE_E4M3>(c.page_tokens)
+                                                                       : append_kernel<128, FCP_CACHE_INT8>(c.page_tokens))
+                                          : (c.kind == FCP_CACHE_E4M3 ? append_kernel<64, FCP_CACHE_E4M3>(c.page_tokens)
+                                                                      : append_kernel<64, FCP_CACHE_INT8>(c.page_tokens));
+  FCP_CUDA_CHECK(launch(kernel, dim3((unsigned)a.slots, (unsigned)(2 * c.hkv)), APPEND_THREADS, 0, (cudaStream_t)stream, a));
+  return FCP_OK;
+}
+
+extern "C" int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t hq, int64_t* bytes) {
+  const char* call = "fcp_cache_attn_workspace_bytes";
+  if (!bytes) {
+    fcp_set_error("%s: NULL argument", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  int rc = check_batch(call, cache, batch, true);
+  if (rc == FCP_OK) rc = check_heads(call, cache->config, hq);
+  if (rc != FCP_OK) return rc;
+  *bytes = attn_space(tile_warps((int64_t)batch->max_new * (hq / cache->config.hkv)), cache->config.head_dim).bytes;
+  return FCP_OK;
+}
+
+extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const void* q, int64_t q_stride, int32_t hq,
+                              float scale, void* o, float* lse, int32_t accumulate, void* workspace, int64_t workspace_bytes,
+                              void* stream) {
+  const char* call = "fcp_cache_attn";
+  int rc = check_batch(call, cache, batch, true);
+  if (rc != FCP_OK) return rc;
+  const fcp_cache_config& c = cache->config;
+  if ((rc = check_heads(call, c, hq)) != FCP_OK) return rc;
+  if (accumulate && !c.weight) {
+    fcp_set_error("%s: accumulate without weights in the cache", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (!(scale <= 3e38f)) {
+    fcp_set_error("%s: scale is not finite", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  const int group = hq / c.hkv;
+  if ((int64_t)batch->max_new * group >= int64_t(1) << 31) {
+    fcp_set_error("%s: %d new tokens of %d heads each", call, batch->max_new, group);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (batch->B == 0 || batch->rows == 0 || batch->max_new == 0) return FCP_OK;
+  if ((rc = check_rows(call, "q", q, q_stride, (int64_t)hq * c.head_dim)) != FCP_OK) return rc;
+  if (!o || !lse || ((uintptr_t)o & 15) != 0 || ((uintptr_t)lse & 3) != 0) {
+    fcp_set_error("%s: an output is NULL or not aligned", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  const int wr = tile_warps((int64_t)batch->max_new * group);
+  const AttnSpace space = attn_space(wr, c.head_dim);
+  if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < space.bytes) {
+    fcp_set_error("%s: workspace of %lld bytes (aligned to 256) needed, %lld given", call, (long long)space.bytes, (long long)workspace_bytes);
+    return FCP_ERR_WORKSPACE;
+  }
+  if ((rc = ready(call, cache)) != FCP_OK) return rc;
+  AttnArgs a;
+  a.c = view(c);
+  a.s = view(c, *batch);
+  a.q = (const __nv_bfloat16*)q;
+  a.q_stride = q_stride;
+  a.o = (__nv_bfloat16*)o;
+  a.lse = lse;
+  a.scale_log2 = (scale > 0 ? scale : (c.head_dim == 128 ? 0.08838834764831845f : 0.125f)) * 1.4426950408889634f;
+  a.hq = hq;
+  a.group = group;
+  a.box = box_keys(c);
+  a.part_o = (float*)((char*)workspace + space.o);
+  a.part_lse = (float*)((char*)workspace + space.lse);
+  a.split = (int32_t*)((char*)workspace + space.split);
+  cudaStream_t st = (cudaStream_t)stream;
+  const int smem = attn_smem(c), grid = cache->sm_count;
+  FCP_CUDA_CHECK(launch(attn_kernel(c, wr), grid, CT_THREADS, smem, st, cache->k_map, cache->v_map, a));
+  if (c.head_dim == 128) FCP_CUDA_CHECK(launch(cache_merge_kernel<128>, grid, MERGE_THREADS, 0, st, a, rows_per_tile(wr)));
+  else FCP_CUDA_CHECK(launch(cache_merge_kernel<64>, grid, MERGE_THREADS, 0, st, a, rows_per_tile(wr)));
+  if (accumulate) FCP_CUDA_CHECK(launch(attn_kernel(c, 0), grid, CT_THREADS, smem, st, cache->k_map, cache->v_map, a));
+  return FCP_OK;
+}
+
+extern "C" int fcp_cache_evict(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t n_sink, int32_t n_heavy, int32_t n_recent,
+                               const int32_t* dst_table, int32_t dst_width, int32_t* new_length, int32_t* kept, void* stream) {
+  const char* call = "fcp_cache_evict";
+  int rc = check_batch(call, cache, batch, false);
+  if (rc != FCP_OK) return rc;
+  const fcp_cache_config& c = cache->config;
+  const int64_t keep = (int64_t)n_sink + n_heavy + n_recent;
+  if (!c.weight) {
+    fcp_set_error("%s: the cache has no weights", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (n_sink < 0 || n_heavy < 0 || n_recent < 0 || keep < 1 || keep >= int64_t(1) << 31 || dst_width < 1 ||
+      (int64_t)dst_width * c.page_tokens < keep) {
+    fcp_set_error("%s: %d + %d + %d tokens to keep on %d pages of %d", call, n_sink, n_heavy, n_recent, dst_width, c.page_tokens);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if (batch->B > 65535) {
+    fcp_set_error("%s: more than 65535 sequences", call);
+    return FCP_ERR_UNSUPPORTED;
+  }
+  if (batch->B == 0) return FCP_OK;
+  if (!dst_table || !new_length || !kept) {
+    fcp_set_error("%s: NULL buffer", call);
+    return FCP_ERR_INVALID_ARG;
+  }
+  if ((rc = ready(call, cache)) != FCP_OK) return rc;
+  EvictArgs a;
+  a.c = view(c);
+  a.s = view(c, *batch);
+  a.n_sink = n_sink;
+  a.n_heavy = n_heavy;
+  a.n_recent = n_recent;
+  a.dst_table = dst_table;
+  a.dst_width = dst_width;
+  a.new_length = new_length;
+  a.kept = kept;
+  cudaStream_t st = (cudaStream_t)stream;
+  const size_t smem = (size_t)std::min<int64_t>(SELECT_KEYS, (int64_t)a.s.capacity) * 4;
+  FCP_CUDA_CHECK(launch(cache_select_kernel, dim3((unsigned)c.hkv, (unsigned)batch->B), SELECT_THREADS, smem, st, a));
+  const dim3 grid((unsigned)((keep + c.page_tokens - 1) / c.page_tokens), (unsigned)c.hkv, (unsigned)batch->B);
+  if (c.head_dim == 128) {
+    if (c.kind == FCP_CACHE_E4M3) FCP_CUDA_CHECK(launch(cache_move_kernel<128, FCP_CACHE_E4M3>, grid, MOVE_THREADS, 0, st, a));
+    else FCP_CUDA_CHECK(launch(cache_move_kernel<128, FCP_CACHE_INT8>, grid, MOVE_THREADS, 0, st, a));
+  } else {
+    if (c.kind == FCP_CACHE_E4M3) FCP_CUDA_CHECK(launch(cache_move_kernel<64, FCP_CACHE_E4M3>, grid, MOVE_THREADS, 0, st, a));
+    else FCP_CUDA_CHECK(launch(cache_move_kernel<64, FCP_CACHE_INT8>, grid, MOVE_THREADS, 0, st, a));
+  }
+  return FCP_OK;
+}

@@ -11,38 +11,14 @@
 
 #include "fcp_bwd.cuh"
 #include "fcp_fwd.cuh"
+#include "fcp_launch.cuh"
 
 using namespace fcp;
-
-#define FCP_CUDA_CHECK(expr)                                                             \
-  do {                                                                                   \
-    cudaError_t e_ = (expr);                                                             \
-    if (e_ != cudaSuccess) {                                                             \
-      fcp_set_error("%s failed: %s (%s:%d)", #expr, cudaGetErrorString(e_), __FILE__, __LINE__); \
-      return FCP_ERR_CUDA;                                                               \
-    }                                                                                    \
-  } while (0)
 
 // ---------------------------------------------------------------------------------------------
 // Tensor maps
 // ---------------------------------------------------------------------------------------------
 namespace {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (fn) return fn;
-  void* p = nullptr;
-  cudaDriverEntryPointQueryResult qres;
-  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) != cudaSuccess ||
-      qres != cudaDriverEntryPointSuccess)
-    return nullptr;
-  fn = (EncodeTiledFn)p;
-  return fn;
-}
 
 // bf16 tensor [T][H][D]; box = 64 columns x 1 head x `box_rows` tokens, 128-byte swizzle, zero fill.
 int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int D, int box_rows) {
@@ -67,27 +43,6 @@ int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int D, int 
     return FCP_ERR_CUDA;
   }
   return FCP_OK;
-}
-
-// Launch that may begin while the kernel before it in the stream still runs (grid_begin of sm100_ptx.cuh); hides the
-// launch latency and the set-up of barriers and tensor memory: 4K-token step, seven queue entries before and four launches now, 59 -> 50 us.
-template <typename... P, typename... A>
-cudaError_t launch_when(bool early, void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = early ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-}
-template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
-  return launch_when(true, kernel, grid, threads, smem, st, args...);
 }
 
 // Records an event pair around a kernel launch when the plan is in profiling mode.

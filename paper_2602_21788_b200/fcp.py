@@ -31,6 +31,8 @@ EXPORTS = ["fcp_plan_strategy", "fcp_plan_blocks", "fcp_plan_blocks_spans", "fcp
            "fcp_attn_fwd_fused", "fcp_lse_merge", "fcp_attn_bwd", "fcp_attn_bwd_heads",
            "fcp_host_workspace_bytes", "fcp_attn_fwd_bwd_host", "fcp_last_device_status", "fcp_plan_set_profiling",
            "fcp_plan_kernel_ms", "fcp_noalloc_bytes_needed", "fcp_attn_bwd_noalloc", "fcp_noalloc_device_status",
+           "fcp_rope_init", "fcp_rope_fwd", "fcp_rope_bwd", "fcp_cache_create", "fcp_cache_destroy",
+           "fcp_cache_device_status", "fcp_cache_append", "fcp_cache_attn_workspace_bytes", "fcp_cache_attn", "fcp_cache_evict",
            "fcp_selftest_bounded_wait", "fcp_status_string",
            "fcp_last_error_message"]
 
@@ -42,6 +44,28 @@ class FcpParams(C.Structure):
 class FcpCostCoeffs(C.Structure):
     _fields_ = [("alpha1", C.c_double), ("alpha2", C.c_double), ("alpha3", C.c_double), ("beta1", C.c_double),
                 ("beta2", C.c_double), ("v", C.c_double), ("eta", C.POINTER(C.c_double))]
+
+
+class FcpRopeConfig(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("original_length", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("magnitude", C.c_double)]
+
+
+class FcpRopeTable(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float),
+                ("turn", C.c_uint64 * 64)]
+
+
+class FcpCacheConfig(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("weight", C.c_void_p), ("status", C.c_void_p), ("n_pages", C.c_int32), ("page_tokens", C.c_int32),
+                ("hkv", C.c_int32), ("head_dim", C.c_int32), ("kind", C.c_int32)]
+
+
+class FcpCacheBatch(C.Structure):
+    _fields_ = [("B", C.c_int32), ("rows", C.c_int32), ("max_new", C.c_int32), ("table_width", C.c_int32),
+                ("page_table", C.c_void_p), ("length", C.c_void_p), ("row_offset", C.c_void_p)]
 
 
 class FcpError(RuntimeError):
@@ -89,6 +113,18 @@ def lib() -> C.CDLL:
     L.fcp_noalloc_bytes_needed.argtypes = [vp, i64p]
     L.fcp_attn_bwd_noalloc.argtypes = [vp] * 11
     L.fcp_noalloc_device_status.argtypes = [i32p]
+    L.fcp_rope_init.argtypes = [C.POINTER(FcpRopeConfig), C.POINTER(FcpRopeTable)]
+    for f in (L.fcp_rope_fwd, L.fcp_rope_bwd):
+        f.argtypes = [C.POINTER(FcpRopeTable), C.c_int64, vp, C.c_int64, C.c_int32, vp, C.c_int64, C.c_int32, vp, C.c_int64, vp,
+                      C.c_int64, vp, vp, vp, C.c_int32, vp]
+    batch = C.POINTER(FcpCacheBatch)
+    L.fcp_cache_create.argtypes = [C.POINTER(FcpCacheConfig), C.POINTER(vp)]
+    L.fcp_cache_destroy.argtypes = [vp]
+    L.fcp_cache_device_status.argtypes = [vp, i32p]
+    L.fcp_cache_append.argtypes = [vp, batch, vp, C.c_int64, vp, C.c_int64, vp]
+    L.fcp_cache_attn_workspace_bytes.argtypes = [vp, batch, C.c_int32, i64p]
+    L.fcp_cache_attn.argtypes = [vp, batch, vp, C.c_int64, C.c_int32, C.c_float, vp, vp, C.c_int32, vp, C.c_int64, vp]
+    L.fcp_cache_evict.argtypes = [vp, batch, C.c_int32, C.c_int32, C.c_int32, vp, C.c_int32, vp, vp, vp]
     L.fcp_selftest_bounded_wait.argtypes = [C.c_uint32, i32p, vp]
     L.fcp_status_string.argtypes = [C.c_int]
     L.fcp_status_string.restype = C.c_char_p
@@ -280,6 +316,180 @@ def fcp_attn_bwd_heads(plan: Plan, q, k, v, o, d_o, lse, kv_head_begin, kv_head_
 def fcp_attn_fwd_bwd_host(plan: Plan, q, k, v, d_o, o, lse, dq, dk, dv, workspace, workspace_bytes, stream=0):
     _check(lib().fcp_attn_fwd_bwd_host(plan.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(d_o), _ptr(o), _ptr(lse), _ptr(dq),
                                        _ptr(dk), _ptr(dv), _ptr(workspace), int(workspace_bytes), C.c_void_p(stream)))
+
+
+# ---------------------------------------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------------------------------------
+ROPE_LAYOUTS = dict(half=0, interleaved=1)
+ROPE_SCALINGS = dict(none=0, linear=1, ntk=2, yarn=3, wavelength=4)
+
+
+class RopeTable:
+    """Frequencies of fcp_rope_fwd / fcp_rope_bwd (fcp_rope_init)."""
+
+    def __init__(self, head_dim, rotary_dim=None, layout="half", base=10000.0, scaling="none", factor=1.0, original_length=0.0,
+                 low=0.0, high=0.0, magnitude=0.0):
+        config = FcpRopeConfig(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), _named(ROPE_LAYOUTS, layout),
+                               _named(ROPE_SCALINGS, scaling), float(base), float(factor), float(original_length), float(low),
+                               float(high), float(magnitude))
+        self.struct = FcpRopeTable()
+        _check(lib().fcp_rope_init(C.byref(config), C.byref(self.struct)))
+        self.ref = C.byref(self.struct)
+
+    def frequencies(self) -> np.ndarray:
+        """Radians per token of each pair, as the table holds them."""
+        turns = np.asarray(self.struct.turn[:self.struct.rotary_dim // 2], dtype=np.uint64)
+        return turns.astype(np.float64) * (2.0 * np.pi / 2.0 ** 64)
+
+
+def _named(names: dict, value) -> int:
+    """The number of a name; a number as it is."""
+    if isinstance(value, str):
+        if value not in names:
+            raise ValueError(f"{value!r} is none of {', '.join(names)}")
+        return names[value]
+    return int(value)
+
+
+def _heads(x, head_dim, name):
+    """Rows, heads and row stride of a tensor [rows][heads][head_dim] whose heads are contiguous; None has no heads."""
+    if x is None:
+        return None, 0, 0
+    rows, heads, d = x.shape
+    s0, s1, s2 = x.stride()
+    if x.dtype.itemsize != 2 or d != head_dim or (s2 != 1 and d > 1) or (s1 != head_dim and heads > 1):
+        raise ValueError(f"{name}: a bf16 tensor [rows][heads][{head_dim}] with contiguous heads is wanted")
+    return rows, heads, s0 if rows > 1 else heads * head_dim
+
+
+def _i32_ptr(x, n, name):
+    """Address of a contiguous int32 device tensor of n entries (None: NULL)."""
+    if x is None:
+        return None
+    if x.dtype.itemsize != 4 or x.is_floating_point() or not x.is_contiguous() or x.numel() != n:
+        raise ValueError(f"{name}: a contiguous int32 tensor of {n} entries is wanted")
+    return x.data_ptr()
+
+
+def _rope(call, table, q, k, q_out, k_out, positions, row_offset, length, stream):
+    d = table.struct.head_dim
+    rows, hq, qs = _heads(q, d, "q")
+    k_rows, hkv, ks = _heads(k, d, "k")
+    T = rows if rows is not None else k_rows if k_rows is not None else 0
+    q_out_rows, hq_out, qos = _heads(q_out, d, "q_out")
+    k_out_rows, hkv_out, kos = _heads(k_out, d, "k_out")
+    if (hq_out, hkv_out) != (hq, hkv) or any(r not in (None, T) for r in (k_rows, q_out_rows, k_out_rows)):
+        raise ValueError("q, k, q_out, k_out differ in rows or heads")
+    B = 0 if row_offset is None else row_offset.numel() - 1
+    _check(call(table.ref, T, q.data_ptr() if hq else None, qs, hq, k.data_ptr() if hkv else None, ks, hkv,
+                q_out.data_ptr() if hq else None, qos, k_out.data_ptr() if hkv else None, kos,
+                _i32_ptr(positions, T, "positions"), _i32_ptr(row_offset, B + 1, "row_offset"), _i32_ptr(length, B, "length"),
+                B, stream))
+
+
+def fcp_rope_fwd(table: RopeTable, q, k, q_out, k_out, positions=None, row_offset=None, length=None, stream=0):
+    """q, k and their outputs: bf16 [T][heads][head_dim] (slices of wider rows are fine; outputs may be the inputs); either
+    pair may be None.  Positions are given, or follow from the batch's row_offset (and the sequences' lengths)."""
+    _rope(lib().fcp_rope_fwd, table, q, k, q_out, k_out, positions, row_offset, length, stream)
+
+
+def fcp_rope_bwd(table: RopeTable, dq, dk, dq_in, dk_in, positions=None, row_offset=None, length=None, stream=0):
+    """Gradients of the outputs dq, dk -> gradients of the inputs dq_in, dk_in; arguments as in fcp_rope_fwd."""
+    _rope(lib().fcp_rope_bwd, table, dq, dk, dq_in, dk_in, positions, row_offset, length, stream)
+
+
+# ---------------------------------------------------------------------------------------------------------
+# Cache of keys and values in 8 bits
+# ---------------------------------------------------------------------------------------------------------
+CACHE_KINDS = dict(e4m3=0, int8=1)
+FCP_CACHE_MIN_SCALE, FCP_CACHE_MAX_SCALE = 2.0 ** -100, 2.0 ** 122
+FCP_CACHE_BAD_LENGTH, FCP_CACHE_BAD_ROWS, FCP_CACHE_BAD_PAGE, FCP_CACHE_BAD_SCALE = 1001, 1002, 1003, 1004
+
+
+class Cache:
+    """Owns an fcp_cache handle over the caller's pages: k, v [n_pages][hkv][page_tokens][head_dim] (float8_e4m3fn or int8),
+    k_scale, v_scale fp32 [n_pages][hkv], status int32 [4] (zeroed), weight fp32 [n_pages][hkv][page_tokens] or None."""
+
+    def __init__(self, k, v, k_scale, v_scale, status, weight=None, kind=None):
+        n_pages, hkv, page_tokens, head_dim = k.shape
+        name = str(k.dtype)
+        if kind is None:
+            kind = "int8" if name.endswith("int8") and not name.endswith("uint8") else "e4m3"
+        for x, shape, size in ((k, k.shape, 1), (v, k.shape, 1), (k_scale, (n_pages, hkv), 4), (v_scale, (n_pages, hkv), 4),
+                               (weight, (n_pages, hkv, page_tokens), 4), (status, (4,), 4)):
+            if x is not None and (tuple(x.shape) != tuple(shape) or x.dtype.itemsize != size or not x.is_contiguous()):
+                raise ValueError(f"a contiguous tensor {tuple(shape)} of {size}-byte values is wanted, not {tuple(x.shape)} {x.dtype}")
+        self.hkv, self.head_dim, self.page_tokens, self.n_pages = hkv, head_dim, page_tokens, n_pages
+        self.tensors = (k, v, k_scale, v_scale, status, weight)          # the pages live as long as the handle
+        ptr = [None if x is None else x.data_ptr() for x in (k, v, k_scale, v_scale, weight, status)]
+        config = FcpCacheConfig(*ptr, n_pages, page_tokens, hkv, head_dim, _named(CACHE_KINDS, kind))
+        self.handle = C.c_void_p()
+        _check(lib().fcp_cache_create(C.byref(config), C.byref(self.handle)))
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h is not None and h.value and _lib is not None:
+            _lib.fcp_cache_destroy(h)
+            self.handle = None
+
+    def device_status(self):
+        st = np.zeros(4, dtype=np.int32)
+        _check(lib().fcp_cache_device_status(self.handle, st.ctypes.data_as(C.POINTER(C.c_int32))))
+        return st
+
+
+class CacheBatch:
+    """The sequences a call works on: page_table int32 [B][width], length int32 [B] (new tokens included), row_offset int32 [B+1]
+    (device tensors, read when the call runs); rows and max_new bound them (default for max_new: rows)."""
+
+    def __init__(self, page_table, length, row_offset=None, rows=0, max_new=None):
+        B, width = page_table.shape
+        self.tensors = (page_table, length, row_offset)
+        self.struct = FcpCacheBatch(B, int(rows), int(rows if max_new is None else max_new), width,
+                                    _i32_ptr(page_table, B * width, "page_table"), _i32_ptr(length, B, "length"),
+                                    _i32_ptr(row_offset, B + 1, "row_offset"))
+        self.ref = C.byref(self.struct)
+
+
+def _rows(x, batch, heads, head_dim, name):
+    rows, h, stride = _heads(x, head_dim, name)
+    if rows != batch.struct.rows or h != heads:
+        raise ValueError(f"{name}: {rows} rows of {h} heads, the batch has {batch.struct.rows} rows of {heads}")
+    return x.data_ptr(), stride
+
+
+def fcp_cache_append(cache: Cache, batch: CacheBatch, k, v, stream=0):
+    kp, ks = _rows(k, batch, cache.hkv, cache.head_dim, "k")
+    vp, vs = _rows(v, batch, cache.hkv, cache.head_dim, "v")
+    _check(lib().fcp_cache_append(cache.handle, batch.ref, kp, ks, vp, vs, stream))
+
+
+def fcp_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, hq) -> int:
+    v = C.c_int64(0)
+    _check(lib().fcp_cache_attn_workspace_bytes(cache.handle, batch.ref, int(hq), C.byref(v)))
+    return v.value
+
+
+def fcp_cache_attn(cache: Cache, batch: CacheBatch, q, o, lse, workspace, workspace_bytes, scale=0.0, accumulate=False, stream=0):
+    hq = q.shape[1]
+    qp, qs = _rows(q, batch, hq, cache.head_dim, "q")
+    if o.shape != q.shape or o.dtype.itemsize != 2 or not o.is_contiguous():
+        raise ValueError("o: a contiguous bf16 tensor of q's shape is wanted")
+    if tuple(lse.shape) != (q.shape[0], hq) or lse.dtype.itemsize != 4 or not lse.is_contiguous():
+        raise ValueError("lse: a contiguous fp32 tensor [rows][hq] is wanted")
+    _check(lib().fcp_cache_attn(cache.handle, batch.ref, qp, qs, hq, float(scale), o.data_ptr(), lse.data_ptr(), int(bool(accumulate)),
+                                _ptr(workspace), int(workspace_bytes), stream))
+
+
+def fcp_cache_evict(cache: Cache, batch: CacheBatch, n_sink, n_heavy, n_recent, dst_table, new_length, kept, stream=0):
+    B, width = dst_table.shape
+    if B != batch.struct.B:
+        raise ValueError("dst_table and the batch differ in their number of sequences")
+    keep = int(n_sink) + int(n_heavy) + int(n_recent)
+    _check(lib().fcp_cache_evict(cache.handle, batch.ref, int(n_sink), int(n_heavy), int(n_recent),
+                                 _i32_ptr(dst_table, B * width, "dst_table"), width, _i32_ptr(new_length, B, "new_length"),
+                                 _i32_ptr(kept, B * cache.hkv * keep, "kept"), stream))
 
 
 FCP_NOALLOC_MAX_BYTES = 32 << 20

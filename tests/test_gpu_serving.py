@@ -1,0 +1,724 @@
+"""GPU tests of rotary positions and of the paged 8-bit cache against the float64 definitions of oracle/serving_ref.py.
+
+Tolerances count roundings: half a step of bf16 is 2^-8 relative, of a half 2^-11, of fp32 2^-24."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import serving_ref as R
+from paper_2602_21788_b200 import build, fcp
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+BF16, HALF, F32 = 2.0 ** -8, 2.0 ** -11, 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    build.build()
+    torch.cuda.set_device(0)
+
+
+def dev(a, dtype=torch.int32):
+    return torch.as_tensor(np.ascontiguousarray(a)).to(dtype).cuda()
+
+
+def bf16(rng, *shape, scale=1.0):
+    return torch.as_tensor(rng.standard_normal(shape) * scale).to(torch.bfloat16)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+# ---------------------------------------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------------------------------------
+def check_rope(got, x, positions, freqs, rotary, layout, magnitude, backward=False):
+    x = f64(x)
+    want = R.rope(x, positions, freqs, rotary, layout, magnitude, backward)
+    pair = np.abs(x).max(axis=-1, keepdims=True) * 2 * magnitude        # bounds |x| + |y| of any pair
+    # the angle is exact to 2^-24 of a half turn, sine and cosine to a few 2^-24, then two products and a sum in fp32
+    assert np.all(np.abs(f64(got) - want) <= BF16 * np.abs(want) + 24 * F32 * pair + 1e-40)
+    assert np.array_equal(f64(got)[..., rotary:], x[..., rotary:])
+
+
+@pytest.mark.parametrize("head_dim,rotary", [(64, 64), (64, 32), (64, 2), (64, 30), (128, 128), (128, 64), (128, 126), (128, 16), (128, 48)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("backward", [False, True])
+def test_rope_packed_batch(head_dim, rotary, layout, backward):
+    rng = np.random.default_rng(head_dim + rotary)
+    off = np.cumsum([0, 1, 0, 37, 5, 0, 300, 2])
+    T, hq, hkv = int(off[-1]), 6, 2
+    table = fcp.RopeTable(head_dim, rotary, layout, base=10000.0, scaling="yarn", factor=4.0, original_length=2048.0)
+    freqs, m = R.rope_frequencies(rotary, 10000.0, "yarn", 4.0, 2048.0), R.rope_magnitude("yarn", 4.0)
+    q, k = bf16(rng, T, hq, head_dim).cuda(), bf16(rng, T, hkv, head_dim).cuda()
+    q_out, k_out = torch.full_like(q, 7), torch.full_like(k, 7)
+    call = fcp.fcp_rope_bwd if backward else fcp.fcp_rope_fwd
+    call(table, q, k, q_out, k_out, row_offset=dev(off), stream=stream())
+    pos = np.concatenate([np.arange(b - a) for a, b in zip(off, off[1:])])
+    check_rope(q_out, q, pos, freqs, rotary, layout, m, backward)
+    check_rope(k_out, k, pos, freqs, rotary, layout, m, backward)
+    # positions of sequences that go on, in place, on slices of wider rows
+    length = np.diff(off) + np.asarray([100000, 5, 0, 2 ** 31 - 400, 3, 1, 70000])
+    wide = torch.full((T, hq + 2 * hkv, head_dim), 3.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, :hq], wide[:, hq:hq + hkv] = q, k
+    call(table, wide[:, :hq], wide[:, hq:hq + hkv], wide[:, :hq], wide[:, hq:hq + hkv], row_offset=dev(off), length=dev(length), stream=stream())
+    far = np.concatenate([np.arange(b - a) + int(n) - (b - a) for a, b, n in zip(off, off[1:], length)])
+    check_rope(wide[:, :hq], q, far, freqs, rotary, layout, m, backward)
+    check_rope(wide[:, hq:hq + hkv], k, far, freqs, rotary, layout, m, backward)
+    assert bool((wide[:, hq + hkv:] == 3).all())
+    # given positions, negative ones among them; one tensor alone; rows at an address that allows no wide access
+    pos = rng.integers(-2 ** 31, 2 ** 31, T)
+    buf = torch.zeros(T * hkv * head_dim + 1, dtype=torch.bfloat16, device="cuda")
+    odd = buf[1:].view(T, hkv, head_dim)
+    call(table, None, k, None, odd, positions=dev(pos), stream=stream())
+    check_rope(odd, k, pos, freqs, rotary, layout, m, backward)
+    call(table, q, None, q_out, None, positions=dev(pos), stream=stream())
+    check_rope(q_out, q, pos, freqs, rotary, layout, m, backward)
+
+
+@pytest.mark.parametrize("T", [1, 3, 591, 592, 593, 2000])
+def test_rope_rows_behind_the_batch_stay(T):
+    rng = np.random.default_rng(T)
+    q = bf16(rng, T + 3, 2, 64).cuda()
+    table, out = fcp.RopeTable(64), torch.full((T + 3, 2, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    first = min(2, T - 1)
+    fcp.fcp_rope_fwd(table, q, None, out, None, row_offset=dev([first, T]), stream=stream())
+    assert bool((out[T:] == 5).all()) and bool((out[:first] == 5).all())
+    check_rope(out[first:T], q[first:T], np.arange(T - first), R.rope_frequencies(64, 10000.0), 64, "half", 1.0)
+
+
+def test_rope_many_sequences_and_offsets_that_make_no_sense():
+    rng = np.random.default_rng(5)
+    n = rng.integers(0, 3, 70001)
+    off = np.concatenate([[0], np.cumsum(n)])
+    T = int(off[-1])
+    q = bf16(rng, T, 1, 64).cuda()
+    table, out = fcp.RopeTable(64), torch.empty_like(q)
+    fcp.fcp_rope_fwd(table, q, None, out, None, row_offset=dev(off), stream=stream())
+    pos = np.concatenate([np.arange(i) for i in n])
+    check_rope(out, q, pos, R.rope_frequencies(64, 10000.0), 64, "half", 1.0)
+    # falling or far offsets: whatever comes out, the call ends and stays inside its tensors
+    for bad in ([5, 3, 1, 0], [-2 ** 31, 2 ** 31 - 1, -5, 7], [2 ** 31 - 1] * 4):
+        guard = torch.full((T + 64, 1, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+        fcp.fcp_rope_fwd(table, q, None, guard[:T], None, row_offset=dev(bad), stream=stream())
+        torch.cuda.synchronize()
+        assert bool((guard[T:] == 9).all())
+
+
+def test_rope_gradient_is_that_of_the_forward_call():
+    rng = np.random.default_rng(6)
+    T, rotary = 40, 32
+    table = fcp.RopeTable(64, rotary, "interleaved", scaling="linear", factor=2.0)
+    pos = dev(rng.integers(0, 500, T))
+    x, g = bf16(rng, T, 2, 64).cuda(), bf16(rng, T, 2, 64).cuda()
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    fcp.fcp_rope_fwd(table, x, None, y, None, positions=pos, stream=stream())
+    fcp.fcp_rope_bwd(table, g, None, dx, None, positions=pos, stream=stream())
+    # the map is linear: <dx, e> is the difference <g, rope(x + e) - rope(x)> in float64
+    f, p = R.rope_frequencies(rotary, 10000.0, "linear", 2.0), pos.cpu().numpy()
+    for _ in range(8):
+        e = rng.standard_normal((T, 2, 64))
+        rise = (f64(g) * (R.rope(f64(x) + e, p, f, rotary, "interleaved") - R.rope(f64(x), p, f, rotary, "interleaved"))).sum()
+        assert abs((f64(dx) * e).sum() - rise) <= 2 * BF16 * np.abs(f64(dx) * e).sum() + 1e-9
+    # forward and backward undo each other to two roundings
+    fcp.fcp_rope_bwd(table, y, None, y, None, positions=pos, stream=stream())
+    assert np.all(np.abs(f64(y) - f64(x)) <= 4 * BF16 * np.abs(f64(x)).max(axis=-1, keepdims=True))
+
+
+# ---------------------------------------------------------------------------------------------------------
+# The cache
+# ---------------------------------------------------------------------------------------------------------
+class World:
+    """A cache on the device and the same in float64, with a pool of pages in random order."""
+
+    def __init__(self, seed, kind, page, hkv, d, lengths, weight=True, spare=4, width=None):
+        self.rng = rng = np.random.default_rng(seed)
+        self.kind, self.page, self.hkv, self.d = kind, page, hkv, d
+        need = [-(-n // page) for n in lengths]
+        self.width = max([width or 1] + need)
+        self.n_pages = sum(need) + spare
+        self.order = rng.permutation(self.n_pages)
+        self.table = np.full((len(lengths), self.width), -1)
+        at = 0
+        for b, n in enumerate(need):
+            self.table[b, :n] = self.order[at:at + n]
+            at += n
+        self.free = self.order[at:]
+        self.length = np.asarray(lengths)
+        shape = (self.n_pages, hkv, page, d)
+        self.codes = {n: rng.integers(0, 256, shape).astype(np.uint8) for n in "kv"}       # every code, NaN too
+        self.scale = {n: (2.0 ** rng.integers(-9, -2, shape[:2])).astype(np.float32) for n in "kv"}
+        self.weight = rng.random(shape[:3]).astype(np.float32) if weight else None
+
+    def fill(self, spread=1.0):
+        """Finite values where tokens are; the rest of the pages holds anything."""
+        for b, n in enumerate(self.length):
+            for j in range(-(-n // self.page)):
+                p, m = self.table[b, j], min(self.page, n - j * self.page)
+                for name in "kv":
+                    x = self.rng.standard_normal((self.hkv, m, self.d)) * spread
+                    top = np.abs(x).max(axis=(1, 2))
+                    s = 2.0 ** np.ceil(np.log2(top / R.TOP[self.kind]))
+                    x = torch.as_tensor(x / s[:, None, None])
+                    c = x.float().to(torch.float8_e4m3fn).view(torch.uint8) if self.kind == "e4m3" else x.round().to(torch.int8).view(torch.uint8)
+                    self.codes[name][p, :, :m] = c.numpy()
+                    self.scale[name][p] = s
+        return self
+
+    def up(self):
+        self.k, self.v = (torch.as_tensor(self.codes[n]).cuda() for n in "kv")
+        self.ks, self.vs = (torch.as_tensor(self.scale[n]).cuda() for n in "kv")
+        self.w = None if self.weight is None else torch.as_tensor(self.weight).cuda()
+        self.status = torch.zeros(4, dtype=torch.int32, device="cuda")
+        self.cache = fcp.Cache(self.k, self.v, self.ks, self.vs, self.status, weight=self.w, kind=self.kind)
+        return self
+
+    def batch(self, new, rows=None, max_new=None, length=None):
+        self.off = np.concatenate([[0], np.cumsum(new)])
+        rows = int(self.off[-1]) if rows is None else rows
+        return fcp.CacheBatch(dev(self.table), dev(self.length if length is None else length), dev(self.off), rows=rows,
+                              max_new=int(max(list(new) + [0])) if max_new is None else max_new)
+
+    def state(self):
+        return dict(k=R.code_values(self.kind, self.codes["k"]), v=R.code_values(self.kind, self.codes["v"]),
+                    k_scale=self.scale["k"].astype(np.float64), v_scale=self.scale["v"].astype(np.float64),
+                    weight=None if self.weight is None else self.weight.astype(np.float64))
+
+    def now(self):
+        k, v = self.k.view(torch.uint8).cpu().numpy(), self.v.view(torch.uint8).cpu().numpy()
+        return dict(k=R.code_values(self.kind, k), v=R.code_values(self.kind, v), k_scale=f64(self.ks), v_scale=f64(self.vs),
+                    weight=None if self.w is None else f64(self.w))
+
+
+def same(a, b):
+    for n in a:
+        assert (a[n] is None) == (b[n] is None)
+        if a[n] is not None:
+            assert np.array_equal(a[n], b[n], equal_nan=True), n
+
+
+CASES = [("e4m3", 16, 2, 64), ("int8", 16, 1, 128), ("e4m3", 32, 3, 128), ("int8", 64, 2, 64), ("e4m3", 128, 2, 128), ("int8", 128, 2, 128),
+         ("e4m3", 128, 1, 64)]
+
+
+@pytest.mark.parametrize("kind,page,hkv,d", CASES)
+@pytest.mark.parametrize("new", [[1], [1, 1, 1, 0, 1], [0, 0], [5, 0, 130, 1, 63], [300, 17, 1]])
+def test_append_bit_for_bit(kind, page, hkv, d, new):
+    rng = np.random.default_rng(len(new))
+    before = [int(rng.integers(0, 3 * page)) if b % 3 else [0, page, page - 1, 2 * page + 1][b % 4] for b in range(len(new))]
+    w = World(11, kind, page, hkv, d, [a + n for a, n in zip(before, new)])
+    # a clean start: stale NaN codes may lie in pages, but the earlier tokens are values
+    for n in "kv":
+        w.codes[n] = np.where((w.codes[n] & 127) == 127, 3, w.codes[n]).astype(np.uint8) if kind == "e4m3" else np.where(w.codes[n] == 128, 3, w.codes[n]).astype(np.uint8)
+    w.up()
+    rows = int(np.sum(new))
+    # sizes from far below to far above what the pages hold
+    k = (bf16(w.rng, rows + 2, hkv, d) * torch.as_tensor(2.0 ** w.rng.integers(-12, 6, (rows + 2, hkv, 1)))).to(torch.bfloat16)
+    v = bf16(w.rng, rows + 2, hkv, d)
+    batch = w.batch(new, rows=rows + 2, max_new=max(new))
+    state = w.state()
+    fcp.fcp_cache_append(w.cache, batch, k.cuda(), v.cuda(), stream=stream())
+    R.append(kind, state, w.table, w.length, w.off, f64(k), f64(v))
+    same(w.now(), state)
+    fcp.fcp_cache_append(w.cache, batch, k.cuda(), v.cuda(), stream=stream())           # again: nothing changes
+    same(w.now(), state)
+    assert w.cache.device_status().tolist() == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_append_of_unusual_values(kind):
+    w = World(12, kind, 16, 1, 64, [16, 20, 16, 3, 7, 2])
+    w.up()
+    new = [16, 4, 16, 3, 1, 2]
+    x = torch.zeros(sum(new), 1, 64)
+    x[0:16] = torch.tensor([float("inf"), -float("inf"), float("nan"), 3e38]).repeat(16)
+    x[16:20] = 0.0
+    x[20:36] = 1e-38
+    x[36:39] = float("nan")
+    x[39] = -448 * 2.0 ** 20
+    x[40:42, 0, 0] = 127 * 2.0 ** -130            # a subnormal bf16
+    x = x.to(torch.bfloat16)
+    state = w.state()
+    for n in "kv":
+        state[n][w.table[1][1]], w.codes[n][w.table[1][1]] = 0, 0                       # its earlier tokens
+        state[n][w.table[4][0]], w.codes[n][w.table[4][0]] = 1.0, 0x38 if kind == "e4m3" else 1
+    w.up()
+    batch = w.batch(new)
+    fcp.fcp_cache_append(w.cache, batch, x.cuda(), x.cuda(), stream=stream())
+    R.append(kind, state, w.table, w.length, w.off, f64(x), f64(x))
+    same(w.now(), state)
+
+
+def test_append_scales_that_are_no_powers_of_two():
+    w = World(13, "int8", 32, 2, 64, [40, 9])
+    for n in "kv":
+        w.scale[n] = w.rng.random(w.scale[n].shape).astype(np.float32)
+        w.codes[n] = np.where(w.codes[n] == 128, 0, w.codes[n]).astype(np.uint8)
+    w.up()
+    x = bf16(w.rng, 5, 2, 64, scale=20)
+    state = w.state()
+    fcp.fcp_cache_append(w.cache, w.batch([4, 1]), x.cuda(), x.cuda(), stream=stream())
+    R.append("int8", state, w.table, w.length, w.off, f64(x), f64(x))
+    now = w.now()
+    assert np.array_equal(now["k_scale"], state["k_scale"])
+    # x / scale is rounded to fp32 before it is rounded to a code: at most one code apart, and only next to a border
+    for n in "kv":
+        assert np.abs(now[n] - state[n]).max() <= 1 and (now[n] != state[n]).mean() < 1e-3
+
+
+def check_attn(w, state, r, o, lse, rows):
+    """Against the definition: the rounding of the weights to halves (2^-11), of o to bf16 (2^-8), and the fp32 sums of the scores
+    (D products of size at most `size` in all, each sum truncated at 2^-23)."""
+    off = w.off
+    for name, x in (("o", o), ("lse", lse)):
+        assert x.shape[0] >= rows
+    score = w.d * 2 * F32 * r["size"] + 2.0 ** -20
+    got, got_lse = f64(o)[:rows], f64(lse)[:rows]
+    dead = ~np.isfinite(r["lse"])
+    assert np.array_equal(dead, got_lse == -np.inf)
+    assert np.all(got[dead] == 0)
+    live = ~dead
+    assert np.all(np.abs(got_lse - r["lse"])[live] <= (score + 4 * F32 * np.abs(np.where(live, r["lse"], 0)))[live])
+    bound = BF16 * np.abs(r["o"]) + (HALF + 2 * score[..., None]) * r["spread"] * (1 + BF16) + 1e-30
+    assert np.all(np.abs(got - r["o"]) <= bound), np.max(np.abs(got - r["o"]) / bound)
+    assert off[-1] == rows
+
+
+def attend(w, new, hq, accumulate=False, scale=0.0, spare=2, stride_heads=0, max_new=None):
+    rows = int(np.sum(new))
+    q = bf16(w.rng, rows + spare, hq + stride_heads, w.d)[:, :hq]
+    batch = w.batch(new, rows=rows + spare, max_new=max_new)
+    o = torch.full((rows + spare, hq, w.d), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((rows + spare, hq), 5.0, device="cuda")
+    n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, hq)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    q_dev = torch.zeros(rows + spare, hq + stride_heads, w.d, dtype=torch.bfloat16, device="cuda")
+    q_dev[:, :hq] = q.cuda()
+    fcp.fcp_cache_attn(w.cache, batch, q_dev[:, :hq], o, lse, ws, n, scale=scale, accumulate=accumulate, stream=stream())
+    torch.cuda.synchronize()
+    assert bool((o[rows:] == 3).all()) and bool((lse[rows:] == 5).all())
+    return q, o, lse, rows
+
+
+@pytest.mark.parametrize("kind,page,hkv,d", CASES)
+@pytest.mark.parametrize("group,new,before", [
+    (1, [1], [0]), (1, [1, 1, 1], [15, 16, 127]), (4, [1, 0, 1, 1], [700, 5, 128, 1290]), (8, [2, 2], [300, 0]),
+    (5, [4, 1, 3], [1000, 64, 3]), (3, [20, 1], [250, 900]), (8, [17, 40, 2], [130, 0, 5]),
+])
+def test_attention_over_the_cache(kind, page, hkv, d, group, new, before):
+    w = World(21, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    q, o, lse, rows = attend(w, new, hkv * group, stride_heads=1)
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    check_attn(w, None, r, o, lse, rows)
+    assert w.cache.device_status().tolist() == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("kind,page,hkv,d", [("e4m3", 16, 2, 64), ("int8", 32, 2, 128), ("e4m3", 128, 1, 128)])
+@pytest.mark.parametrize("group,new,before", [(1, [1, 1], [5, 700]), (4, [3, 0, 1], [500, 9, 0]), (8, [5, 30], [1100, 2])])
+def test_weights_that_attention_leaves(kind, page, hkv, d, group, new, before):
+    w = World(22, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    state, was = w.state(), w.now()["weight"]
+    q, o, lse, rows = attend(w, new, hkv * group, accumulate=True)
+    r = R.attention(state, w.table, w.length, w.off, f64(q)[:rows])
+    check_attn(w, None, r, o, lse, rows)
+    want, tol = was.copy(), F32 * 4 * np.abs(was) + 1e-30
+    score = w.d * 2 * F32 * r["size"].max() + 2.0 ** -20
+    for b, t in enumerate(w.length):
+        for p in range(t):
+            page_id, slot = w.table[b][p // page], p % page
+            want[page_id, :, slot] += r["weights"][b][:, p]
+            tol[page_id, :, slot] += r["weights"][b][:, p] * (3 * score + 64 * F32)
+    now = w.now()["weight"]
+    assert np.all(np.abs(now - want) <= tol)                      # places without tokens stay as they were
+    # the same call on the same start gives the same bits
+    w2 = World(22, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    attend(w2, new, hkv * group, accumulate=True)
+    assert np.array_equal(w2.now()["weight"], now)
+
+
+def test_long_ragged_batch_is_split_and_joined():
+    lengths = [20011, 1, 130, 0, 4097, 33, 700]
+    w = World(23, "e4m3", 16, 2, 128, lengths).fill().up()
+    new = [1, 1, 1, 0, 1, 1, 1]
+    q, o, lse, rows = attend(w, new, 8)
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    check_attn(w, None, r, o, lse, rows)
+    a, b = o.clone(), lse.clone()
+    w.rng = np.random.default_rng(99)
+    q1, o1, lse1, _ = attend(w, new, 8)
+    w.rng = np.random.default_rng(99)
+    q2, o2, lse2, _ = attend(w, new, 8)
+    assert torch.equal(o1, o2) and torch.equal(lse1, lse2) and not torch.equal(o1, a)
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(3)
+    lengths = rng.integers(0, 40, 700)
+    lengths[::7] = 0
+    w = World(24, "int8", 16, 1, 64, lengths).fill().up()
+    new = np.minimum(lengths, 1)
+    new[5::70] = 0
+    q, o, lse, rows = attend(w, new, 2)
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    check_attn(w, None, r, o, lse, rows)
+
+
+def test_rows_that_see_nothing():
+    w = World(25, "e4m3", 16, 2, 64, [0, 3, 0]).fill().up()
+    q, o, lse, rows = attend(w, [2, 5, 1], 4)                     # more new rows than tokens: the first ones are no tokens
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    assert np.isneginf(r["lse"]).sum() == 4 * 5
+    check_attn(w, None, r, o, lse, rows)
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_nan_values_behind_and_among_the_new_tokens(new):
+    """What no row may see must not reach it: stale NaN codes behind the length, and a NaN key or value of a later new token."""
+    w = World(26, "e4m3", 16, 1, 128, [117 + new, 64 + new]).fill()
+    place = lambda b, p: (w.table[b][p // 16], 0, p % 16)
+    at = 117 + max(new - 3, 0)
+    w.codes["v"][place(0, at)][::5] = 0x7f
+    w.codes["k"][place(1, 64 + new - 1)][3] = 0xff
+    w.up()
+    q, o, lse, rows = attend(w, [new, new], 2)
+    with np.errstate(invalid="ignore"):
+        r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    first = at - 117                                              # row of sequence 0 that first sees the NaN value
+    got = f64(o)[:rows]
+    assert np.isnan(got[first:new, :, ::5]).all()
+    assert np.isnan(got[2 * new - 1]).all() and np.isnan(f64(lse)[2 * new - 1]).all()
+    rest = np.ones(got.shape, bool)
+    rest[first:new, :, ::5] = False
+    rest[2 * new - 1] = False
+    assert not np.isnan(got[rest]).any()
+    assert np.all(np.abs(got - r["o"])[rest] <= (BF16 * np.abs(r["o"]) + 2 * HALF * np.nan_to_num(r["spread"], nan=1.0) + 1e-3 * np.nan_to_num(r["spread"], nan=1.0))[rest])
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_scales_of_very_different_size(kind):
+    w = World(27, kind, 16, 1, 64, [400]).fill()
+    for i, p in enumerate(w.table[0]):
+        w.scale["v"][p] *= 2.0 ** (-40 + 4 * (i % 20))
+        w.scale["k"][p] *= 2.0 ** -(i % 5)
+    w.up()
+    q, o, lse, rows = attend(w, [1], 3)
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    check_attn(w, None, r, o, lse, rows)
+
+
+def test_queries_of_unusual_size():
+    w = World(28, "int8", 16, 1, 64, [50, 50, 50, 50]).fill().up()
+    rows = 4
+    q = bf16(w.rng, rows, 1, 64)
+    q[0] *= 2.0 ** -130
+    q[1] *= 2.0 ** 12
+    q[2] = 0
+    q[3, 0, 0] = 2.0 ** 9                                         # one large column, the others 2^-20 and less of it
+    q[3, 0, 1:] *= 2.0 ** -12
+    batch = w.batch([1] * 4)
+    o, lse = torch.empty(4, 1, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(4, 1, device="cuda")
+    n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, 1)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    fcp.fcp_cache_attn(w.cache, batch, q.cuda(), o, lse, ws, n, scale=2.0 ** -6, stream=stream())
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q), scale=2.0 ** -6)
+    check_attn(w, None, r, o, lse, rows)
+
+
+def test_what_the_kernels_refuse():
+    """Pages that do not exist, scales out of range, lengths and rows that make no sense: absent, with a status; the rest is right."""
+    w = World(31, "e4m3", 16, 2, 64, [100, 64, 33, 20, 10]).fill()
+    good = World(31, "e4m3", 16, 2, 64, [100, 64, 33, 20, 10]).fill()
+
+    def attn(length, off, rows=6, max_new=2):
+        batch = fcp.CacheBatch(dev(w.table), dev(length), dev(off), rows=rows, max_new=max_new)
+        o = torch.full((rows, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((rows, 4), 5.0, device="cuda")
+        n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, 4)
+        fcp.fcp_cache_attn(w.cache, batch, q, o, lse, torch.empty(n, dtype=torch.uint8, device="cuda"), n, accumulate=True, stream=stream())
+        return f64(o), f64(lse)
+    q = bf16(w.rng, 6, 4, 64).cuda()
+    ref = R.attention(good.state(), good.table, good.length, [0, 1, 2, 3, 4, 5], f64(q))
+    bad_rows = lambda got, rows: [i for i in rows if not np.allclose(got[1][i], ref["lse"][i], atol=1e-4)]
+    for length, off, code, seq, untouched in [
+        ([100, 64, 33, -1, 10], [0, 1, 2, 3, 4, 5], fcp.FCP_CACHE_BAD_LENGTH, 3, [3]),
+        ([100, 10 ** 6, 33, 20, 10], [0, 1, 2, 3, 4, 5], fcp.FCP_CACHE_BAD_LENGTH, 1, [1]),
+        ([100, 64, 33, 20, 10], [0, 1, 2, 3, 4, 7], fcp.FCP_CACHE_BAD_ROWS, 4, [4, 5]),
+    ]:
+        w.up()
+        got = attn(length, off)
+        assert w.cache.device_status().tolist()[:3] == [fcp.FCP_ERR_INVALID_ARG, code, seq]
+        assert np.all(got[0][untouched] == 3) and np.all(got[1][untouched] == 5)
+        assert bad_rows(got, [i for i in range(5) if i not in untouched]) == []
+    w.up()
+    got = attn([100, 64, 33, 20, 10], [5, 4, 4, 4, 4, 4])                               # falling offsets, then nothing
+    assert w.cache.device_status().tolist()[:3] == [fcp.FCP_ERR_INVALID_ARG, fcp.FCP_CACHE_BAD_ROWS, 0]
+    assert np.all(got[0] == 3)
+    for page in (-1, w.n_pages, 2 ** 31 - 1, -2 ** 31):
+        for name, bad in (("page", page), ("scale", 0.0), ("scale", float("nan")), ("scale", -1.0), ("scale", 1e38)):
+            if name == "scale" and page != -1:
+                continue
+            keep, w.scale["k"] = w.table.copy(), w.scale["k"].copy()
+            if name == "page":
+                w.table[0, 2] = bad
+            else:
+                w.scale["v"], saved = w.scale["v"].copy(), w.scale["v"].copy()
+                w.scale["v"][w.table[0, 2], :] = bad
+            w.up()
+            before = f64(w.w)
+            got = attn([100, 64, 33, 20, 10], [0, 1, 2, 3, 4, 5])
+            assert w.cache.device_status().tolist()[:3] == [fcp.FCP_ERR_INVALID_ARG, fcp.FCP_CACHE_BAD_PAGE if name == "page" else fcp.FCP_CACHE_BAD_SCALE, 0]
+            assert bad_rows(got, [1, 2, 3, 4]) == []
+            # sequence 0 without its tokens 32..47
+            pages = [keep[0][i] for i in range(7) if i != 2]
+            k = np.stack([R.gather(good.state(), "k", pages, 84, h) for h in range(2)])
+            s = np.einsum("hd,htd->ht", f64(q)[0], np.repeat(k, 2, 0)) / 8
+            assert np.allclose(got[1][0], np.log(np.exp(s).sum(-1)), atol=1e-4)
+            assert np.array_equal(f64(w.w)[keep[0][2]], before[keep[0][2]])
+            w.table[:] = keep
+            if name == "scale":
+                w.scale["v"] = saved
+    # append and evict: nothing is written through a page that does not exist
+    keep = w.table.copy()
+    w.table[1, 3] = w.n_pages
+    w.up()
+    k = bf16(w.rng, 5, 2, 64).cuda()
+    was = w.now()
+    fcp.fcp_cache_append(w.cache, fcp.CacheBatch(dev(w.table), dev(w.length), dev([0, 1, 2, 3, 4, 5]), rows=5, max_new=1), k, k, stream=stream())
+    assert w.cache.device_status().tolist()[:3] == [fcp.FCP_ERR_INVALID_ARG, fcp.FCP_CACHE_BAD_PAGE, 1]
+    now = w.now()
+    touched = {int(keep[b][(n - 1) // 16]) for b, n in enumerate(w.length) if b != 1}
+    for p in range(w.n_pages):
+        if p not in touched:
+            assert np.array_equal(now["k"][p], was["k"][p], equal_nan=True) and np.array_equal(now["k_scale"][p], was["k_scale"][p])
+    w.up()
+    dst = dev([[-1], [int(w.free[0])]])
+    new_length, kept = torch.empty(2, dtype=torch.int32, device="cuda"), torch.empty(2, 2, 12, dtype=torch.int32, device="cuda")
+    fcp.fcp_cache_evict(w.cache, fcp.CacheBatch(dev(w.table[:2]), dev([100, -4])), 4, 4, 4, dst, new_length, kept, stream=stream())
+    assert w.cache.device_status().tolist()[0] == fcp.FCP_ERR_INVALID_ARG
+    assert new_length.tolist() == [12, 0] and bool((kept[1] == -1).all())
+    same(w.now(), was)
+
+
+def test_wide_offsets():
+    """A pool of more than 2^32 bytes: the last pages are read and written where they are."""
+    page, hkv, d, n_pages = 128, 1, 128, 300000
+    k = torch.zeros((n_pages, hkv, page, d), dtype=torch.uint8, device="cuda")
+    v = torch.zeros_like(k)
+    ks, vs = torch.ones(n_pages, hkv, device="cuda"), torch.ones(n_pages, hkv, device="cuda")
+    status, w = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.ones(n_pages, hkv, page, device="cuda")
+    cache = fcp.Cache(k, v, ks, vs, status, weight=w, kind="e4m3")
+    rng = np.random.default_rng(1)
+    table = np.asarray([[n_pages - 1, 0, n_pages - 2]])
+    x, y = bf16(rng, 300, 1, d), bf16(rng, 300, 1, d)
+    batch = fcp.CacheBatch(dev(table), dev([300]), dev([0, 300]), rows=300)
+    fcp.fcp_cache_append(cache, batch, x.cuda(), y.cuda(), stream=stream())
+    state = dict(k=np.zeros((3, 1, page, d)), v=np.zeros((3, 1, page, d)), k_scale=np.ones((3, 1)), v_scale=np.ones((3, 1)))
+    R.append("e4m3", state, [[0, 1, 2]], [300], [0, 300], f64(x), f64(y))
+    at = torch.as_tensor(table[0]).cuda()
+    assert np.array_equal(R.code_values("e4m3", k[at].cpu().numpy()), state["k"]) and np.array_equal(f64(vs[at]), state["v_scale"])
+    q, o, lse = bf16(rng, 1, 2, d), torch.empty(1, 2, d, dtype=torch.bfloat16, device="cuda"), torch.empty(1, 2, device="cuda")
+    step = fcp.CacheBatch(dev(table), dev([300]), dev([0, 1]), rows=1)
+    n = fcp.fcp_cache_attn_workspace_bytes(cache, step, 2)
+    fcp.fcp_cache_attn(cache, step, q.cuda(), o, lse, torch.empty(n, dtype=torch.uint8, device="cuda"), n, accumulate=True, stream=stream())
+    r = R.attention(state, [[0, 1, 2]], [300], [0, 1], f64(q))
+    assert np.allclose(f64(lse), r["lse"], atol=1e-4) and np.abs(f64(o) - r["o"]).max() < 0.02
+    assert math.isclose(float(w.double().sum()), n_pages * page - 300 + 2, rel_tol=1e-9)      # append zeroed 300 weights, attention added 2
+    dst = dev([[n_pages - 3]])
+    new_length, kept = torch.empty(1, dtype=torch.int32, device="cuda"), torch.empty(1, 1, 40, dtype=torch.int32, device="cuda")
+    fcp.fcp_cache_evict(cache, step, 4, 30, 6, dst, new_length, kept, stream=stream())
+    assert torch.equal(k[n_pages - 3, 0, :4], k[n_pages - 1, 0, :4]) and torch.equal(v[n_pages - 3, 0, 34:40].cpu(), v[n_pages - 2, 0, 38:44].cpu())
+
+
+@pytest.mark.parametrize("kind,page,hkv,d", CASES)
+@pytest.mark.parametrize("sink,heavy,recent", [(4, 20, 10), (0, 37, 0), (0, 1, 0), (130, 0, 3), (1, 200, 64), (0, 0, 16)])
+def test_eviction(kind, page, hkv, d, sink, heavy, recent):
+    keep = sink + heavy + recent
+    lengths = [keep + 1, 1000, keep, 0, 1, 333, 1500]
+    need = -(-keep // page)
+    w = World(41, kind, page, hkv, d, lengths, spare=len(lengths) * need + 1).fill()
+    w.weight = np.where(w.rng.random(w.weight.shape) < 0.5, np.round(w.weight * 8) / 8, w.weight).astype(np.float32)       # many equal ones
+    w.weight[w.table[1][0], 0, :5] = [np.nan, np.inf, -1.0, -np.inf, -0.0]
+    w.weight[w.table[5][0]] = 0
+    w.up()
+    dst = w.free[:len(lengths) * need].reshape(len(lengths), need)
+    new_length = torch.full((len(lengths),), -7, dtype=torch.int32, device="cuda")
+    kept = torch.full((len(lengths), hkv, keep), -7, dtype=torch.int32, device="cuda")
+    state = w.state()
+    fcp.fcp_cache_evict(w.cache, fcp.CacheBatch(dev(w.table), dev(w.length)), sink, heavy, recent, dev(dst), new_length, kept, stream=stream())
+    want_kept, want_length = R.evict(kind, state, w.table, w.length, sink, heavy, recent, dst)
+    assert new_length.tolist() == want_length.tolist()
+    assert np.array_equal(kept.cpu().numpy(), want_kept)
+    same(w.now(), state)
+    assert w.cache.device_status().tolist() == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("length", [49152 + 60, 49152 + 61, 90001])
+def test_eviction_from_a_long_sequence(length):
+    """Around as many candidates as fit shared memory, and beyond; weights that share their upper bits."""
+    w = World(42, "int8", 128, 1, 64, [length], spare=120)
+    w.weight = (1.0 + np.round(w.rng.random(w.weight.shape) * 5000) * 2.0 ** -23).astype(np.float32)
+    w.codes = {n: np.where(c == 128, 0, c).astype(np.uint8) for n, c in w.codes.items()}
+    w.up()
+    dst = w.free[:118][None]
+    new_length, kept = torch.empty(1, dtype=torch.int32, device="cuda"), torch.empty(1, 1, 15000, dtype=torch.int32, device="cuda")
+    fcp.fcp_cache_evict(w.cache, fcp.CacheBatch(dev(w.table), dev(w.length)), 10, 14940, 50, dev(dst), new_length, kept, stream=stream())
+    pos = R.choose(w.weight[w.table[0], 0].reshape(-1)[:length].tolist(), 10, 14940, 50)
+    assert np.array_equal(kept.cpu().numpy()[0, 0], pos)
+    src = torch.as_tensor(w.table[0][pos // 128] * 128 + pos % 128).cuda()
+    to = torch.as_tensor(dst[0][np.arange(15000) // 128] * 128 + np.arange(15000) % 128).cuda()
+    assert torch.equal(w.w.view(-1)[to], w.w.view(-1)[src])
+
+
+# ---------------------------------------------------------------------------------------------------------
+# Streams, graphs, and the calls as they are used together
+# ---------------------------------------------------------------------------------------------------------
+def test_captured_step_is_replayed_with_new_contents():
+    """A decode step (rotary, append, attention) captured once, with row and length buffers larger than the batch it sees."""
+    w = World(51, "e4m3", 16, 2, 64, [60, 30, 17, 5], width=8).fill().up()
+    B, hq, table = 4, 4, fcp.RopeTable(64, 32, "interleaved")
+    length, off = dev([0] * B), dev([0] * (B + 1))
+    q, k, v = (torch.zeros(B, h, 64, dtype=torch.bfloat16, device="cuda") for h in (hq, 2, 2))
+    o, lse = torch.zeros(B, hq, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, hq, device="cuda")
+    batch = fcp.CacheBatch(dev(w.table), length, off, rows=B, max_new=1)
+    n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, hq)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+
+    def step():
+        s = stream()
+        fcp.fcp_rope_fwd(table, q, k, q, k, row_offset=off, length=length, stream=s)
+        fcp.fcp_cache_append(w.cache, batch, k, v, stream=s)
+        fcp.fcp_cache_attn(w.cache, batch, q, o, lse, ws, n, accumulate=True, stream=s)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()                                                    # lengths of zero: nothing happens
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    f = R.rope_frequencies(32, 10000.0)
+    for lengths in ([60, 30, 17, 5], [60, 0, 17, 1], [1, 30, 0, 0]):
+        new = [int(x > 0) for x in lengths]
+        rows = sum(new)
+        xq, xk, xv = (bf16(w.rng, B, h, 64) for h in (hq, 2, 2))
+        q.copy_(xq), k.copy_(xk), v.copy_(xv), o.fill_(3.0)
+        length.copy_(dev(lengths)), off.copy_(dev(np.concatenate([[0], np.cumsum(new)])))
+        state = w.now()
+        graph.replay()
+        torch.cuda.synchronize()
+        pos = [x - 1 for x in lengths if x]
+        check_rope(q[:rows], xq[:rows].cuda(), pos, f, 32, "interleaved", 1.0)
+        R.append("e4m3", state, w.table, lengths, off.cpu().numpy(), f64(k), f64(v))
+        now = w.now()
+        for name in ("k", "v", "k_scale", "v_scale"):
+            assert np.array_equal(now[name], state[name], equal_nan=True)
+        w.off = off.cpu().numpy()
+        r = R.attention(state, w.table, lengths, w.off, f64(q)[:rows])
+        check_attn(w, None, r, o[:rows], lse[:rows], rows)
+        assert bool((o[rows:] == 3).all())
+    assert w.cache.device_status().tolist() == [0, 0, 0, 0]
+
+
+def test_calls_on_two_streams():
+    """Two batches on two caches at once, each with its own workspace."""
+    worlds = [World(52 + i, "int8", 64, 2, 128, [3000, 500]).fill().up() for i in range(2)]
+    want, got, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for w in worlds:
+        w.q = bf16(w.rng, 2, 8, 128).cuda()
+        w.b = w.batch([1, 1])
+        w.n = fcp.fcp_cache_attn_workspace_bytes(w.cache, w.b, 8)
+        w.ws = torch.empty(w.n, dtype=torch.uint8, device="cuda")
+        o, lse = torch.empty(2, 8, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(2, 8, device="cuda")
+        fcp.fcp_cache_attn(w.cache, w.b, w.q, o, lse, w.ws, w.n, stream=stream())
+        want.append((o, lse))
+    torch.cuda.synchronize()
+    for i in range(20):
+        for w, s in zip(worlds, streams):
+            o, lse = torch.empty(2, 8, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(2, 8, device="cuda")
+            s.wait_stream(torch.cuda.current_stream())
+            fcp.fcp_cache_attn(w.cache, w.b, w.q, o, lse, w.ws, w.n, stream=s.cuda_stream)
+            got.append((o, lse))
+    torch.cuda.synchronize()
+    for i, (o, lse) in enumerate(got):
+        assert torch.equal(o, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])
+
+
+def test_a_cache_in_host_memory_is_refused():
+    z = lambda *s, t: torch.zeros(s, dtype=t)
+    cache = fcp.Cache(z(2, 1, 16, 64, t=torch.int8), z(2, 1, 16, 64, t=torch.int8), z(2, 1, t=torch.float32), z(2, 1, t=torch.float32), z(4, t=torch.int32))
+    x = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(fcp.FcpError) as e:
+        fcp.fcp_cache_append(cache, fcp.CacheBatch(dev([[0]]), dev([1]), dev([0, 1]), rows=1), x, x, stream=stream())
+    assert e.value.status == fcp.FCP_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kind,d", [("e4m3", 128), ("int8", 64)])
+def test_prompt_then_tokens_then_eviction(kind, d):
+    """As a model would use them: the prompt through rotary, the packed attention of this library and the cache; tokens one by one;
+    eviction; tokens again on the new pages."""
+    hq, hkv, page, prompts, steps = 4, 2, 16, [200, 33], 6
+    w = World(61, kind, page, hkv, d, [p + steps for p in prompts], spare=20)
+    w.weight[:] = 0
+    w.up()
+    table = fcp.RopeTable(d, d, base=10000.0, scaling="wavelength", factor=4.0, original_length=128.0)
+    freqs = R.rope_frequencies(d, 10000.0, "wavelength", 4.0, 128.0)
+    rows = sum(prompts)
+    q, k, v = (bf16(w.rng, rows, h, d).cuda() for h in (hq, hkv, hkv))
+    off = dev(np.concatenate([[0], np.cumsum(prompts)]))
+    fcp.fcp_rope_fwd(table, q, k, q, k, row_offset=off, stream=stream())
+    plan = fcp.Plan(prompts, [1, 1], hq, hkv, d).upload()
+    o, lse = torch.empty_like(q), torch.empty(rows, hq, device="cuda")
+    fcp.fcp_attn_fwd_fused(plan, q, k, v, o, lse, stream=stream())
+    pages, length = dev(w.table), dev(prompts)
+    batch = fcp.CacheBatch(pages, length, off, rows=rows, max_new=max(prompts))
+    fcp.fcp_cache_append(w.cache, batch, k, v, stream=stream())
+    o8, lse8 = torch.empty_like(q), torch.empty(rows, hq, device="cuda")
+    n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, hq)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    fcp.fcp_cache_attn(w.cache, batch, q, o8, lse8, ws, n, accumulate=True, stream=stream())
+    # the cache's keys are off by half a step of e4m3 (2^-4) or of int8 under a power-of-two scale (2^-7 of the page's largest)
+    step = 2.0 ** -4 if kind == "e4m3" else 2.0 ** -7 * 6
+    assert (o8.float() - o.float()).norm() <= 2 * step * o.float().norm() and (lse8 - lse).abs().max() < 12 * step
+
+    def tokens(pages, lengths, times):
+        lengths = list(lengths)
+        for _ in range(times):
+            positions = dev([p + done[0] for p in prompts])
+            done[0] += 1
+            lengths = [x + 1 for x in lengths]
+            step_batch = fcp.CacheBatch(pages, dev(lengths), dev([0, 1, 2]), rows=2, max_new=1)
+            q1, k1, v1 = (bf16(w.rng, 2, h, d).cuda() for h in (hq, hkv, hkv))
+            raw = k1.clone()
+            fcp.fcp_rope_fwd(table, q1, k1, q1, k1, positions=positions, stream=stream())
+            check_rope(k1, raw, positions.cpu().numpy(), freqs, d, "half", 1.0)
+            fcp.fcp_cache_append(w.cache, step_batch, k1, v1, stream=stream())
+            o1, lse1 = torch.empty(2, hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(2, hq, device="cuda")
+            state = w.now()
+            m = fcp.fcp_cache_attn_workspace_bytes(w.cache, step_batch, hq)
+            fcp.fcp_cache_attn(w.cache, step_batch, q1, o1, lse1, torch.empty(m, dtype=torch.uint8, device="cuda"), m, accumulate=True, stream=stream())
+            w.off = np.asarray([0, 1, 2])
+            r = R.attention(state, pages.cpu().numpy(), lengths, w.off, f64(q1))
+            check_attn(w, None, r, o1, lse1, 2)
+            assert math.isclose(float(w.w.double().sum() - state["weight"].sum()), 2 * hq, rel_tol=1e-5)
+        return lengths
+    done = [0]
+    lengths = tokens(pages, prompts, 3)
+    state = w.now()
+    dst = np.full((2, 6), -1)
+    dst[0], dst[1] = w.free[:6], w.free[6:12]
+    new_length, kept = torch.empty(2, dtype=torch.int32, device="cuda"), torch.empty(2, hkv, 80, dtype=torch.int32, device="cuda")
+    fcp.fcp_cache_evict(w.cache, fcp.CacheBatch(pages, dev(lengths)), 4, 60, 16, dev(dst), new_length, kept, stream=stream())
+    want_kept, want_length = R.evict(kind, state, w.table, lengths, 4, 60, 16, dst)
+    assert np.array_equal(kept.cpu().numpy(), want_kept) and new_length.tolist() == want_length.tolist() == [80, 36]
+    same(w.now(), state)
+    tokens(dev(dst), new_length.tolist(), 3)
+    assert w.cache.device_status().tolist() == [0, 0, 0, 0]
