@@ -21,10 +21,16 @@ struct fcp_cache {
 
 namespace {
 
-inline int rows_per_tile(int wr) { return 16 * wr; }
-// Row tiles of 16, 32, 64 or 128 rows: the smallest that holds a KV head's rows, because the warps that stand side by side
-// for more rows all convert the same codes.
-int tile_warps(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
+// Row tiles: the smallest that holds a KV head's rows, because a block of 8 rows costs as much whether it is full or not, and
+// warps that stand side by side for more rows all convert the same codes.
+struct RowTile {
+  int blocks, warps;                                  // blocks of 8 rows per warp, warps side by side
+  int rows() const { return 8 * blocks * warps; }
+};
+constexpr RowTile kWeights = {4, 0};
+RowTile row_tile(int64_t rows) {
+  return rows <= 8 ? RowTile{1, 1} : rows <= 16 ? RowTile{2, 1} : rows <= 32 ? RowTile{2, 2} : rows <= 64 ? RowTile{2, 4} : RowTile{2, 8};
+}
 int box_keys(const fcp_cache_config& c) { return std::min(c.page_tokens, CT_KEYS); }
 
 CacheView view(const fcp_cache_config& c) {
@@ -37,6 +43,7 @@ CacheView view(const fcp_cache_config& c) {
   v.status = c.status;
   v.n_pages = c.n_pages;
   v.page_tokens = c.page_tokens;
+  v.page_shift = c.page_tokens == 16 ? 4 : c.page_tokens == 32 ? 5 : c.page_tokens == 64 ? 6 : 7;
   v.hkv = c.hkv;
   return v;
 }
@@ -105,15 +112,24 @@ int cache_map(CUtensorMap* m, const fcp_cache_config& c, void* base) {
 
 typedef void (*AttnKernel)(const CUtensorMap, const CUtensorMap, const AttnArgs);
 template <int D, int KIND>
-AttnKernel attn_kernel(int wr) {
-  return wr == 0 ? cache_attn_kernel<D, KIND, 0> : wr == 1 ? cache_attn_kernel<D, KIND, 1> : wr == 2 ? cache_attn_kernel<D, KIND, 2>
-         : wr == 4 ? cache_attn_kernel<D, KIND, 4> : cache_attn_kernel<D, KIND, 8>;
+AttnKernel attn_kernel(RowTile t) {
+  switch (t.warps) {
+    case 0: return cache_attn_kernel<D, KIND, kWeights.blocks, 0>;
+    case 1: return t.blocks == 1 ? cache_attn_kernel<D, KIND, 1, 1> : cache_attn_kernel<D, KIND, 2, 1>;
+    case 2: return cache_attn_kernel<D, KIND, 2, 2>;
+    case 4: return cache_attn_kernel<D, KIND, 2, 4>;
+    default: return cache_attn_kernel<D, KIND, 2, 8>;
+  }
 }
-AttnKernel attn_kernel(const fcp_cache_config& c, int wr) {
-  if (c.head_dim == 128) return c.kind == FCP_CACHE_E4M3 ? attn_kernel<128, FCP_CACHE_E4M3>(wr) : attn_kernel<128, FCP_CACHE_INT8>(wr);
-  return c.kind == FCP_CACHE_E4M3 ? attn_kernel<64, FCP_CACHE_E4M3>(wr) : attn_kernel<64, FCP_CACHE_INT8>(wr);
+AttnKernel attn_kernel(const fcp_cache_config& c, RowTile t) {
+  if (c.head_dim == 128) return c.kind == FCP_CACHE_E4M3 ? attn_kernel<128, FCP_CACHE_E4M3>(t) : attn_kernel<128, FCP_CACHE_INT8>(t);
+  return c.kind == FCP_CACHE_E4M3 ? attn_kernel<64, FCP_CACHE_E4M3>(t) : attn_kernel<64, FCP_CACHE_INT8>(t);
 }
-int attn_smem(const fcp_cache_config& c) { return c.head_dim == 128 ? AttnSmem<128>::DYN_BYTES : AttnSmem<64>::DYN_BYTES; }
+int attn_smem(const fcp_cache_config& c, RowTile t) {
+  const bool one = t.blocks == 1 || t.warps == 0;
+  return c.head_dim == 128 ? (one ? AttnSmem<128, 1>::DYN_BYTES : AttnSmem<128, 2>::DYN_BYTES)
+                           : (one ? AttnSmem<64, 1>::DYN_BYTES : AttnSmem<64, 2>::DYN_BYTES);
+}
 
 // The first compute call of a handle: device, kernel attributes, tensor maps.  Later ones: the device is still the current one.
 int ready(const char* call, const fcp_cache* cache) {
@@ -143,9 +159,9 @@ int ready(const char* call, const fcp_cache* cache) {
     return FCP_ERR_CUDA;
   }
   const fcp_cache_config& c = cache->config;
-  for (int wr : {0, 1, 2, 4, 8})
-    FCP_CUDA_CHECK(cudaFuncSetAttribute(attn_kernel(c, wr), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(c)));
-  FCP_CUDA_CHECK(cudaFuncSetAttribute(cache_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_BYTES));
+  for (RowTile t : {kWeights, row_tile(8), row_tile(16), row_tile(32), row_tile(64), row_tile(128)})
+    FCP_CUDA_CHECK(cudaFuncSetAttribute(attn_kernel(c, t), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(c, t)));
+  FCP_CUDA_CHECK(cudaFuncSetAttribute(cache_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_KEYS * 4));
   int rc = cache_map(&cache->k_map, c, c.k);
   if (rc == FCP_OK) rc = cache_map(&cache->v_map, c, c.v);
   if (rc != FCP_OK) return rc;
@@ -158,8 +174,8 @@ int ready(const char* call, const fcp_cache* cache) {
 struct AttnSpace {
   int64_t o, lse, split, bytes;
 };
-AttnSpace attn_space(int wr, int D) {
-  const int64_t parts = 2 * (int64_t)FCP_PLAN_SMS * rows_per_tile(wr);
+AttnSpace attn_space(RowTile t, int D) {
+  const int64_t parts = 2 * (int64_t)FCP_PLAN_SMS * t.rows();
   AttnSpace s;
   s.o = 0;
   s.lse = parts * D * 4;
@@ -282,7 +298,7 @@ extern "C" int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_
   int rc = check_batch(call, cache, batch, true);
   if (rc == FCP_OK) rc = check_heads(call, cache->config, hq);
   if (rc != FCP_OK) return rc;
-  *bytes = attn_space(tile_warps((int64_t)batch->max_new * (hq / cache->config.hkv)), cache->config.head_dim).bytes;
+  *bytes = attn_space(row_tile((int64_t)batch->max_new * (hq / cache->config.hkv)), cache->config.head_dim).bytes;
   return FCP_OK;
 }
 
@@ -313,8 +329,8 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
     fcp_set_error("%s: an output is NULL or not aligned", call);
     return FCP_ERR_INVALID_ARG;
   }
-  const int wr = tile_warps((int64_t)batch->max_new * group);
-  const AttnSpace space = attn_space(wr, c.head_dim);
+  const RowTile tile = row_tile((int64_t)batch->max_new * group);
+  const AttnSpace space = attn_space(tile, c.head_dim);
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < space.bytes) {
     fcp_set_error("%s: workspace of %lld bytes (aligned to 256) needed, %lld given", call, (long long)space.bytes, (long long)workspace_bytes);
     return FCP_ERR_WORKSPACE;
@@ -335,11 +351,12 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
   a.part_lse = (float*)((char*)workspace + space.lse);
   a.split = (int32_t*)((char*)workspace + space.split);
   cudaStream_t st = (cudaStream_t)stream;
-  const int smem = attn_smem(c), grid = cache->sm_count;
-  FCP_CUDA_CHECK(launch(attn_kernel(c, wr), grid, CT_THREADS, smem, st, cache->k_map, cache->v_map, a));
-  if (c.head_dim == 128) FCP_CUDA_CHECK(launch(cache_merge_kernel<128>, grid, MERGE_THREADS, 0, st, a, rows_per_tile(wr)));
-  else FCP_CUDA_CHECK(launch(cache_merge_kernel<64>, grid, MERGE_THREADS, 0, st, a, rows_per_tile(wr)));
-  if (accumulate) FCP_CUDA_CHECK(launch(attn_kernel(c, 0), grid, CT_THREADS, smem, st, cache->k_map, cache->v_map, a));
+  const int grid = cache->sm_count;
+  FCP_CUDA_CHECK(launch(attn_kernel(c, tile), grid, CT_THREADS, attn_smem(c, tile), st, cache->k_map, cache->v_map, a));
+  if (c.head_dim == 128) FCP_CUDA_CHECK(launch(cache_merge_kernel<128>, grid, MERGE_THREADS, 0, st, a, tile.rows()));
+  else FCP_CUDA_CHECK(launch(cache_merge_kernel<64>, grid, MERGE_THREADS, 0, st, a, tile.rows()));
+  if (accumulate)
+    FCP_CUDA_CHECK(launch(attn_kernel(c, kWeights), grid, CT_THREADS, attn_smem(c, kWeights), st, cache->k_map, cache->v_map, a));
   return FCP_OK;
 }
 
@@ -380,9 +397,11 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const fcp_cache_batch* ba
   a.new_length = new_length;
   a.kept = kept;
   cudaStream_t st = (cudaStream_t)stream;
-  const size_t smem = (size_t)std::min<int64_t>(SELECT_KEYS, (int64_t)a.s.capacity) * 4;
-  FCP_CUDA_CHECK(launch(cache_select_kernel, dim3((unsigned)c.hkv, (unsigned)batch->B), SELECT_THREADS, smem, st, a));
-  const dim3 grid((unsigned)((keep + c.page_tokens - 1) / c.page_tokens), (unsigned)c.hkv, (unsigned)batch->B);
+  // about 8 candidates per thread, as far as eight blocks go
+  const int cluster = a.s.capacity > 32768 ? 8 : a.s.capacity > 16384 ? 4 : a.s.capacity > 8192 ? 2 : 1;
+  const size_t smem = (size_t)std::min(SELECT_KEYS, (a.s.capacity + cluster - 1) / cluster) * 4;
+  FCP_CUDA_CHECK(launch_clusters(cluster, cache_select_kernel, dim3((unsigned)(c.hkv * cluster), (unsigned)batch->B), SELECT_THREADS, smem, st, a));
+  const dim3 grid((unsigned)((keep + MOVE_TOKENS - 1) / MOVE_TOKENS), (unsigned)c.hkv, (unsigned)batch->B);
   if (c.head_dim == 128) {
     if (c.kind == FCP_CACHE_E4M3) FCP_CUDA_CHECK(launch(cache_move_kernel<128, FCP_CACHE_E4M3>, grid, MOVE_THREADS, 0, st, a));
     else FCP_CUDA_CHECK(launch(cache_move_kernel<128, FCP_CACHE_INT8>, grid, MOVE_THREADS, 0, st, a));

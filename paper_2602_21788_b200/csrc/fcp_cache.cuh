@@ -1,5 +1,6 @@
 // Kernels on a paged cache of 8-bit keys and values: append, attention of the newest tokens, the weights it leaves, eviction.
 #pragma once
+#include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -15,7 +16,7 @@ struct CacheView {
   uint8_t *k, *v;
   float *k_scale, *v_scale, *weight;
   int32_t* status;
-  int32_t n_pages, page_tokens, hkv;
+  int32_t n_pages, page_tokens, page_shift, hkv;      // page_tokens = 1 << page_shift
 };
 struct BatchView {
   int32_t B, rows, max_new, table_width, capacity;     // capacity: tokens that a row of the page table can name
@@ -45,22 +46,24 @@ __device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cas
 // Two codes (the low or the high half of a word) -> two halves, exactly: e4m3 has 4 significant bits, int8 8, a half 11.
 template <int KIND>
 __device__ __forceinline__ uint32_t halves_lo(uint32_t w) {
+  uint32_t r;
   if (KIND == FCP_CACHE_E4M3) {
-    __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3);
-    return (uint32_t)r.x | ((uint32_t)r.y << 16);
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
+    return r;
   }
   // byte + 128 under the exponent of 1024 is the half 1024 + 128 + value
-  const uint32_t h = __byte_perm(w ^ 0x80808080u, 0x64646464u, 0x4140);
-  return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(1152.f)));
+  r = __byte_perm(w ^ 0x80808080u, 0x64646464u, 0x4140);
+  return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&r), __float2half2_rn(1152.f)));
 }
 template <int KIND>
 __device__ __forceinline__ uint32_t halves_hi(uint32_t w) {
+  uint32_t r;
   if (KIND == FCP_CACHE_E4M3) {
-    __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-    return (uint32_t)r.x | ((uint32_t)r.y << 16);
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
+    return r;
   }
-  const uint32_t h = __byte_perm(w ^ 0x80808080u, 0x64646464u, 0x4342);
-  return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&h), __float2half2_rn(1152.f)));
+  r = __byte_perm(w ^ 0x80808080u, 0x64646464u, 0x4342);
+  return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&r), __float2half2_rn(1152.f)));
 }
 // Four values over their scale -> four codes, nearest, ties to even; too large ones the largest code.
 template <int KIND>
@@ -217,9 +220,10 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
 // per CTA, joined by a second kernel in a fixed order.
 //
 // Products by mma.sync, not tcgen05: a decode step has 1 to 16 rows per KV head, tcgen05 wants 64 or 128, and codes
-// have to pass through registers to become halves anyway.
+// have to pass through registers to become halves anyway.  Keys and value columns are the 16-row operand, the rows the 8
+// columns: S^T = K Q^T, O^T = V^T P^T, so that 8 rows (one token of 8 query heads) fill a product.
 constexpr int CT_KEYS = 128;                          // keys of a tile
-constexpr int CT_STAGES = 4;
+constexpr int CT_STEP = 32;                           // keys that a warp takes at a time
 constexpr int CT_WARPS = 8;                           // consumer warps; one more loads
 constexpr int CT_THREADS = (CT_WARPS + 1) * 32;
 
@@ -233,7 +237,7 @@ struct AttnArgs {
   float scale_log2;
   int32_t hq, group;                                  // group: query heads of a KV head
   int32_t box;                                        // keys of a TMA box
-  float* part_o;                                      // workspace: [2 * CTAs][16 * WR][D], [2 * CTAs][16 * WR], [CTAs][8]
+  float* part_o;                                      // workspace: [2 * CTAs][rows of a tile][D], [2 * CTAs][rows], [CTAs][SP_W]
   float* part_lse;
   int32_t* split;
 };
@@ -241,16 +245,19 @@ struct AttnArgs {
 struct StageMeta {                                    // what a stage holds, for the consumers
   int32_t row0, n, length, head;                      // of the sequence and group
   int32_t row_tile, key0, flags, part;
-  float ks[CT_KEYS / 16], vs[CT_KEYS / 16];           // per 16 keys; ks = 0: absent
+  // per 16 keys: key scale (0: absent), log2 and inverse of the value scale, row of the first code (bits)
+  float4 sub[CT_KEYS / 16];
 };
 enum { ST_FIRST = 1, ST_LAST = 2, ST_WHOLE = 4, ST_END = 8 };
 enum { SP_COUNT = 0, SP_ROW0, SP_N, SP_HEAD, SP_ROW_TILE, SP_W = 8 };
 
-template <int D>
+// NR blocks of 8 rows per warp, WR warps side by side: 8 * NR * WR rows of a group.
+template <int D, int NR>
 struct AttnSmem {
   static constexpr int TILE = CT_KEYS * D;            // bytes of K or of V
-  static constexpr int RING = CT_STAGES * 2 * TILE;
-  static constexpr int JOIN = CT_WARPS * 16 * D * 4;  // the warps' partial outputs
+  static constexpr int STAGES = D == 64 ? 8 : NR == 1 ? 6 : 4;
+  static constexpr int RING = STAGES * 2 * TILE;
+  static constexpr int JOIN = CT_WARPS * 8 * NR * D * 4;       // the warps' partial outputs
   static constexpr int DYN_BYTES = RING + JOIN + 1024;
 };
 
@@ -259,21 +266,17 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* m, 
                ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1)
                : "memory");
 }
-__device__ __forceinline__ uint4 lds_v4(uint32_t addr) {
-  uint4 x;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(addr) : "memory");
-  return x;
-}
-__device__ __forceinline__ uint2 lds_v2(uint32_t addr) {
-  uint2 x;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(addr) : "memory");
-  return x;
-}
 // D (fp32) += A (16 x 16 halves) * B (16 x 8 halves)
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 8 x 8 halves held as (row g, columns 2t, 2t + 1) -> (column g, rows 2t, 2t + 1)
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -353,29 +356,25 @@ __device__ __forceinline__ CtaRange cta_range(const BatchView& s, const TileOrde
   return r;
 }
 
-// The rows of a thread's fragments: thread (g, t) of a warp holds rows g and g + 8, and of them the head's columns
-// [t * D / 4, (t + 1) * D / 4): the sum over columns may be taken in any order, as long as queries and keys agree.
-template <int D>
+// NR blocks of 8 rows.  As the operand of S^T = K Q^T, thread (g, t) holds row g of a block and of it the columns
+// [t * D / 4, (t + 1) * D / 4): the sum over columns may be taken in any order, as long as queries and keys agree.  Of the
+// result it has rows 2t and 2t + 1, and so of everything that goes with rows.
+template <int D, int NR>
 struct QueryRows {
   static constexpr int KS = D / 16;                   // steps of 16 columns
-  uint32_t a[KS][4];
-  float factor[2];                                    // score of the product -> log2 units, without the key scale
-  int32_t limit[2];                                   // keys in front of this position are seen
-  int32_t least, most;                                // of the warp's 16 rows (least: of the existing ones)
-  int32_t token[2], head[2];                          // packed row and query head; token -1: no such row
+  uint32_t b[NR][KS][2];
+  float factor[NR][2];                                // score of the product -> log2 units, without the key scale
+  int32_t limit[NR][2];                               // keys in front of this position are seen; 0: no such row
+  int32_t least, most;                                // of the rows that exist
 
   __device__ __forceinline__ void fill(const AttnArgs& A, const StageMeta& m, int first_row, int lane) {
     const int g = lane >> 2, t = lane & 3, n_rows = m.n * A.group;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = first_row + g + 8 * i, j = r / A.group;
-      const bool is = r < n_rows;
-      token[i] = is ? m.row0 + j : -1;
-      head[i] = m.head * A.group + r - j * A.group;
-      limit[i] = is ? m.length - m.n + j + 1 : 0;
+    for (int i = 0; i < NR; ++i) {
+      const int r = first_row + 8 * i + g, j = r / A.group;
       uint32_t w[D / 8];
-      if (is) {
-        const __nv_bfloat16* p = A.q + (int64_t)token[i] * A.q_stride + head[i] * D + t * (D / 4);
+      if (r < n_rows) {
+        const __nv_bfloat16* p = A.q + (int64_t)(m.row0 + j) * A.q_stride + (m.head * A.group + r - j * A.group) * D + t * (D / 4);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           const uint4 x = ld_v4(p + c * 8);
@@ -393,54 +392,62 @@ struct QueryRows {
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = max((int)(top >> 7), 20);         // biased exponent; 20: smaller rows are taken as they are scaled then
-      const float up = __uint_as_float((uint32_t)(262 - e) << 23);            // 2^(8 - (e - 127)), e <= 255
-      factor[i] = A.scale_log2 * __uint_as_float((uint32_t)(e - 8) << 23);    // 2^(e - 127 - 8)
+      const float up = __uint_as_float((uint32_t)(262 - e) << 23);                     // 2^(8 - (e - 127)), e <= 255
+      const float f = A.scale_log2 * __uint_as_float((uint32_t)(e - 8) << 23);         // 2^(e - 127 - 8)
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        a[k][i] = pack_half(bf_lo(w[2 * k]) * up, bf_hi(w[2 * k]) * up);
-        a[k][i + 2] = pack_half(bf_lo(w[2 * k + 1]) * up, bf_hi(w[2 * k + 1]) * up);
+        b[i][k][0] = pack_half(bf_lo(w[2 * k]) * up, bf_hi(w[2 * k]) * up);
+        b[i][k][1] = pack_half(bf_lo(w[2 * k + 1]) * up, bf_hi(w[2 * k + 1]) * up);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int row = first_row + 8 * i + 2 * t + c;
+        factor[i][c] = __shfl_sync(0xffffffffu, f, (2 * t + c) * 4);
+        limit[i][c] = row < n_rows ? m.length - m.n + row / A.group + 1 : 0;
       }
     }
-    const int last = min(first_row + 15, n_rows - 1);
+    const int last = min(first_row + 8 * NR, n_rows) - 1;
     least = m.length - m.n + first_row / A.group + 1;
     most = first_row < n_rows ? m.length - m.n + last / A.group + 1 : 0;
   }
 };
 
-// Shared-memory address of 16 bytes `chunk` of key `key` of a tile, as TMA has swizzled them.
+// 16 bytes `chunk` of key `key` of a tile, as TMA has swizzled them.
 template <int D>
-__device__ __forceinline__ uint32_t tile_addr(uint32_t tile, int key, int chunk) {
+__device__ __forceinline__ const uint8_t* tile_at(const uint8_t* tile, int key, int chunk) {
   return D == 128 ? tile + key * 128 + ((chunk ^ (key & 7)) << 4) : tile + key * 64 + ((chunk ^ ((key >> 1) & 3)) << 4);
 }
-
-// Scores of 16 keys (two blocks of 8 columns): S[i][..] = codes of key 8 i + g against the rows.
-template <int D, int KIND>
-__device__ __forceinline__ void key_codes(uint32_t tile, int key0, int lane, uint32_t (&w)[2][D / 16]) {
-  const int g = lane >> 2, t = lane & 3;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      const uint4 x = lds_v4(tile_addr<D>(tile, key0 + 8 * i + g, t * (D / 64) + c));
-      w[i][4 * c] = x.x; w[i][4 * c + 1] = x.y; w[i][4 * c + 2] = x.z; w[i][4 * c + 3] = x.w;
-    }
-  }
+__device__ __forceinline__ void words(const uint8_t* p, uint32_t* w) {
+  const uint4 x = *reinterpret_cast<const uint4*>(p);
+  w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
 }
-template <int D, int KIND>
-__device__ __forceinline__ void scores(const QueryRows<D>& q, const uint32_t (&w)[2][D / 16], float (&s)[2][4]) {
+
+// Scores of 16 keys from `key0` of the tile on, against NR blocks of rows: s[i] = (key g | g + 8) x (row 2t | 2t + 1).
+template <int D, int KIND, int NR>
+__device__ __forceinline__ void scores(const QueryRows<D, NR>& q, const uint8_t* tile, int key0, int lane, float (&s)[NR][4]) {
+  const int g = lane >> 2, t = lane & 3;
+  uint32_t lo[D / 16], hi[D / 16];                    // of keys g and g + 8
 #pragma unroll
-  for (int i = 0; i < 2; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+  for (int c = 0; c < D / 64; ++c) {
+    words(tile_at<D>(tile, key0 + g, t * (D / 64) + c), lo + 4 * c);
+    words(tile_at<D>(tile, key0 + g + 8, t * (D / 64) + c), hi + 4 * c);
+  }
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k)
+  for (int i = 0; i < NR; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) mma_f16(s[i], q.a[k][0], q.a[k][1], q.a[k][2], q.a[k][3], halves_lo<KIND>(w[i][k]), halves_hi<KIND>(w[i][k]));
+  for (int k = 0; k < D / 16; ++k) {
+    const uint32_t a0 = halves_lo<KIND>(lo[k]), a1 = halves_lo<KIND>(hi[k]), a2 = halves_hi<KIND>(lo[k]), a3 = halves_hi<KIND>(hi[k]);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) mma_f16(s[i], a0, a1, a2, a3, q.b[i][k][0], q.b[i][k][1]);
+  }
 }
 
 // Loading warp: walks the CTA's tiles.  Lanes look 32 sub-blocks of 16 keys (four stages) ahead in page table and scales.
-template <int D, bool WEIGHTS>
+template <int D, int NR, bool WEIGHTS>
 __device__ __forceinline__ void attn_producer(const AttnArgs& A, const CUtensorMap* tk, const CUtensorMap* tv, const TileOrder& order,
                                               const CtaRange& range, uint32_t ring, StageMeta* meta, uint32_t full, uint32_t empty,
                                               const WaitCtx& ctx) {
+  using S = AttnSmem<D, NR>;
   constexpr int SUBS = CT_KEYS / 16;
   const int lane = threadIdx.x & 31, sub = lane & (SUBS - 1);
   const int page_tokens = A.c.page_tokens;
@@ -471,23 +478,25 @@ __device__ __forceinline__ void attn_producer(const AttnArgs& A, const CUtensorM
       split[SP_ROW0] = s.row0; split[SP_N] = s.n; split[SP_HEAD] = head; split[SP_ROW_TILE] = rt;
     }
     for (int i0 = 0; ok && i0 < tiles; i0 += 4) {
-      float ks = 0.f, vs = 0.f;
+      float ks = 0.f, vs = 1.f;
       int32_t row = -1;
       const int my_tile = i0 + lane / SUBS, key = (tile0 + my_tile) * CT_KEYS + sub * 16;
       if (my_tile < tiles && key < seen) {
-        const int32_t page = ld_i32(A.s.page_table + (int64_t)b * A.s.table_width + key / page_tokens);
+        const int32_t page = ld_i32(A.s.page_table + (int64_t)b * A.s.table_width + (key >> A.c.page_shift));
         row = page_row(page, A.c.n_pages, A.c.hkv, head, page_tokens);
         if (row >= 0) {
           ks = ld_f32(A.c.k_scale + page * A.c.hkv + head);
           vs = ld_f32(A.c.v_scale + page * A.c.hkv + head);
-          row += key % page_tokens;
+          row += (key & (page_tokens - 1));
         }
         if (row < 0 || !usable_scale(ks) || !usable_scale(vs)) {
           mark_bad(A.c.status, row < 0 ? FCP_CACHE_BAD_PAGE : FCP_CACHE_BAD_SCALE, b);
           row = -1;
-          ks = vs = 0.f;
+          ks = 0.f;
+          vs = 1.f;
         }
       }
+      const float4 about = make_float4(ks, __log2f(vs), 1.f / vs, __int_as_float(row));
       for (int i = i0; i < min(i0 + 4, tiles); ++i) {
         if (!mbar_wait_warp(empty + stage * 8, phase ^ 1, ctx, 911)) {
           ok = false;
@@ -497,10 +506,7 @@ __device__ __forceinline__ void attn_producer(const AttnArgs& A, const CUtensorM
         const bool loads = here && leads && row >= 0;
         const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, loads));
         StageMeta& m = meta[stage];
-        if (here) {
-          m.ks[sub] = ks;
-          m.vs[sub] = WEIGHTS ? __int_as_float(row) : vs;       // the weights' place is the codes' row
-        }
+        if (here) m.sub[sub] = about;
         if (lane == 0) {
           m.row0 = s.row0; m.n = s.n; m.length = s.length; m.head = head;
           m.row_tile = rt;
@@ -517,12 +523,12 @@ __device__ __forceinline__ void attn_producer(const AttnArgs& A, const CUtensorM
         }
         __syncwarp();
         if (loads) {
-          const uint32_t dst = ring + stage * 2 * AttnSmem<D>::TILE + sub * 16 * D;
+          const uint32_t dst = ring + stage * 2 * S::TILE + sub * 16 * D;
           tma_load_2d(dst, tk, bar, 0, row);
-          if (!WEIGHTS) tma_load_2d(dst + AttnSmem<D>::TILE, tv, bar, 0, row);
+          if (!WEIGHTS) tma_load_2d(dst + S::TILE, tv, bar, 0, row);
         }
         __syncwarp();
-        if (++stage == CT_STAGES) {
+        if (++stage == S::STAGES) {
           stage = 0;
           phase ^= 1;
         }
@@ -545,187 +551,196 @@ __device__ __forceinline__ void attn_producer(const AttnArgs& A, const CUtensorM
   }
 }
 
-// WR warps side by side hold 16 * WR rows of a group; the 8 / WR warps behind each other take different keys of a tile.
-template <int D, int KIND, int WR>
+// WR warps side by side hold the rows of a tile, 8 * NR each; the 8 / WR warps behind each other take different keys: 32 of a
+// tile (64, 128 with four, eight warps side by side), with one warp side by side of every second tile only.
+template <int D, int KIND, int NR, int WR>
 struct AttnConsumer {
-  static constexpr int RT = 16 * WR, KG = CT_WARPS / WR, NT = D / 8;
-  QueryRows<D> q;
-  float o[NT][4];
-  float m[2], l[2];
+  using S = AttnSmem<D, NR>;
+  static constexpr int RT = 8 * NR * WR, KG = CT_WARPS / WR, MT = D / 16;
+  static constexpr int STEPS = WR <= 2 ? 1 : WR / 2;  // of 32 keys, per warp and tile
+  QueryRows<D, NR> q;
+  float o[NR][MT][4];                                 // O^T: block j of 16 columns: columns g MT*2 + 2j (| + 1) x rows 2t (| + 1)
+  float ref[NR][2], l[NR][2];                         // weights are 2^(a - ref); their sum over the value scale
 
-  // 16 keys from `key` (position) on, at `at` in the stage
-  __device__ __forceinline__ void step(uint32_t ktile, uint32_t vtile, int at, int key, float ks, float vs, int lane) {
+  // 32 keys from `key` (position) on, at `at` in the stage
+  __device__ __forceinline__ void step(const uint8_t* ktile, const uint8_t* vtile, int at, int key, const float4 (&about)[2], int lane) {
     const int g = lane >> 2, t = lane & 3;
-    float s[2][4];
-    {
-      uint32_t w[2][D / 16];
-      key_codes<D, KIND>(ktile, at, lane, w);
-      scores<D, KIND>(q, w, s);
-    }
-    // In log2 units plus log2 of the value scale: w = 2^(a - m) are the weights of the value codes, and the sum of the
-    // probabilities is that of w / vs.  The largest w is 2^14, which leaves a half 2^38 below it before it is rounded to 0.
-    const float shift = __log2f(vs), f0 = q.factor[0] * ks, f1 = q.factor[1] * ks, inverse = 1.f / vs;
-    const bool edge = key + 16 > q.least;
-    float m0 = m[0], m1 = m[1];
+    float s[2][NR][4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int h = 0; h < 2; ++h) scores<D, KIND, NR>(q, ktile, at + 16 * h, lane, s[h]);
+    // a = score in log2 units plus log2 of the value scale, so that 2^(a - ref) are the weights of the value codes, and the sum
+    // of the probabilities is that of the weights over the value scale.  ref follows the largest a from 8 below it and is left
+    // alone until a weight would pass 2^15: a half holds weights down to 2^-24, 2^-32 of the largest and less.
+    const bool edge = key + 32 > q.least || about[0].x == 0.f || about[1].x == 0.f;
+    float top[NR][2];
+    bool high = false;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        s[i][c] = fmaf(s[i][c], f0, shift);
-        s[i][c + 2] = fmaf(s[i][c + 2], f1, shift);
-        if (edge) {
-          const int pos = key + 8 * i + 2 * t + c;
-          if (pos >= q.limit[0]) s[i][c] = -INFINITY;
-          if (pos >= q.limit[1]) s[i][c + 2] = -INFINITY;
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float f = q.factor[i][r] * about[h].x;
+          float &x = s[h][i][r], &y = s[h][i][r + 2];
+          x = fmaf(x, f, about[h].y);
+          y = fmaf(y, f, about[h].y);
+          if (edge) {
+            if (about[h].x == 0.f || key + 16 * h + g >= q.limit[i][r]) x = -INFINITY;
+            if (about[h].x == 0.f || key + 16 * h + g + 8 >= q.limit[i][r]) y = -INFINITY;
+          }
         }
-        m0 = fmaxf(m0, s[i][c]);
-        m1 = fmaxf(m1, s[i][c + 2]);
+        top[i][r] = fmaxf(fmaxf(s[0][i][r], s[0][i][r + 2]), fmaxf(s[1][i][r], s[1][i][r + 2]));
+        high |= top[i][r] > ref[i][r] + 15.f;
       }
-    m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 1));
-    m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
-    m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
-    m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
-    if (__any_sync(0xffffffffu, m0 > m[0] || m1 > m[1])) {
-      const float r0 = exp2_approx(m[0] - m0), r1 = exp2_approx(m[1] - m1);
-      l[0] *= r0;
-      l[1] *= r1;
+    if (__any_sync(0xffffffffu, high)) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        o[j][0] *= r0; o[j][1] *= r0;
-        o[j][2] *= r1; o[j][3] *= r1;
-      }
-      m[0] = m0;
-      m[1] = m1;
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float m = top[i][r];
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+          m = fmaxf(ref[i][r], m - 8.f);
+          const float shrink = exp2_approx(ref[i][r] - m);
+          ref[i][r] = m;
+          l[i][r] *= shrink;
+#pragma unroll
+          for (int j = 0; j < MT; ++j) {
+            o[i][j][r] *= shrink;
+            o[i][j][r + 2] *= shrink;
+          }
+        }
     }
-    const float e0 = m0 - 14.f, e1 = m1 - 14.f;
-    float z0 = 0.f, z1 = 0.f;
+    uint32_t p[2][NR][2];                             // P^T as the second operand: keys 2t, 2t + 1 (| + 8) x row g
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        s[i][c] = exp2_approx(s[i][c] - e0);
-        s[i][c + 2] = exp2_approx(s[i][c + 2] - e1);
-        z0 += s[i][c];
-        z1 += s[i][c + 2];
+      for (int i = 0; i < NR; ++i) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[h][i][c] = exp2_approx(s[h][i][c] - ref[i][c & 1]);
+        l[i][0] = fmaf(s[h][i][0] + s[h][i][2], about[h].z, l[i][0]);
+        l[i][1] = fmaf(s[h][i][1] + s[h][i][3], about[h].z, l[i][1]);
+        p[h][i][0] = transpose8(pack_half(s[h][i][0], s[h][i][1]));
+        p[h][i][1] = transpose8(pack_half(s[h][i][2], s[h][i][3]));
       }
-    l[0] = fmaf(z0, inverse, l[0]);
-    l[1] = fmaf(z1, inverse, l[1]);
-    const uint32_t p0 = pack_half(s[0][0], s[0][1]), p1 = pack_half(s[0][2], s[0][3]);
-    const uint32_t p2 = pack_half(s[1][0], s[1][1]), p3 = pack_half(s[1][2], s[1][3]);
-    // value codes: thread (g, t) reads columns [g D/8, (g+1) D/8) of keys 2t, 2t+1, 2t+8, 2t+9; block j of 8 output columns
-    // is then column g D/8 + j
-    uint32_t v[4][D / 32];
+    // value codes: thread (g, t) reads columns [g D/8, (g + 1) D/8) of keys 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int kk = 2 * t + (i & 1) + 8 * (i >> 1);
-      if (D == 128) {
-        const uint4 x = lds_v4(tile_addr<D>(vtile, at + kk, g));
-        v[i][0] = x.x; v[i][1] = x.y; v[i][D / 32 - 2] = x.z; v[i][D / 32 - 1] = x.w;
-      } else {
-        const uint2 x = lds_v2(tile_addr<D>(vtile, at + kk, g >> 1) + (g & 1) * 8);
-        v[i][0] = x.x; v[i][1] = x.y;
-      }
-    }
-    bool careful = false;
-    if (edge) {
-      // what lies behind the last key that any row sees is whatever the page held: it must not meet a zero weight
-      bool nan = false;
+    for (int h = 0; h < 2; ++h) {
+      uint32_t v[4][D / 32];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool past = key + 2 * t + (i & 1) + 8 * (i >> 1) >= q.most;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          if (past) v[i][c] = 0;
-          if (KIND == FCP_CACHE_E4M3) nan |= __vcmpeq4(v[i][c] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+        const int kk = at + 16 * h + 2 * t + (i & 1) + 8 * (i >> 1);
+        if (D == 128) {
+          words(tile_at<D>(vtile, kk, g), v[i]);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(tile_at<D>(vtile, kk, g >> 1) + (g & 1) * 8);
+          v[i][0] = x.x;
+          v[i][1] = x.y;
         }
       }
-      careful = KIND == FCP_CACHE_E4M3 && __any_sync(0xffffffffu, nan);
-    }
-    if (KIND == FCP_CACHE_E4M3 && careful) {
-      // a NaN that only some of the rows see: key by key, and only into the rows that see it
+      bool careful = false;
+      if (edge) {
+        // what lies behind the last key that any row sees is whatever the page held: it must not meet a zero weight
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool past = about[h].x == 0.f || key + 16 * h + 2 * t + (i & 1) + 8 * (i >> 1) >= q.most;
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            if (past) v[i][c] = 0;
+            if (KIND == FCP_CACHE_E4M3) nan |= __vcmpeq4(v[i][c] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+          }
+        }
+        careful = KIND == FCP_CACHE_E4M3 && __any_sync(0xffffffffu, nan);
+      }
+      if (KIND == FCP_CACHE_E4M3 && careful) {
+        // a NaN that only some of the rows see: key by key, and only into the rows that see it
 #pragma unroll 1
-      for (int k = 0; k < 16; ++k) {
-        const bool mine = t == ((k & 7) >> 1), odd = k & 1, high = k >> 3;
-        const uint32_t keep = odd ? 0xffff0000u : 0x0000ffffu;
-        const uint32_t a0 = mine && !high ? p0 & keep : 0, a1 = mine && !high ? p1 & keep : 0;
-        const uint32_t a2 = mine && high ? p2 & keep : 0, a3 = mine && high ? p3 & keep : 0;
-        const bool see0 = key + k < q.limit[0], see1 = key + k < q.limit[1];
+        for (int k = 0; k < 16; ++k) {
+          const bool mine = t == ((k & 7) >> 1), odd = k & 1, high8 = k >> 3;
+          const uint32_t keep = mine ? (odd ? 0xffff0000u : 0x0000ffffu) : 0u;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t x[4];
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t x[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = mine && (i & 1) == odd && (i >> 1) == high ? v[i][c] : 0;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t b0 = __byte_perm(x[0], x[1], h ? 0x7362 : 0x5140), b1 = __byte_perm(x[2], x[3], h ? 0x7362 : 0x5140);
+            for (int i = 0; i < 4; ++i) x[i] = mine && (i & 1) == odd && (i >> 1) == high8 ? v[i][c] : 0;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float d[4] = {0.f, 0.f, 0.f, 0.f};
-              mma_f16(d, a0, a1, a2, a3, e ? halves_hi<KIND>(b0) : halves_lo<KIND>(b0), e ? halves_hi<KIND>(b1) : halves_lo<KIND>(b1));
-              float (&acc)[4] = o[4 * c + 2 * h + e];
-              if (see0) { acc[0] += d[0]; acc[1] += d[1]; }
-              if (see1) { acc[2] += d[2]; acc[3] += d[3]; }
+              const uint32_t b0 = __byte_perm(x[0], x[1], e ? 0x7362 : 0x5140), b1 = __byte_perm(x[2], x[3], e ? 0x7362 : 0x5140);
+#pragma unroll
+              for (int i = 0; i < NR; ++i) {
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(d, halves_lo<KIND>(b0), halves_hi<KIND>(b0), halves_lo<KIND>(b1), halves_hi<KIND>(b1), high8 ? 0 : p[h][i][0] & keep,
+                        high8 ? p[h][i][1] & keep : 0);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                  if (key + 16 * h + k < q.limit[i][r]) {
+                    o[i][2 * c + e][r] += d[r];
+                    o[i][2 * c + e][r + 2] += d[r + 2];
+                  }
+              }
             }
           }
         }
+        continue;
       }
-      return;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          // bytes of two keys side by side: columns 4c + 2e (low half) and 4c + 2e + 1 of the thread's run
+          const uint32_t b0 = __byte_perm(v[0][c], v[1][c], e ? 0x7362 : 0x5140), b1 = __byte_perm(v[2][c], v[3][c], e ? 0x7362 : 0x5140);
+          const uint32_t a0 = halves_lo<KIND>(b0), a1 = halves_hi<KIND>(b0), a2 = halves_lo<KIND>(b1), a3 = halves_hi<KIND>(b1);
+#pragma unroll
+          for (int i = 0; i < NR; ++i) mma_f16(o[i][2 * c + e], a0, a1, a2, a3, p[h][i][0], p[h][i][1]);
+        }
     }
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t b0 = __byte_perm(v[0][c], v[1][c], h ? 0x7362 : 0x5140), b1 = __byte_perm(v[2][c], v[3][c], h ? 0x7362 : 0x5140);
-        mma_f16(o[4 * c + 2 * h], p0, p1, p2, p3, halves_lo<KIND>(b0), halves_lo<KIND>(b1));
-        mma_f16(o[4 * c + 2 * h + 1], p0, p1, p2, p3, halves_hi<KIND>(b0), halves_hi<KIND>(b1));
-      }
   }
 
-  // Place of 16 bytes `i` of the thread column t's run (D / 16 of them) of a row, spread over the banks.
-  __device__ static __forceinline__ int join_slot(int row, int t, int i) {
-    return row * (D / 4) + t * (D / 16) + (D == 128 ? (i ^ (2 * t + (row & 1))) : (i ^ ((t >> 1) + 2 * (row & 1))));
+  // Place of 16 bytes `f` of a row of the join area, spread over the banks.
+  __device__ static __forceinline__ int join_slot(int row, int f) {
+    const int t = (row >> 1) & 3;
+    return row * (D / 4) + (D == 128 ? f ^ t : f ^ ((t & 1) | (t >> 1) << 2));
   }
 
   // The end of a group's tiles on this CTA: joins the warps and writes the rows, or their partial result.
-  __device__ __forceinline__ void finish(const AttnArgs& A, const StageMeta& meta, float4* join, float2 (*stats)[16], int warp, int lane) {
+  __device__ __forceinline__ void finish(const AttnArgs& A, const StageMeta& meta, float4* join, float2* stats, int warp, int lane) {
     const int g = lane >> 2, t = lane & 3, tid = warp * 32 + lane;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    }
     asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory");       // the join area's last readers are done
-    float4* mine = join + warp * 16 * (D / 4);
+    float4* mine = join + warp * 8 * NR * (D / 4);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (q.token[i] < 0) continue;
-      const int row = g + 8 * i;
-      if (t == 0) stats[warp][row] = make_float2(m[i], l[i]);
+    for (int i = 0; i < NR; ++i)
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        const int j = 4 * (c % (D / 32)), e = 2 * i + c / (D / 32);
-        mine[join_slot(row, t, c)] = make_float4(o[j][e], o[j + 1][e], o[j + 2][e], o[j + 3][e]);
+      for (int r = 0; r < 2; ++r) {
+        l[i][r] += __shfl_xor_sync(0xffffffffu, l[i][r], 4);
+        l[i][r] += __shfl_xor_sync(0xffffffffu, l[i][r], 8);
+        l[i][r] += __shfl_xor_sync(0xffffffffu, l[i][r], 16);
+        const int row = 8 * i + 2 * t + r;
+        if (g == 0) stats[warp * 8 * NR + row] = make_float2(ref[i][r], l[i][r]);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+          mine[join_slot(row, g * (D / 32) + c)] = make_float4(o[i][2 * c][r], o[i][2 * c][r + 2], o[i][2 * c + 1][r], o[i][2 * c + 1][r + 2]);
       }
-    }
     asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory");
     const int n_rows = min(RT, meta.n * A.group - meta.row_tile * RT);
     for (int e = tid; e < n_rows * (D / 4); e += CT_WARPS * 32) {
-      const int r = e / (D / 4), f = e % (D / 4), wr = r / 16, row = r % 16;
+      const int r = e / (D / 4), f = e % (D / 4), wr = r / (8 * NR), row = r % (8 * NR);
       float top = -3e38f;
 #pragma unroll
-      for (int k = 0; k < KG; ++k) top = fmaxf(top, stats[k * WR + wr][row].x);
+      for (int k = 0; k < KG; ++k) top = fmaxf(top, stats[(k * WR + wr) * 8 * NR + row].x);
       float z = 0.f;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < KG; ++k) {
-        const float2 ml = stats[k * WR + wr][row];
+        const float2 ml = stats[(k * WR + wr) * 8 * NR + row];
         const float w = exp2_approx(ml.x - top);
-        const float4 y = join[(k * WR + wr) * 16 * (D / 4) + join_slot(row, f / (D / 16), f % (D / 16))];
+        const float4 y = join[(k * WR + wr) * 8 * NR * (D / 4) + join_slot(row, f)];
         z = fmaf(ml.y, w, z);
         x.x = fmaf(y.x, w, x.x); x.y = fmaf(y.y, w, x.y); x.z = fmaf(y.z, w, x.z); x.w = fmaf(y.w, w, x.w);
       }
       const float inverse = z == 0.f ? 0.f : 1.f / z;
-      const float lse2 = z == 0.f ? -INFINITY : top - 14.f + __log2f(z);
+      const float lse2 = z == 0.f ? -INFINITY : top + __log2f(z);
       x.x *= inverse; x.y *= inverse; x.z *= inverse; x.w *= inverse;
       if (meta.flags & ST_WHOLE) {
         const int gr = meta.row_tile * RT + r, j = gr / A.group;
@@ -739,33 +754,40 @@ struct AttnConsumer {
     }
   }
 
-  __device__ __forceinline__ void run(const AttnArgs& A, uint32_t ring, StageMeta* metas, float4* join, float2 (*stats)[16], uint32_t full,
-                                      uint32_t empty, const WaitCtx& ctx) {
+  __device__ __forceinline__ void run(const AttnArgs& A, const uint8_t* ring, const StageMeta* metas, float4* join, float2* stats,
+                                      uint32_t full, uint32_t empty, const WaitCtx& ctx) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, kg = warp / WR;
-    int stage = 0;
+    const int turn = WR == 1 ? kg >> 2 : 0, first = (WR == 1 ? kg & 3 : kg) * STEPS;       // which tiles, which 32 keys of them
+    int stage = 0, tile = 0;
     uint32_t phase = 0;
     while (mbar_wait_warp(full + stage * 8, phase, ctx, 921)) {
       const StageMeta& meta = metas[stage];
       const int flags = meta.flags;
       if (flags & ST_END) break;
       if (flags & ST_FIRST) {
-        q.fill(A, meta, meta.row_tile * RT + wr * 16, lane);
-        m[0] = m[1] = -3e38f;
-        l[0] = l[1] = 0.f;
+        q.fill(A, meta, meta.row_tile * RT + wr * 8 * NR, lane);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+        for (int i = 0; i < NR; ++i) {
+          ref[i][0] = ref[i][1] = -3e38f;
+          l[i][0] = l[i][1] = 0.f;
+#pragma unroll
+          for (int j = 0; j < MT; ++j) o[i][j][0] = o[i][j][1] = o[i][j][2] = o[i][j][3] = 0.f;
+        }
       }
-      const uint32_t ktile = ring + stage * 2 * AttnSmem<D>::TILE, vtile = ktile + AttnSmem<D>::TILE;
+      if (WR > 1 || (tile & 1) == turn) {
+        const uint8_t* ktile = ring + stage * 2 * S::TILE;
 #pragma unroll 1
-      for (int i = 0; i < WR; ++i) {
-        const int sub = kg * WR + i, key = meta.key0 + sub * 16;
-        const float ks = meta.ks[sub], vs = meta.vs[sub];
-        if (key < q.most && ks != 0.f) step(ktile, vtile, sub * 16, key, ks, vs, lane);
+        for (int i = first; i < first + STEPS; ++i) {
+          const int key = meta.key0 + i * CT_STEP;
+          const float4 about[2] = {meta.sub[2 * i], meta.sub[2 * i + 1]};
+          if (key < q.most && (about[0].x != 0.f || about[1].x != 0.f)) step(ktile, ktile + S::TILE, i * CT_STEP, key, about, lane);
+        }
       }
       if (flags & ST_LAST) finish(A, meta, join, stats, warp, lane);
       __syncwarp();
       if (lane == 0) mbar_arrive(empty + stage * 8);
-      if (++stage == CT_STAGES) {
+      ++tile;
+      if (++stage == S::STAGES) {
         stage = 0;
         phase ^= 1;
       }
@@ -773,88 +795,82 @@ struct AttnConsumer {
   }
 };
 
-// Weights of the cached keys: the scores once more, against the finished log-sum-exps.  A warp holds 16 keys and goes over
-// the rows in tiles of 16, so that a key's sum is taken by one thread column in a fixed order.
-template <int D, int KIND>
-__device__ __forceinline__ void weight_consumer(const AttnArgs& A, uint32_t ring, StageMeta* metas, uint32_t full, uint32_t empty,
-                                                const WaitCtx& ctx) {
+// Weights of the cached keys: the scores once more, against the finished log-sum-exps.  A warp holds 16 keys and goes over the
+// rows in blocks of 8 (32 rows stay in registers), so that a key's sum is taken by four threads in a fixed order.
+template <int D, int KIND, int NR>
+__device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t* ring, const StageMeta* metas, uint32_t full,
+                                                uint32_t empty, const WaitCtx& ctx) {
+  using S = AttnSmem<D, 1>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int stage = 0;
   uint32_t phase = 0;
-  QueryRows<D> q;
-  float lse2[2] = {0.f, 0.f};
+  QueryRows<D, NR> q;
+  float lse2[NR][2];
   while (mbar_wait_warp(full + stage * 8, phase, ctx, 931)) {
     const StageMeta& meta = metas[stage];
     if (meta.flags & ST_END) break;
-    const int sub = warp, key = meta.key0 + sub * 16, n_rows = meta.n * A.group;
-    const float ks = meta.ks[sub];
-    auto rows_from = [&](int r) {
-      q.fill(A, meta, r, lane);
+    const int key = meta.key0 + warp * 16, n_rows = meta.n * A.group;
+    const float4 about = meta.sub[warp];
+    auto rows_from = [&](int r0) {
+      q.fill(A, meta, r0, lane);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        lse2[i] = q.token[i] >= 0 ? ld_f32(A.lse + (int64_t)q.token[i] * A.hq + q.head[i]) * 1.4426950408889634f : INFINITY;
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int r = r0 + 8 * i + 2 * t + c, j = r / A.group;
+          lse2[i][c] = r < n_rows ? ld_f32(A.lse + (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + r - j * A.group) * 1.4426950408889634f : INFINITY;
+        }
     };
-    if (n_rows <= 16 && (meta.flags & ST_FIRST)) rows_from(0);
-    if (key < meta.length && ks != 0.f) {
-      uint32_t w[2][D / 16];
-      key_codes<D, KIND>(ring + stage * 2 * AttnSmem<D>::TILE, sub * 16, lane, w);
-      float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+    if (n_rows <= 8 * NR && (meta.flags & ST_FIRST)) rows_from(0);
+    if (key < meta.length && about.x != 0.f) {
+      float sum[2] = {0.f, 0.f};                      // of keys g and g + 8
 #pragma unroll 1
-      for (int r = 0; r < n_rows; r += 16) {
-        if (n_rows > 16) rows_from(r);
-        float s[2][4];
-        scores<D, KIND>(q, w, s);
-        const float f0 = q.factor[0] * ks, f1 = q.factor[1] * ks;
+      for (int r = 0; r < n_rows; r += 8 * NR) {
+        if (n_rows > 8 * NR) rows_from(r);
+        float s[NR][4];
+        scores<D, KIND, NR>(q, ring + stage * 2 * S::TILE, warp * 16, lane, s);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int pos = key + 8 * i + 2 * t + c;
-            if (pos < q.limit[0]) sum[i][c] += exp2_approx(fmaf(s[i][c], f0, -lse2[0]));
-            if (pos < q.limit[1]) sum[i][c] += exp2_approx(fmaf(s[i][c + 2], f1, -lse2[1]));
-          }
+          for (int c = 0; c < 4; ++c)
+            if (key + g + 8 * (c >> 1) < q.limit[i][c & 1])
+              sum[c >> 1] += exp2_approx(fmaf(s[i][c], q.factor[i][c & 1] * about.x, -lse2[i][c & 1]));
       }
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) sum[i][c] += __shfl_xor_sync(0xffffffffu, sum[i][c], o);
-      // lanes of thread row 0 and 1 write the two blocks of 8 keys
-      const int pos = key + 8 * g + 2 * t;
-      if (g < 2 && pos < meta.length) {
-        float* dst = A.c.weight + (int64_t)__float_as_int(meta.vs[sub]) + 8 * g + 2 * t;
-        dst[0] += g ? sum[1][0] : sum[0][0];
-        if (pos + 1 < meta.length) dst[1] += g ? sum[1][1] : sum[0][1];
+      for (int k = 0; k < 2; ++k) {
+        sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 1);
+        sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 2);
       }
+      if (t < 2 && key + g + 8 * t < meta.length) A.c.weight[(int64_t)__float_as_int(about.w) + g + 8 * t] += sum[t];
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(empty + stage * 8);
-    if (++stage == CT_STAGES) {
+    if (++stage == S::STAGES) {
       stage = 0;
       phase ^= 1;
     }
   }
 }
 
-// WR = 0: the weights.
-template <int D, int KIND, int WR>
+// WR = 0: the weights, of NR blocks of rows at a time.
+template <int D, int KIND, int NR, int WR>
 __global__ void __launch_bounds__(CT_THREADS, 1)
 cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ AttnArgs A) {
+  using S = AttnSmem<D, WR ? NR : 1>;
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t bars[2 * CT_STAGES];
-  __shared__ __align__(16) StageMeta metas[CT_STAGES];
-  __shared__ float2 stats[CT_WARPS][16];
+  __shared__ __align__(8) uint64_t bars[2 * S::STAGES];
+  __shared__ __align__(16) StageMeta metas[S::STAGES];
+  __shared__ float2 stats[CT_WARPS * 8 * (WR ? NR : 1)];
   __shared__ int64_t scratch[16];
   __shared__ int abort_flag;
   const int warp = threadIdx.x >> 5;
-  const uint32_t full = smem_u32(bars), empty = full + CT_STAGES * 8;
+  const uint32_t full = smem_u32(bars), empty = full + S::STAGES * 8;
   // the swizzle pattern repeats every 1024 bytes of address
-  const uint32_t ring = (smem_u32(smem) + 1023u) & ~1023u;
-  uint8_t* base = smem + (ring - smem_u32(smem));
+  const uint32_t skip = (1024u - (smem_u32(smem) & 1023u)) & 1023u;
+  uint8_t* base = smem + skip;
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int i = 0; i < CT_STAGES; ++i) {
+    for (int i = 0; i < S::STAGES; ++i) {
       mbar_init(full + i * 8, 1);
       mbar_init(empty + i * 8, CT_WARPS);
     }
@@ -865,15 +881,15 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   grid_wait();
   __syncthreads();
   const WaitCtx ctx = {&abort_flag, A.c.status, (uint32_t)FCP_WAIT_NS};
-  TileOrder order = {WR ? 16 * WR : 16, A.group, A.c.hkv, WR == 0};
+  TileOrder order = {8 * NR * (WR ? WR : 1), A.group, A.c.hkv, WR == 0};
   const CtaRange range = cta_range(A.s, order, A.c.status, scratch);
   if (warp == CT_WARPS) {
-    attn_producer<D, WR == 0>(A, &tk, &tv, order, range, ring, metas, full, empty, ctx);
+    attn_producer<D, WR ? NR : 1, WR == 0>(A, &tk, &tv, order, range, smem_u32(base), metas, full, empty, ctx);
   } else if constexpr (WR == 0) {
-    weight_consumer<D, KIND>(A, ring, metas, full, empty, ctx);
+    weight_consumer<D, KIND, NR>(A, base, metas, full, empty, ctx);
   } else {
-    AttnConsumer<D, KIND, WR> consumer;
-    consumer.run(A, ring, metas, reinterpret_cast<float4*>(base + AttnSmem<D>::RING), stats, full, empty, ctx);
+    AttnConsumer<D, KIND, NR, WR> consumer;
+    consumer.run(A, base, metas, reinterpret_cast<float4*>(base + S::RING), stats, full, empty, ctx);
   }
   __syncthreads();
   wait_teardown(ctx);
@@ -936,172 +952,256 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// Which tokens of a head stay: one block per (KV head, sequence).  The n_heavy largest weights by four counting passes over
-// 8 bits of the keys, from the top; then one pass writes the kept positions in order.
+// Which tokens of a head stay: one cluster of blocks per (KV head, sequence), each with its slice of the candidates.  The n_heavy
+// largest weights by three counting passes over 11, 11 and 10 bits of the keys, from the top, the counts added up over the cluster;
+// then one pass writes the kept positions in order.
 constexpr int SELECT_THREADS = 1024;
-constexpr int SELECT_KEYS = 49152;                    // as many keys stay in shared memory
-constexpr int SELECT_COPIES = 8;                      // of the counters: fewer threads meet on one
-constexpr int SELECT_BYTES = SELECT_KEYS * 4;
-__global__ void __launch_bounds__(SELECT_THREADS) cache_select_kernel(const __grid_constant__ EvictArgs a) {
+constexpr int SELECT_KEYS = 49152;                    // as many keys of a slice stay in shared memory
+constexpr int SELECT_BINS = 2048;
+constexpr int SELECT_BLOCKS = 8;                      // most blocks of a cluster
+__global__ void __launch_bounds__(SELECT_THREADS, 2) cache_select_kernel(const __grid_constant__ EvictArgs a) {
   extern __shared__ uint32_t keys[];
-  __shared__ uint32_t count[SELECT_COPIES][256];
+  __shared__ __align__(8) uint32_t sums[2][SELECT_BINS];       // of this block, read by the others: one per pass in turn
   __shared__ uint32_t warp_count[32][2];
+  __shared__ uint32_t share[2];                       // kept and equal keys of this block, read by the others
   __shared__ uint32_t chosen[2];                      // digit, how many are still wanted among the keys that have it
   grid_begin();
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int h = blockIdx.x / blocks, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int keep = a.n_sink + a.n_heavy + a.n_recent;
   const int length = usable_length(a.s, b);
-  if (length < 0 && h == 0 && tid == 0) mark_bad(a.c.status, FCP_CACHE_BAD_LENGTH, b);
+  const bool reports = blockIdx.x == 0 && tid == 0;
+  if (length < 0 && reports) mark_bad(a.c.status, FCP_CACHE_BAD_LENGTH, b);
   int32_t* kept = a.kept + ((int64_t)b * a.c.hkv + h) * keep;
-  if (h == 0 && tid == 0) a.new_length[b] = max(0, min(length, keep));
+  if (reports) a.new_length[b] = max(0, min(length, keep));
+  const int first = rank * SELECT_THREADS + tid, stride = blocks * SELECT_THREADS;
   if (length <= keep) {
-    for (int i = tid; i < keep; i += SELECT_THREADS) kept[i] = i < length ? i : -1;
+    for (int i = first; i < keep; i += stride) kept[i] = i < length ? i : -1;
     return;
   }
-  const int page_tokens = a.c.page_tokens, end = length - a.n_recent, n = end - a.n_sink;      // candidates [n_sink, end)
-  auto key_at = [&](int pos) {
-    const int32_t row = page_row(ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + pos / page_tokens), a.c.n_pages, a.c.hkv, h, page_tokens);
-    return row < 0 ? 0u : weight_key(ld_f32(a.c.weight + (int64_t)row + pos % page_tokens));
+  const int page_tokens = a.c.page_tokens, end = length - a.n_recent, n_all = end - a.n_sink;  // candidates [n_sink, end)
+  for (int i = first; i < a.n_sink; i += stride) kept[i] = i;
+  for (int i = first; i < a.n_recent; i += stride) kept[a.n_sink + a.n_heavy + i] = end + i;
+  if (a.n_heavy == 0) return;
+  const int per = (n_all + blocks - 1) / blocks, from = a.n_sink + min(n_all, rank * per), n = min(n_all, rank * per + per) - min(n_all, rank * per);
+  auto key_at = [&](int i) {
+    const int pos = from + i;
+    const int32_t row = page_row(ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + (pos >> a.c.page_shift)), a.c.n_pages, a.c.hkv, h, page_tokens);
+    return row < 0 ? 0u : weight_key(ld_f32(a.c.weight + (int64_t)row + (pos & (page_tokens - 1))));
   };
   const bool in_smem = n <= SELECT_KEYS;
-  if (in_smem)
-    for (int i = tid; i < n; i += SELECT_THREADS) keys[i] = key_at(a.n_sink + i);
+  if (in_smem) {
+    constexpr int U = 4;                              // page entries, then weights, in flight per thread
+    for (int i0 = tid; i0 < n; i0 += U * SELECT_THREADS) {
+      int32_t row[U];
+      float w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * SELECT_THREADS;
+        row[u] = i < n ? ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + ((from + i) >> a.c.page_shift)) : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int pos = from + i0 + u * SELECT_THREADS;
+        row[u] = page_row(row[u], a.c.n_pages, a.c.hkv, h, page_tokens);
+        w[u] = row[u] < 0 ? __int_as_float(0x7fffffff) : ld_f32(a.c.weight + (int64_t)row[u] + (pos & (page_tokens - 1)));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * SELECT_THREADS;
+        if (i < n) keys[i] = weight_key(w[u]);
+      }
+    }
+  }
   uint32_t prefix = 0, wanted = (uint32_t)a.n_heavy;
-  for (int shift = 24; shift >= 0 && a.n_heavy > 0; shift -= 8) {
-    for (int i = tid; i < SELECT_COPIES * 256; i += SELECT_THREADS) (&count[0][0])[i] = 0;
+  for (int pass = 0; pass < 3; ++pass) {              // 11, 11 and 10 bits
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    const uint32_t mask = (1u << bits) - 1u;
+    uint32_t* mine = sums[pass & 1];
+    for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) mine[i] = 0;
     __syncthreads();
     for (int i = tid; i < n; i += SELECT_THREADS) {
-      const uint32_t k = in_smem ? keys[i] : key_at(a.n_sink + i);
-      if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&count[warp % SELECT_COPIES][(k >> shift) & 255u], 1u);
+      const uint32_t k = in_smem ? keys[i] : key_at(i);
+      if (pass == 0 || k >> (shift + bits) == prefix) atomicAdd(&mine[(k >> shift) & mask], 1u);
+    }
+    if (blocks > 1) cluster.sync();
+    else __syncthreads();
+    // from the highest digit down, two digits per thread
+    static_assert(SELECT_BINS == 2 * SELECT_THREADS, "");
+    uint32_t c[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < SELECT_BLOCKS; ++k) {
+      if (k >= blocks) break;
+      const uint2 x = reinterpret_cast<const uint2*>(cluster.map_shared_rank(mine, k))[SELECT_THREADS - 1 - tid];
+      c[0] += x.y;
+      c[1] += x.x;
+    }
+    uint32_t upto = c[0] + c[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) warp_count[warp][0] = upto;
+    __syncthreads();
+    uint32_t w = warp_count[lane][0];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, w, o);
+      if (lane >= o) w += x;
+    }
+    w = __shfl_sync(0xffffffffu, w, (warp - 1) & 31);
+    uint32_t before = upto - c[0] - c[1] + (warp ? w : 0u);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (before < wanted && wanted <= before + c[j]) {
+        chosen[0] = (uint32_t)(SELECT_BINS - 1 - (2 * tid + j));
+        chosen[1] = wanted - before;
+      }
+      before += c[j];
     }
     __syncthreads();
-    if (warp == 0) {                                  // from digit 255 down, 8 digits per lane
-      uint32_t c[8], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        c[j] = 0;
-#pragma unroll
-        for (int k = 0; k < SELECT_COPIES; ++k) c[j] += count[k][255 - (lane * 8 + j)];
-        sum += c[j];
-      }
-      uint32_t upto = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-      }
-      uint32_t before = upto - sum;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (before < wanted && wanted <= before + c[j]) {
-          chosen[0] = (uint32_t)(255 - (lane * 8 + j));
-          chosen[1] = wanted - before;
-        }
-        before += c[j];
-      }
-    }
-    __syncthreads();
-    prefix = prefix << 8 | chosen[0];
+    prefix = prefix << bits | chosen[0];
     wanted = chosen[1];
   }
   // prefix is the smallest kept key, `wanted` of its equals are kept: the first ones
-  uint32_t above_base = 0, equal_base = 0;            // kept and equal keys in front of this trip
-  for (int i = tid; i < a.n_sink; i += SELECT_THREADS) kept[i] = i;
-  for (int i = tid; i < a.n_recent; i += SELECT_THREADS) kept[a.n_sink + a.n_heavy + i] = end + i;
-  for (int i0 = 0; i0 < n && a.n_heavy > 0; i0 += SELECT_THREADS) {
-    const int i = i0 + tid;
-    const uint32_t k = i < n ? (in_smem ? keys[i] : key_at(a.n_sink + i)) : 0u;
-    const bool above = i < n && k > prefix, equal = i < n && k == prefix;
-    const uint32_t am = __ballot_sync(0xffffffffu, above), em = __ballot_sync(0xffffffffu, equal);
-    if (lane == 0) {
-      warp_count[warp][0] = __popc(am);
-      warp_count[warp][1] = __popc(em);
-    }
-    __syncthreads();
-    uint32_t av = warp_count[lane][0], ev = warp_count[lane][1];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, av, o), y = __shfl_up_sync(0xffffffffu, ev, o);
-      if (lane >= o) {
-        av += x;
-        ev += y;
-      }
-    }
-    const uint32_t below = (1u << lane) - 1u;
-    const uint32_t a_before = above_base + (warp ? __shfl_sync(0xffffffffu, av, warp - 1) : 0u) + __popc(am & below);
-    const uint32_t e_before = equal_base + (warp ? __shfl_sync(0xffffffffu, ev, warp - 1) : 0u) + __popc(em & below);
-    if (above || (equal && e_before < wanted)) kept[a.n_sink + a_before + min(e_before, wanted)] = a.n_sink + i;
-    above_base += __shfl_sync(0xffffffffu, av, 31);
-    equal_base += __shfl_sync(0xffffffffu, ev, 31);
-    __syncthreads();
+  // every warp takes a run of the keys, so that only its first place needs the others
+  const int run = (n + SELECT_THREADS - 1) / SELECT_THREADS * 32, w0 = min(n, warp * run), w1 = min(n, w0 + run);
+  uint32_t above_n = 0, equal_n = 0;
+  for (int i = w0 + lane; i < w1; i += 32) {
+    const uint32_t k = in_smem ? keys[i] : key_at(i);
+    above_n += k > prefix;
+    equal_n += k == prefix;
   }
+  above_n = __reduce_add_sync(0xffffffffu, above_n);
+  equal_n = __reduce_add_sync(0xffffffffu, equal_n);
+  if (lane == 0) {
+    warp_count[warp][0] = above_n;
+    warp_count[warp][1] = equal_n;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    above_n = __reduce_add_sync(0xffffffffu, warp_count[lane][0]);
+    equal_n = __reduce_add_sync(0xffffffffu, warp_count[lane][1]);
+    if (lane == 0) {
+      share[0] = above_n;
+      share[1] = equal_n;
+    }
+  }
+  cluster.sync();
+  // kept and equal keys in front of this warp: blocks and warps before it
+  uint32_t a_base = lane < warp ? warp_count[lane][0] : 0u, e_base = lane < warp ? warp_count[lane][1] : 0u;
+  if (lane < rank) {
+    const uint32_t* x = cluster.map_shared_rank(share, lane);
+    a_base += x[0];
+    e_base += x[1];
+  }
+  a_base = __reduce_add_sync(0xffffffffu, a_base);
+  e_base = __reduce_add_sync(0xffffffffu, e_base);
+  for (int i0 = w0; i0 < w1; i0 += 32) {
+    const int i = i0 + lane;
+    const uint32_t k = i < w1 ? (in_smem ? keys[i] : key_at(i)) : 0u;
+    const bool above = i < w1 && k > prefix, equal = i < w1 && k == prefix;
+    const uint32_t am = __ballot_sync(0xffffffffu, above), em = __ballot_sync(0xffffffffu, equal), below = (1u << lane) - 1u;
+    const uint32_t a_before = a_base + __popc(am & below), e_before = e_base + __popc(em & below);
+    if (above || (equal && e_before < wanted)) kept[a.n_sink + a_before + min(e_before, wanted)] = from + i;
+    a_base += __popc(am);
+    e_base += __popc(em);
+  }
+  cluster.sync();                                     // no block leaves while another reads its shares
 }
 
-// The kept tokens into their new pages: one block per (new page, KV head, sequence).
-constexpr int MOVE_THREADS = 128;
+// The kept tokens into their new pages: one block per 128 of a head, i.e. 1 to 8 new pages.  Loads depend on one another three
+// deep: length, position and new page; old page; scales, weight and codes.
+constexpr int MOVE_THREADS = 256;
+constexpr int MOVE_TOKENS = 128;
 template <int D, int KIND>
 __global__ void __launch_bounds__(MOVE_THREADS) cache_move_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ int32_t src_row[128];                    // of every token; -1: none
-  __shared__ float src_scale[2][128];
-  __shared__ float top[2];
+  __shared__ int32_t src_row[MOVE_TOKENS];            // of every token; -1: none
+  __shared__ int32_t dst_row[MOVE_TOKENS];            // of every token; -1: nowhere
+  __shared__ float src_scale[2][MOVE_TOKENS], top[2][MOVE_TOKENS / 16];
   grid_begin();
-  const int page = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int t0 = blockIdx.x * MOVE_TOKENS, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int keep = a.n_sink + a.n_heavy + a.n_recent, page_tokens = a.c.page_tokens;
-  const int n = min(page_tokens, ld_i32(a.new_length + b) - page * page_tokens);
-  if (n <= 0) return;
-  const int32_t dst_page = ld_i32(a.dst_table + (int64_t)b * a.dst_width + page);
-  const int32_t dst_row = page_row(dst_page, a.c.n_pages, a.c.hkv, h, page_tokens);
-  if (dst_row < 0) {
-    if (tid == 0) mark_bad(a.c.status, FCP_CACHE_BAD_PAGE, b);
-    return;
-  }
-  if (tid < n) {
-    const int pos = ld_i32(a.kept + ((int64_t)b * a.c.hkv + h) * keep + page * page_tokens + tid);
-    const int32_t src = ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + pos / page_tokens);
-    int32_t row = page_row(src, a.c.n_pages, a.c.hkv, h, page_tokens);
+  float weight = 0.f;
+  int32_t dst = -1, dst_page = -1;
+  if (tid < MOVE_TOKENS) {
+    const int i = t0 + tid;
+    const bool in = i < keep;
+    const int32_t length = usable_length(a.s, b);
+    const int32_t pos = in ? ld_i32(a.kept + ((int64_t)b * a.c.hkv + h) * keep + i) : -1;
+    dst_page = in ? ld_i32(a.dst_table + (int64_t)b * a.dst_width + (i >> a.c.page_shift)) : -1;
+    int32_t row = -1;
     float ks = 0.f, vs = 0.f;
-    if (row >= 0) {
-      ks = ld_f32(a.c.k_scale + src * a.c.hkv + h);
-      vs = ld_f32(a.c.v_scale + src * a.c.hkv + h);
-    }
-    if (row < 0 || !usable_scale(ks) || !usable_scale(vs)) {
-      mark_bad(a.c.status, row < 0 ? FCP_CACHE_BAD_PAGE : FCP_CACHE_BAD_SCALE, b);
-      row = -1;
-      ks = vs = 0.f;
-    } else {
-      row += pos % page_tokens;
-    }
-    src_row[tid] = row;
-    src_scale[0][tid] = ks;
-    src_scale[1][tid] = vs;
-    a.c.weight[(int64_t)dst_row + tid] = row < 0 ? 0.f : ld_f32(a.c.weight + row);
-  }
-  __syncthreads();
-  if (tid < 64) {                                     // one warp for the keys' scale, one for the values'
-    const int which = tid >> 5;
-    float m = FCP_CACHE_MIN_SCALE;
-    for (int i = tid & 31; i < n; i += 32) m = fmaxf(m, src_scale[which][i]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if ((tid & 31) == 0) {
-      top[which] = m;
-      (which ? a.c.v_scale : a.c.k_scale)[dst_page * a.c.hkv + h] = m;
-    }
-  }
-  __syncthreads();
-  constexpr int C = D / 16;
-  for (int e = tid; e < 2 * n * C; e += MOVE_THREADS) {
-    const int which = e / (n * C), r = e - which * n * C, s = r / C, c = r % C;
-    uint8_t* codes = which ? a.c.v : a.c.k;
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (src_row[s] >= 0) {
-      x = ld_v4(codes + (int64_t)src_row[s] * D + c * 16);
-      if (src_scale[which][s] != top[which]) {
-        const float ratio = __fdiv_rn(src_scale[which][s], top[which]);
-        x = make_uint4(rescale_codes<KIND>(x.x, ratio), rescale_codes<KIND>(x.y, ratio), rescale_codes<KIND>(x.z, ratio), rescale_codes<KIND>(x.w, ratio));
+    if (i < min(length, keep)) {
+      const int32_t at = page_row(dst_page, a.c.n_pages, a.c.hkv, h, page_tokens);
+      if (at < 0) mark_bad(a.c.status, FCP_CACHE_BAD_PAGE, b);
+      else dst = at + (i & (page_tokens - 1));
+      const int32_t src = ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + (pos >> a.c.page_shift));
+      row = page_row(src, a.c.n_pages, a.c.hkv, h, page_tokens);
+      if (row >= 0) {
+        ks = ld_f32(a.c.k_scale + src * a.c.hkv + h);
+        vs = ld_f32(a.c.v_scale + src * a.c.hkv + h);
+        row += (pos & (page_tokens - 1));
+        weight = ld_f32(a.c.weight + row);
       }
     }
-    *reinterpret_cast<uint4*>(codes + ((int64_t)dst_row + s) * D + c * 16) = x;
+    src_row[tid] = row;
+    dst_row[tid] = dst;
+    __syncwarp();
+    src_scale[0][tid] = ks;
+    src_scale[1][tid] = vs;
+  }
+  __syncthreads();
+  constexpr int C = D / 16, N = 2 * MOVE_TOKENS * C / MOVE_THREADS;
+  uint4 x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {                       // codes before the scales are known to be usable
+    const int e = i * MOVE_THREADS + tid, which = e / (MOVE_TOKENS * C), s = e / C % MOVE_TOKENS, c = e % C;
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (src_row[s] >= 0 && dst_row[s] >= 0) x[i] = ld_v4((which ? a.c.v : a.c.k) + (int64_t)src_row[s] * D + c * 16);
+  }
+  if (tid < MOVE_TOKENS && src_row[tid] >= 0 && (!usable_scale(src_scale[0][tid]) || !usable_scale(src_scale[1][tid]))) {
+    mark_bad(a.c.status, FCP_CACHE_BAD_SCALE, b);
+    src_scale[0][tid] = src_scale[1][tid] = 0.f;
+    weight = 0.f;
+  } else if (tid < MOVE_TOKENS && dst >= 0 && src_row[tid] < 0) {
+    mark_bad(a.c.status, FCP_CACHE_BAD_PAGE, b);
+  }
+  if (tid < MOVE_TOKENS && dst >= 0) a.c.weight[dst] = weight;
+  __syncthreads();
+  if (tid < 2 * MOVE_TOKENS) {                        // the largest scale of each new page: 16 threads a piece, then the page's
+    const int which = tid / MOVE_TOKENS, s = tid % MOVE_TOKENS;
+    float m = dst_row[s] >= 0 ? fmaxf(src_scale[which][s], FCP_CACHE_MIN_SCALE) : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (s % 16 == 0) top[which][s / 16] = m;
+  }
+  __syncthreads();
+  const int pieces = page_tokens / 16;
+  auto page_top = [&](int which, int s) {
+    float m = 0.f;
+    const int p = s / 16 / pieces * pieces;
+    for (int i = 0; i < pieces; ++i) m = fmaxf(m, top[which][p + i]);
+    return m;
+  };
+  if (tid < MOVE_TOKENS && tid % page_tokens == 0 && dst >= 0) {
+    a.c.k_scale[dst_page * a.c.hkv + h] = page_top(0, tid);
+    a.c.v_scale[dst_page * a.c.hkv + h] = page_top(1, tid);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = i * MOVE_THREADS + tid, which = e / (MOVE_TOKENS * C), s = e / C % MOVE_TOKENS, c = e % C;
+    if (dst_row[s] < 0) continue;
+    const float from = src_scale[which][s], to = page_top(which, s);
+    if (from == 0.f) {
+      x[i] = make_uint4(0, 0, 0, 0);
+    } else if (from != to) {
+      const float ratio = __fdiv_rn(from, to);
+      x[i] = make_uint4(rescale_codes<KIND>(x[i].x, ratio), rescale_codes<KIND>(x[i].y, ratio), rescale_codes<KIND>(x[i].z, ratio), rescale_codes<KIND>(x[i].w, ratio));
+    }
+    *reinterpret_cast<uint4*>((which ? a.c.v : a.c.k) + (int64_t)dst_row[s] * D + c * 16) = x[i];
   }
 }
 
