@@ -125,11 +125,15 @@ AttnKernel attn_kernel(const fcp_cache_config& c, RowTile t) {
   if (c.head_dim == 128) return c.kind == FCP_CACHE_E4M3 ? attn_kernel<128, FCP_CACHE_E4M3>(t) : attn_kernel<128, FCP_CACHE_INT8>(t);
   return c.kind == FCP_CACHE_E4M3 ? attn_kernel<64, FCP_CACHE_E4M3>(t) : attn_kernel<64, FCP_CACHE_INT8>(t);
 }
-int attn_smem(const fcp_cache_config& c, RowTile t) {
-  const bool one = t.blocks == 1 || t.warps == 0;
-  return c.head_dim == 128 ? (one ? AttnSmem<128, 1>::DYN_BYTES : AttnSmem<128, 2>::DYN_BYTES)
-                           : (one ? AttnSmem<64, 1>::DYN_BYTES : AttnSmem<64, 2>::DYN_BYTES);
+template <int D>
+int attn_smem(RowTile t) {
+  switch (t.warps) {
+    case 0: return AttnSmem<D, kWeights.blocks, 0>::DYN_BYTES;
+    case 1: return t.blocks == 1 ? AttnSmem<D, 1, 1>::DYN_BYTES : AttnSmem<D, 2, 1>::DYN_BYTES;
+    default: return AttnSmem<D, 2, 2>::DYN_BYTES;     // the same for 4 and 8
+  }
 }
+int attn_smem(const fcp_cache_config& c, RowTile t) { return c.head_dim == 128 ? attn_smem<128>(t) : attn_smem<64>(t); }
 
 // The first compute call of a handle: device, kernel attributes, tensor maps.  Later ones: the device is still the current one.
 int ready(const char* call, const fcp_cache* cache) {

@@ -224,8 +224,8 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
 // columns: S^T = K Q^T, O^T = V^T P^T, so that 8 rows (one token of 8 query heads) fill a product.
 constexpr int CT_KEYS = 128;                          // keys of a tile
 constexpr int CT_STEP = 32;                           // keys that a warp takes at a time
-constexpr int CT_WARPS = 8;                           // consumer warps; one more loads
-constexpr int CT_THREADS = (CT_WARPS + 1) * 32;
+constexpr int CT_WARPS = 8;                           // consumer warps; two more load keys and values
+constexpr int CT_THREADS = (CT_WARPS + 2) * 32;
 
 struct AttnArgs {
   CacheView c;
@@ -251,19 +251,26 @@ struct StageMeta {                                    // what a stage holds, for
 enum { ST_FIRST = 1, ST_LAST = 2, ST_WHOLE = 4, ST_END = 8 };
 enum { SP_COUNT = 0, SP_ROW0, SP_N, SP_HEAD, SP_ROW_TILE, SP_W = 8 };
 
-// NR blocks of 8 rows per warp, WR warps side by side: 8 * NR * WR rows of a group.
-template <int D, int NR>
+// NR blocks of 8 rows per warp, WR warps side by side: 8 * NR * WR rows of a group (WR = 0: the weights).
+template <int D, int NR, int WR>
 struct AttnSmem {
   static constexpr int TILE = CT_KEYS * D;            // bytes of K or of V
-  static constexpr int STAGES = D == 64 ? 8 : NR == 1 ? 6 : 4;
+  static constexpr int STAGES = D == 64 ? 8 : NR == 2 && WR > 0 ? 4 : 5;
   static constexpr int RING = STAGES * 2 * TILE;
-  static constexpr int JOIN = CT_WARPS * 8 * NR * D * 4;       // the warps' partial outputs
-  static constexpr int DYN_BYTES = RING + JOIN + 1024;
+  // the queries of a group travel with its first tile where they are few; else the warps fetch their own
+  static constexpr int QUERY_BYTES = WR == 1 ? 8 * NR * D * 2 : 0;
+  static constexpr int JOIN = WR == 0 ? 0 : CT_WARPS * 8 * NR * D * 4;           // the warps' partial outputs
+  static constexpr int DYN_BYTES = RING + STAGES * QUERY_BYTES + JOIN + 1024;
 };
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
 // D (fp32) += A (16 x 16 halves) * B (16 x 8 halves)
@@ -286,14 +293,16 @@ __device__ __forceinline__ float exp2_approx(float x) {
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
 
 // How the tiles of a batch lie in a row: sequence after sequence, its KV heads, their row tiles, their key tiles.
+// A group counts for GROUP_COST tiles more than it has, for what its queries and its end take: TODO
 struct TileOrder {
+  static constexpr int GROUP_COST = 2;
   int32_t rows_per_tile, group, hkv;
   bool all_rows;                                      // one group per KV head, whatever its rows (the weights)
   __device__ __forceinline__ int32_t row_tiles(const SeqView& s) const {
     return s.n <= 0 ? 0 : all_rows ? 1 : (s.n * group + rows_per_tile - 1) / rows_per_tile;
   }
   __device__ __forceinline__ int32_t key_tiles(const SeqView& s) const { return s.length <= 0 ? 1 : (s.length + CT_KEYS - 1) / CT_KEYS; }
-  __device__ __forceinline__ int64_t tiles(const SeqView& s) const { return (int64_t)row_tiles(s) * hkv * key_tiles(s); }
+  __device__ __forceinline__ int64_t tiles(const SeqView& s) const { return (int64_t)row_tiles(s) * hkv * (key_tiles(s) + GROUP_COST); }
 };
 
 struct CtaRange {
@@ -367,7 +376,8 @@ struct QueryRows {
   int32_t limit[NR][2];                               // keys in front of this position are seen; 0: no such row
   int32_t least, most;                                // of the rows that exist
 
-  __device__ __forceinline__ void fill(const AttnArgs& A, const StageMeta& m, int first_row, int lane) {
+  // `rows`: where the rows from first_row on lie in shared memory; NULL: they are fetched
+  __device__ __forceinline__ void fill(const AttnArgs& A, const StageMeta& m, int first_row, int lane, const uint8_t* rows) {
     const int g = lane >> 2, t = lane & 3, n_rows = m.n * A.group;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
@@ -377,7 +387,7 @@ struct QueryRows {
         const __nv_bfloat16* p = A.q + (int64_t)(m.row0 + j) * A.q_stride + (m.head * A.group + r - j * A.group) * D + t * (D / 4);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
-          const uint4 x = ld_v4(p + c * 8);
+          const uint4 x = rows ? *reinterpret_cast<const uint4*>(rows + (8 * i + g) * (2 * D) + t * (D / 2) + c * 16) : ld_v4(p + c * 8);
           w[4 * c] = x.x; w[4 * c + 1] = x.y; w[4 * c + 2] = x.z; w[4 * c + 3] = x.w;
         }
       } else {
@@ -442,120 +452,204 @@ __device__ __forceinline__ void scores(const QueryRows<D, NR>& q, const uint8_t*
   }
 }
 
-// Loading warp: walks the CTA's tiles.  Lanes look 32 sub-blocks of 16 keys (four stages) ahead in page table and scales.
-template <int D, int NR, bool WEIGHTS>
-__device__ __forceinline__ void attn_producer(const AttnArgs& A, const CUtensorMap* tk, const CUtensorMap* tv, const TileOrder& order,
-                                              const CtaRange& range, uint32_t ring, StageMeta* meta, uint32_t full, uint32_t empty,
-                                              const WaitCtx& ctx) {
-  using S = AttnSmem<D, NR>;
-  constexpr int SUBS = CT_KEYS / 16;
-  const int lane = threadIdx.x & 31, sub = lane & (SUBS - 1);
-  const int page_tokens = A.c.page_tokens;
-  const bool leads = (sub * 16) % A.box == 0;         // this lane's sub-block begins a box
-  int64_t at = range.begin, seq_begin = range.seq_begin;
-  int b = range.b, stage = 0;
-  uint32_t phase = 0;
-  int32_t split[SP_W] = {0, 0, 0, 0, 0, 0, 0, 0};
-  bool ok = true;
-  while (ok && at < range.end) {
-    SeqView s = load_seq(A.s, b);
-    int64_t n = order.tiles(s);
-    while (at >= seq_begin + n) {                     // sequences without tiles
-      seq_begin += n;
-      s = load_seq(A.s, ++b);
-      n = order.tiles(s);
+// A run of at most four tiles of one group, as the loading warp sees it.  Lane l stands for 16 keys of it: tile l / 8, sub-block l % 8.
+struct TileRun {
+  SeqView s;
+  int32_t b, head, row_tile, tile, tiles, seen;       // seen: keys in front of this position are of use
+  bool first, last, begins, ends;                     // of the group's tiles on this CTA; of the group
+  int32_t page, row;                                  // this lane's page, and the row of its first code (-1: none)
+  float ks, vs;
+};
+
+// A loading warp walks the CTA's tiles.  Page numbers are fetched two runs ahead, the scales they lead to one run ahead, so that
+// the loop waits for neither; fetched when needed, the two in a row held the ring up for 1 to 2 us in every four tiles.
+template <int D, int NR, int WR>
+struct AttnProducer {
+  using S = AttnSmem<D, NR, WR>;
+  static constexpr bool WEIGHTS = WR == 0;
+  static constexpr int SUBS = CT_KEYS / 16;
+  const AttnArgs& A;
+  const TileOrder& order;
+  const CtaRange& range;
+  int64_t at, group_end;                              // next tile to hand out (in the order's units), end of its group
+  int64_t seq_begin;
+  SeqView s, ahead;                                   // of sequence b and of the next one
+  int32_t b, kt, rt_n, head, rt, tile;
+  bool fresh;                                         // no run handed out yet
+  int32_t split[SP_W];
+
+  __device__ __forceinline__ AttnProducer(const AttnArgs& A, const TileOrder& order, const CtaRange& range) : A(A), order(order), range(range) {
+#pragma unroll
+    for (int i = 0; i < SP_W; ++i) split[i] = 0;
+    fresh = true;
+    at = range.begin;
+    seq_begin = range.seq_begin;
+    b = range.b;
+    if (at >= range.end) return;
+    s = load_seq(A.s, b);
+    look_ahead();
+    enter();
+  }
+  __device__ __forceinline__ void look_ahead() {
+    ahead = {0, 0, 0, 0};
+    if (b + 1 < A.s.B) ahead = load_seq(A.s, b + 1);
+  }
+  // The group that `at` lies in.  It occupies GROUP_COST units more than it has tiles, the first ones.
+  __device__ __forceinline__ void enter() {
+    while (at >= seq_begin + order.tiles(s)) {
+      seq_begin += order.tiles(s);
+      ++b;
+      s = ahead;
+      look_ahead();
     }
-    const int kt = order.key_tiles(s), rt_n = order.row_tiles(s);
-    const int64_t rel = at - seq_begin, grp = rel / kt;
-    const int tile0 = (int)(rel - grp * kt), head = (int)(grp / rt_n), rt = (int)(grp - (int64_t)head * rt_n);
-    const int tiles = (int)min((int64_t)(kt - tile0), range.end - at);
-    const bool begins = tile0 == 0, ends = tile0 + tiles == kt;
-    // keys that the last row of the row tile sees
+    kt = order.key_tiles(s);
+    rt_n = order.row_tiles(s);
+    const int64_t rel = at - seq_begin, grp = rel / (kt + TileOrder::GROUP_COST);
+    head = (int)(grp / rt_n);
+    rt = (int)(grp - (int64_t)head * rt_n);
+    group_end = seq_begin + (grp + 1) * (kt + TileOrder::GROUP_COST);
+    at = max(at, group_end - kt);
+    tile = kt - (int)(group_end - at);
+  }
+  // The next run, its pages on their way; false: none left.
+  __device__ __forceinline__ bool next(TileRun& r, int lane) {
+    if (at >= range.end) return false;
+    const int left = (int)(min(group_end, range.end) - at);
+    r.s = s;
+    r.b = b;
+    r.head = head;
+    r.row_tile = rt;
+    r.tile = tile;
+    r.tiles = min(left, 4);
+    r.begins = tile == 0;
+    r.first = tile == 0 || fresh;
+    fresh = false;
+    r.last = r.tiles == left;
+    r.ends = group_end <= range.end;
     const int last_row = min((rt + 1) * order.rows_per_tile, s.n * A.group) - 1;
-    const int seen = WEIGHTS ? s.length : s.length - s.n + last_row / A.group + 1;
-    if (begins && !ends) {
-      split[SP_COUNT] = (int)((seq_begin + (grp + 1) * kt - 1) / range.per) - (int)blockIdx.x;
+    r.seen = WEIGHTS ? s.length : s.length - s.n + last_row / A.group + 1;
+    const int key = (tile + lane / SUBS) * CT_KEYS + (lane % SUBS) * 16;
+    r.page = -1;
+    r.row = -2;                                       // nothing to load
+    if (lane / SUBS < r.tiles && key < r.seen) {
+      r.page = ld_i32(A.s.page_table + (int64_t)b * A.s.table_width + (key >> A.c.page_shift));
+      r.row = key & (A.c.page_tokens - 1);
+    }
+    if (tile == 0 && !r.ends) {
+      split[SP_COUNT] = (int)((group_end - 1) / range.per) - (int)blockIdx.x;
       split[SP_ROW0] = s.row0; split[SP_N] = s.n; split[SP_HEAD] = head; split[SP_ROW_TILE] = rt;
     }
-    for (int i0 = 0; ok && i0 < tiles; i0 += 4) {
-      float ks = 0.f, vs = 1.f;
-      int32_t row = -1;
-      const int my_tile = i0 + lane / SUBS, key = (tile0 + my_tile) * CT_KEYS + sub * 16;
-      if (my_tile < tiles && key < seen) {
-        const int32_t page = ld_i32(A.s.page_table + (int64_t)b * A.s.table_width + (key >> A.c.page_shift));
-        row = page_row(page, A.c.n_pages, A.c.hkv, head, page_tokens);
-        if (row >= 0) {
-          ks = ld_f32(A.c.k_scale + page * A.c.hkv + head);
-          vs = ld_f32(A.c.v_scale + page * A.c.hkv + head);
-          row += (key & (page_tokens - 1));
-        }
-        if (row < 0 || !usable_scale(ks) || !usable_scale(vs)) {
-          mark_bad(A.c.status, row < 0 ? FCP_CACHE_BAD_PAGE : FCP_CACHE_BAD_SCALE, b);
-          row = -1;
-          ks = 0.f;
-          vs = 1.f;
-        }
+    at += r.tiles;
+    tile += r.tiles;
+    if (at >= group_end && at < range.end) enter();
+    return true;
+  }
+  __device__ __forceinline__ void fetch_scales(TileRun& r) {
+    r.ks = r.vs = 0.f;
+    if (r.row < 0) return;
+    const int32_t at_page = page_row(r.page, A.c.n_pages, A.c.hkv, r.head, A.c.page_tokens);
+    if (at_page < 0) {
+      r.row = -1;
+      return;
+    }
+    r.row += at_page;
+    r.ks = ld_f32(A.c.k_scale + r.page * A.c.hkv + r.head);
+    r.vs = ld_f32(A.c.v_scale + r.page * A.c.hkv + r.head);
+  }
+
+  // `map`: of the keys, or of the values (is_v); the keys' warp also describes the stages and fetches the queries.
+  __device__ __forceinline__ void run(const CUtensorMap* map, int is_v, uint32_t ring, uint32_t queries, StageMeta* meta, uint32_t full,
+                                      uint32_t empty, const WaitCtx& ctx) {
+    const int lane = threadIdx.x & 31, sub = lane & (SUBS - 1);
+    const bool leads = (sub * 16) % A.box == 0;       // this lane's sub-block begins a box
+    int stage = 0;
+    uint32_t phase = 0;
+    TileRun now, soon, later;
+    bool have = next(now, lane), have_soon = have && next(soon, lane), have_later = false;
+    if (have) fetch_scales(now);
+    bool ok = true, whole = false, from_start = false;
+    while (have) {
+      if (have_soon) fetch_scales(soon);
+      have_later = have_soon && next(later, lane);
+      const bool bad = now.row == -1 || (now.row >= 0 && (!usable_scale(now.ks) || !usable_scale(now.vs)));
+      if (bad) {
+        mark_bad(A.c.status, now.row == -1 ? FCP_CACHE_BAD_PAGE : FCP_CACHE_BAD_SCALE, now.b);
+        now.row = -1;
       }
-      const float4 about = make_float4(ks, __log2f(vs), 1.f / vs, __int_as_float(row));
-      for (int i = i0; i < min(i0 + 4, tiles); ++i) {
+      const bool usable = now.row >= 0;
+      const float4 about = usable ? make_float4(now.ks, __log2f(now.vs), 1.f / now.vs, __int_as_float(now.row)) : make_float4(0.f, 0.f, 1.f, 0.f);
+      for (int i = 0; i < now.tiles; ++i) {
         if (!mbar_wait_warp(empty + stage * 8, phase ^ 1, ctx, 911)) {
           ok = false;
           break;
         }
-        const bool here = lane / SUBS == i - i0;
-        const bool loads = here && leads && row >= 0;
+        const bool here = lane / SUBS == i, loads = here && leads && usable;
+        const bool first = now.first && i == 0, last = now.last && i == now.tiles - 1;
         const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, loads));
         StageMeta& m = meta[stage];
-        if (here) m.sub[sub] = about;
-        if (lane == 0) {
-          m.row0 = s.row0; m.n = s.n; m.length = s.length; m.head = head;
-          m.row_tile = rt;
-          m.key0 = (tile0 + i) * CT_KEYS;
-          m.flags = (i == 0 ? ST_FIRST : 0) | (i == tiles - 1 ? ST_LAST : 0) | (begins && ends ? ST_WHOLE : 0);
-          m.part = 2 * (int)blockIdx.x + (begins ? 1 : 0);
+        if (here && !is_v) m.sub[sub] = about;
+        if (first) {
+          from_start = now.begins;
+          whole = now.begins && now.ends;
+        }
+        if (lane == 0 && !is_v) {
+          m.row0 = now.s.row0; m.n = now.s.n; m.length = now.s.length; m.head = now.head;
+          m.row_tile = now.row_tile;
+          m.key0 = (now.tile + i) * CT_KEYS;
+          m.flags = (first ? ST_FIRST : 0) | (last ? ST_LAST : 0) | (whole ? ST_WHOLE : 0);
+          m.part = 2 * (int)blockIdx.x + (from_start ? 1 : 0);
         }
         __syncwarp();
         const uint32_t bar = full + stage * 8;
+        // the queries of a group travel with its first tile, a row per lane
+        const int row = now.row_tile * order.rows_per_tile + lane;
+        const bool asks = S::QUERY_BYTES > 0 && !is_v && first && lane < order.rows_per_tile && row < now.s.n * A.group;
+        const uint32_t rows = __popc(__ballot_sync(0xffffffffu, asks));
         if (lane == 0) {
-          const uint32_t bytes = boxes * (uint32_t)(A.box * D) * (WEIGHTS ? 1u : 2u);
+          const uint32_t bytes = boxes * (uint32_t)(A.box * D) + rows * (uint32_t)(2 * D);
           if (bytes) mbar_expect_tx(bar, bytes);
           else mbar_arrive(bar);
         }
         __syncwarp();
-        if (loads) {
-          const uint32_t dst = ring + stage * 2 * S::TILE + sub * 16 * D;
-          tma_load_2d(dst, tk, bar, 0, row);
-          if (!WEIGHTS) tma_load_2d(dst + S::TILE, tv, bar, 0, row);
+        if (asks) {
+          const int j = row / A.group;
+          bulk_load(queries + (stage * order.rows_per_tile + lane) * (2 * D),
+                    A.q + (int64_t)(now.s.row0 + j) * A.q_stride + (now.head * A.group + row - j * A.group) * D, 2 * D, bar);
         }
+        if (loads) tma_load_2d(ring + stage * 2 * S::TILE + is_v * S::TILE + sub * 16 * D, map, bar, 0, now.row);
         __syncwarp();
         if (++stage == S::STAGES) {
           stage = 0;
           phase ^= 1;
         }
       }
+      if (!ok) break;
+      now = soon;
+      soon = later;
+      have = have_soon;
+      have_soon = have_later;
     }
-    at += tiles;
-  }
-  grid_launch_next();
-  if (ok && mbar_wait_warp(empty + stage * 8, phase ^ 1, ctx, 912)) {
-    if (lane == 0) {
-      meta[stage].flags = ST_END;
-      mbar_arrive(full + stage * 8);
+    grid_launch_next();
+    if (ok && mbar_wait_warp(empty + stage * 8, phase ^ 1, ctx, 912)) {
+      if (lane == 0) {
+        if (!is_v) meta[stage].flags = ST_END;
+        mbar_arrive(full + stage * 8);
+      }
     }
-  }
-  if (!WEIGHTS && lane < SP_W) {
-    int32_t x = 0;
+    if (!WEIGHTS && !is_v && lane < SP_W) {
+      int32_t x = 0;
 #pragma unroll
-    for (int i = 0; i < SP_W; ++i) x = lane == i ? split[i] : x;
-    A.split[blockIdx.x * SP_W + lane] = x;
+      for (int i = 0; i < SP_W; ++i) x = lane == i ? split[i] : x;
+      A.split[blockIdx.x * SP_W + lane] = x;
+    }
   }
-}
+};
 
 // WR warps side by side hold the rows of a tile, 8 * NR each; the 8 / WR warps behind each other take different keys: 32 of a
 // tile (64, 128 with four, eight warps side by side), with one warp side by side of every second tile only.
 template <int D, int KIND, int NR, int WR>
 struct AttnConsumer {
-  using S = AttnSmem<D, NR>;
+  using S = AttnSmem<D, NR, WR>;
   static constexpr int RT = 8 * NR * WR, KG = CT_WARPS / WR, MT = D / 16;
   static constexpr int STEPS = WR <= 2 ? 1 : WR / 2;  // of 32 keys, per warp and tile
   QueryRows<D, NR> q;
@@ -709,6 +803,7 @@ struct AttnConsumer {
     const int g = lane >> 2, t = lane & 3, tid = warp * 32 + lane;
     asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory");       // the join area's last readers are done
     float4* mine = join + warp * 8 * NR * (D / 4);
+    const int n_rows = min(RT, meta.n * A.group - meta.row_tile * RT);
 #pragma unroll
     for (int i = 0; i < NR; ++i)
 #pragma unroll
@@ -717,13 +812,13 @@ struct AttnConsumer {
         l[i][r] += __shfl_xor_sync(0xffffffffu, l[i][r], 8);
         l[i][r] += __shfl_xor_sync(0xffffffffu, l[i][r], 16);
         const int row = 8 * i + 2 * t + r;
+        if (warp % WR * 8 * NR + row >= n_rows) continue;
         if (g == 0) stats[warp * 8 * NR + row] = make_float2(ref[i][r], l[i][r]);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
           mine[join_slot(row, g * (D / 32) + c)] = make_float4(o[i][2 * c][r], o[i][2 * c][r + 2], o[i][2 * c + 1][r], o[i][2 * c + 1][r + 2]);
       }
     asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory");
-    const int n_rows = min(RT, meta.n * A.group - meta.row_tile * RT);
     for (int e = tid; e < n_rows * (D / 4); e += CT_WARPS * 32) {
       const int r = e / (D / 4), f = e % (D / 4), wr = r / (8 * NR), row = r % (8 * NR);
       float top = -3e38f;
@@ -754,7 +849,7 @@ struct AttnConsumer {
     }
   }
 
-  __device__ __forceinline__ void run(const AttnArgs& A, const uint8_t* ring, const StageMeta* metas, float4* join, float2* stats,
+  __device__ __forceinline__ void run(const AttnArgs& A, const uint8_t* ring, const uint8_t* queries, const StageMeta* metas, float4* join, float2* stats,
                                       uint32_t full, uint32_t empty, const WaitCtx& ctx) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, kg = warp / WR;
     const int turn = WR == 1 ? kg >> 2 : 0, first = (WR == 1 ? kg & 3 : kg) * STEPS;       // which tiles, which 32 keys of them
@@ -765,7 +860,7 @@ struct AttnConsumer {
       const int flags = meta.flags;
       if (flags & ST_END) break;
       if (flags & ST_FIRST) {
-        q.fill(A, meta, meta.row_tile * RT + wr * 8 * NR, lane);
+        q.fill(A, meta, meta.row_tile * RT + wr * 8 * NR, lane, S::QUERY_BYTES ? queries + stage * S::QUERY_BYTES : nullptr);
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
           ref[i][0] = ref[i][1] = -3e38f;
@@ -800,7 +895,7 @@ struct AttnConsumer {
 template <int D, int KIND, int NR>
 __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t* ring, const StageMeta* metas, uint32_t full,
                                                 uint32_t empty, const WaitCtx& ctx) {
-  using S = AttnSmem<D, 1>;
+  using S = AttnSmem<D, NR, 0>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int stage = 0;
   uint32_t phase = 0;
@@ -812,7 +907,7 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
     const int key = meta.key0 + warp * 16, n_rows = meta.n * A.group;
     const float4 about = meta.sub[warp];
     auto rows_from = [&](int r0) {
-      q.fill(A, meta, r0, lane);
+      q.fill(A, meta, r0, lane, nullptr);
 #pragma unroll
       for (int i = 0; i < NR; ++i)
 #pragma unroll
@@ -856,22 +951,23 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
 template <int D, int KIND, int NR, int WR>
 __global__ void __launch_bounds__(CT_THREADS, 1)
 cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ AttnArgs A) {
-  using S = AttnSmem<D, WR ? NR : 1>;
+  using S = AttnSmem<D, NR, WR>;
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[2 * S::STAGES];
   __shared__ __align__(16) StageMeta metas[S::STAGES];
-  __shared__ float2 stats[CT_WARPS * 8 * (WR ? NR : 1)];
+  __shared__ float2 stats[WR ? CT_WARPS * 8 * NR : 1];
   __shared__ int64_t scratch[16];
   __shared__ int abort_flag;
   const int warp = threadIdx.x >> 5;
   const uint32_t full = smem_u32(bars), empty = full + S::STAGES * 8;
   // the swizzle pattern repeats every 1024 bytes of address
   const uint32_t skip = (1024u - (smem_u32(smem) & 1023u)) & 1023u;
-  uint8_t* base = smem + skip;
+  uint8_t* ring = smem + skip;
+  uint8_t* queries = ring + S::RING;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < S::STAGES; ++i) {
-      mbar_init(full + i * 8, 1);
+      mbar_init(full + i * 8, WR ? 2 : 1);
       mbar_init(empty + i * 8, CT_WARPS);
     }
     fence_mbar_init();
@@ -881,15 +977,16 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   grid_wait();
   __syncthreads();
   const WaitCtx ctx = {&abort_flag, A.c.status, (uint32_t)FCP_WAIT_NS};
-  TileOrder order = {8 * NR * (WR ? WR : 1), A.group, A.c.hkv, WR == 0};
+  const TileOrder order = {8 * NR * (WR ? WR : 1), A.group, A.c.hkv, WR == 0};
   const CtaRange range = cta_range(A.s, order, A.c.status, scratch);
-  if (warp == CT_WARPS) {
-    attn_producer<D, WR ? NR : 1, WR == 0>(A, &tk, &tv, order, range, smem_u32(base), metas, full, empty, ctx);
+  if (warp >= CT_WARPS) {
+    AttnProducer<D, NR, WR> producer(A, order, range);
+    if (warp == CT_WARPS || WR > 0) producer.run(warp == CT_WARPS ? &tk : &tv, warp - CT_WARPS, smem_u32(ring), smem_u32(queries), metas, full, empty, ctx);
   } else if constexpr (WR == 0) {
-    weight_consumer<D, KIND, NR>(A, base, metas, full, empty, ctx);
+    weight_consumer<D, KIND, NR>(A, ring, metas, full, empty, ctx);
   } else {
     AttnConsumer<D, KIND, NR, WR> consumer;
-    consumer.run(A, base, metas, reinterpret_cast<float4*>(base + S::RING), stats, full, empty, ctx);
+    consumer.run(A, ring, queries, metas, reinterpret_cast<float4*>(queries + S::STAGES * S::QUERY_BYTES), stats, full, empty, ctx);
   }
   __syncthreads();
   wait_teardown(ctx);
