@@ -27,7 +27,7 @@ struct RowTile {
   int blocks, warps;                                  // blocks of 8 rows per warp, warps side by side
   int rows() const { return 8 * blocks * warps; }
 };
-constexpr RowTile kWeights = {4, 0};
+constexpr RowTile kWeights = {16, 0};
 RowTile row_tile(int64_t rows) {
   return rows <= 8 ? RowTile{1, 1} : rows <= 16 ? RowTile{2, 1} : rows <= 32 ? RowTile{2, 2} : rows <= 64 ? RowTile{2, 4} : RowTile{2, 8};
 }
@@ -130,7 +130,9 @@ int attn_smem(RowTile t) {
   switch (t.warps) {
     case 0: return AttnSmem<D, kWeights.blocks, 0>::DYN_BYTES;
     case 1: return t.blocks == 1 ? AttnSmem<D, 1, 1>::DYN_BYTES : AttnSmem<D, 2, 1>::DYN_BYTES;
-    default: return AttnSmem<D, 2, 2>::DYN_BYTES;     // the same for 4 and 8
+    case 2: return AttnSmem<D, 2, 2>::DYN_BYTES;
+    case 4: return AttnSmem<D, 2, 4>::DYN_BYTES;
+    default: return AttnSmem<D, 2, 8>::DYN_BYTES;
   }
 }
 int attn_smem(const fcp_cache_config& c, RowTile t) { return c.head_dim == 128 ? attn_smem<128>(t) : attn_smem<64>(t); }

@@ -251,16 +251,19 @@ struct StageMeta {                                    // what a stage holds, for
 enum { ST_FIRST = 1, ST_LAST = 2, ST_WHOLE = 4, ST_END = 8 };
 enum { SP_COUNT = 0, SP_ROW0, SP_N, SP_HEAD, SP_ROW_TILE, SP_W = 8 };
 
-// NR blocks of 8 rows per warp, WR warps side by side: 8 * NR * WR rows of a group (WR = 0: the weights).
+// NR blocks of 8 rows per warp, WR warps side by side: 8 * NR * WR rows of a group (WR = 0: the weights, NR blocks at a time).
 template <int D, int NR, int WR>
 struct AttnSmem {
+  static constexpr int BLOCKS = NR * (WR ? WR : 1), ROWS = 8 * BLOCKS;
   static constexpr int TILE = CT_KEYS * D;            // bytes of K or of V
-  static constexpr int STAGES = D == 64 ? 8 : NR == 2 && WR > 0 ? 4 : 5;
-  static constexpr int RING = STAGES * 2 * TILE;
-  // the queries of a group travel with its first tile where they are few; else the warps fetch their own
-  static constexpr int QUERY_BYTES = WR == 1 ? 8 * NR * D * 2 : 0;
+  static constexpr int STAGE = WR ? 2 * TILE : TILE;
+  static constexpr int STAGES = D == 64 || WR == 0 ? 8 : WR == 8 ? 3 : NR == 2 ? 4 : 5;
+  static constexpr int RING = STAGES * STAGE;
+  // the queries of a group travel with its first tile where they are few; else the warps fetch them
+  static constexpr int QUERY_BYTES = WR == 1 ? ROWS * D * 2 : 0;
+  static constexpr int FRAGS = ROWS * D * 2;          // the queries as operands
   static constexpr int JOIN = WR == 0 ? 0 : CT_WARPS * 8 * NR * D * 4;           // the warps' partial outputs
-  static constexpr int DYN_BYTES = RING + STAGES * QUERY_BYTES + JOIN + 1024;
+  static constexpr int DYN_BYTES = RING + STAGES * QUERY_BYTES + FRAGS + JOIN + 1024;
 };
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
@@ -365,29 +368,35 @@ __device__ __forceinline__ CtaRange cta_range(const BatchView& s, const TileOrde
   return r;
 }
 
-// NR blocks of 8 rows.  As the operand of S^T = K Q^T, thread (g, t) holds row g of a block and of it the columns
-// [t * D / 4, (t + 1) * D / 4): the sum over columns may be taken in any order, as long as queries and keys agree.  Of the
-// result it has rows 2t and 2t + 1, and so of everything that goes with rows.
-template <int D, int NR>
-struct QueryRows {
+// The rows of a group's tile in shared memory: queries as the 8-column operand of S^T = K Q^T, and what goes with each row.
+// Thread (g, t) of the operand holds row g of a block and of it the columns [t * D / 4, (t + 1) * D / 4): the sum over columns
+// may be taken in any order, as long as queries and keys agree.  In registers they would take half a warp's budget.
+struct RowInfo {
+  float factor;                                       // score of the product -> log2 units, without the key scale
+  int32_t limit;                                      // keys in front of this position are seen; 0: no such row
+  float lse2;                                         // for the weights
+  int32_t unused;
+};
+template <int D>
+struct QueryArea {
   static constexpr int KS = D / 16;                   // steps of 16 columns
-  uint32_t b[NR][KS][2];
-  float factor[NR][2];                                // score of the product -> log2 units, without the key scale
-  int32_t limit[NR][2];                               // keys in front of this position are seen; 0: no such row
-  int32_t least, most;                                // of the rows that exist
+  uint2* frag;                                        // [block][KS][32 lanes]
+  RowInfo* row;
 
-  // `rows`: where the rows from first_row on lie in shared memory; NULL: they are fetched
-  __device__ __forceinline__ void fill(const AttnArgs& A, const StageMeta& m, int first_row, int lane, const uint8_t* rows) {
+  // Blocks of 8 rows from first_row on, a warp each.  `raw`: where the rows lie in shared memory; NULL: they are fetched.
+  template <bool WEIGHTS>
+  __device__ __forceinline__ void fill(const AttnArgs& A, const StageMeta& m, int first_row, int blocks, const uint8_t* raw, int warp, int lane) const {
     const int g = lane >> 2, t = lane & 3, n_rows = m.n * A.group;
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
+    for (int i = warp; i < blocks; i += CT_WARPS) {
       const int r = first_row + 8 * i + g, j = r / A.group;
+      const int64_t token = m.row0 + j;
+      const int head = m.head * A.group + r - j * A.group;
       uint32_t w[D / 8];
       if (r < n_rows) {
-        const __nv_bfloat16* p = A.q + (int64_t)(m.row0 + j) * A.q_stride + (m.head * A.group + r - j * A.group) * D + t * (D / 4);
+        const __nv_bfloat16* p = A.q + token * A.q_stride + head * D + t * (D / 4);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
-          const uint4 x = rows ? *reinterpret_cast<const uint4*>(rows + (8 * i + g) * (2 * D) + t * (D / 2) + c * 16) : ld_v4(p + c * 8);
+          const uint4 x = raw ? *reinterpret_cast<const uint4*>(raw + (8 * i + g) * (2 * D) + t * (D / 2) + c * 16) : ld_v4(p + c * 8);
           w[4 * c] = x.x; w[4 * c + 1] = x.y; w[4 * c + 2] = x.z; w[4 * c + 3] = x.w;
         }
       } else {
@@ -403,24 +412,22 @@ struct QueryRows {
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = max((int)(top >> 7), 20);         // biased exponent; 20: smaller rows are taken as they are scaled then
       const float up = __uint_as_float((uint32_t)(262 - e) << 23);                     // 2^(8 - (e - 127)), e <= 255
-      const float f = A.scale_log2 * __uint_as_float((uint32_t)(e - 8) << 23);         // 2^(e - 127 - 8)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        b[i][k][0] = pack_half(bf_lo(w[2 * k]) * up, bf_hi(w[2 * k]) * up);
-        b[i][k][1] = pack_half(bf_lo(w[2 * k + 1]) * up, bf_hi(w[2 * k + 1]) * up);
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int row = first_row + 8 * i + 2 * t + c;
-        factor[i][c] = __shfl_sync(0xffffffffu, f, (2 * t + c) * 4);
-        limit[i][c] = row < n_rows ? m.length - m.n + row / A.group + 1 : 0;
+      for (int k = 0; k < KS; ++k)
+        frag[(i * KS + k) * 32 + lane] = make_uint2(pack_half(bf_lo(w[2 * k]) * up, bf_hi(w[2 * k]) * up),
+                                                    pack_half(bf_lo(w[2 * k + 1]) * up, bf_hi(w[2 * k + 1]) * up));
+      if (t == 0) {
+        RowInfo x;
+        x.factor = A.scale_log2 * __uint_as_float((uint32_t)(e - 8) << 23);            // 2^(e - 127 - 8)
+        x.limit = r < n_rows ? m.length - m.n + j + 1 : 0;
+        x.lse2 = WEIGHTS && r < n_rows ? ld_f32(A.lse + token * A.hq + head) * 1.4426950408889634f : INFINITY;
+        x.unused = 0;
+        row[8 * i + g] = x;
       }
     }
-    const int last = min(first_row + 8 * NR, n_rows) - 1;
-    least = m.length - m.n + first_row / A.group + 1;
-    most = first_row < n_rows ? m.length - m.n + last / A.group + 1 : 0;
   }
 };
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory"); }
 
 // 16 bytes `chunk` of key `key` of a tile, as TMA has swizzled them.
 template <int D>
@@ -432,23 +439,34 @@ __device__ __forceinline__ void words(const uint8_t* p, uint32_t* w) {
   w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
 }
 
-// Scores of 16 keys from `key0` of the tile on, against NR blocks of rows: s[i] = (key g | g + 8) x (row 2t | 2t + 1).
-template <int D, int KIND, int NR>
-__device__ __forceinline__ void scores(const QueryRows<D, NR>& q, const uint8_t* tile, int key0, int lane, float (&s)[NR][4]) {
+// Scores of HB blocks of 16 keys from `key0` of the tile on, against NR blocks of rows: s[h][i] = (key g | g + 8) x (row 2t | 2t + 1).
+template <int D, int KIND, int HB, int NR>
+__device__ __forceinline__ void scores(const uint2* frag, const uint8_t* tile, int key0, int lane, float (&s)[HB][NR][4]) {
   const int g = lane >> 2, t = lane & 3;
-  uint32_t lo[D / 16], hi[D / 16];                    // of keys g and g + 8
+#pragma unroll
+  for (int h = 0; h < HB; ++h)
+#pragma unroll
+    for (int i = 0; i < NR; ++i) s[h][i][0] = s[h][i][1] = s[h][i][2] = s[h][i][3] = 0.f;
 #pragma unroll
   for (int c = 0; c < D / 64; ++c) {
-    words(tile_at<D>(tile, key0 + g, t * (D / 64) + c), lo + 4 * c);
-    words(tile_at<D>(tile, key0 + g + 8, t * (D / 64) + c), hi + 4 * c);
-  }
+    uint32_t lo[HB][4], hi[HB][4];                    // of keys g and g + 8
 #pragma unroll
-  for (int i = 0; i < NR; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+    for (int h = 0; h < HB; ++h) {
+      words(tile_at<D>(tile, key0 + 16 * h + g, t * (D / 64) + c), lo[h]);
+      words(tile_at<D>(tile, key0 + 16 * h + g + 8, t * (D / 64) + c), hi[h]);
+    }
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) {
-    const uint32_t a0 = halves_lo<KIND>(lo[k]), a1 = halves_lo<KIND>(hi[k]), a2 = halves_hi<KIND>(lo[k]), a3 = halves_hi<KIND>(hi[k]);
+    for (int k = 0; k < 4; ++k) {
+      uint2 b[NR];
 #pragma unroll
-    for (int i = 0; i < NR; ++i) mma_f16(s[i], a0, a1, a2, a3, q.b[i][k][0], q.b[i][k][1]);
+      for (int i = 0; i < NR; ++i) b[i] = frag[(i * (D / 16) + 4 * c + k) * 32 + lane];
+#pragma unroll
+      for (int h = 0; h < HB; ++h) {
+        const uint32_t a0 = halves_lo<KIND>(lo[h][k]), a1 = halves_lo<KIND>(hi[h][k]), a2 = halves_hi<KIND>(lo[h][k]), a3 = halves_hi<KIND>(hi[h][k]);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) mma_f16(s[h][i], a0, a1, a2, a3, b[i].x, b[i].y);
+      }
+    }
   }
 }
 
@@ -616,7 +634,7 @@ struct AttnProducer {
           bulk_load(queries + (stage * order.rows_per_tile + lane) * (2 * D),
                     A.q + (int64_t)(now.s.row0 + j) * A.q_stride + (now.head * A.group + row - j * A.group) * D, 2 * D, bar);
         }
-        if (loads) tma_load_2d(ring + stage * 2 * S::TILE + is_v * S::TILE + sub * 16 * D, map, bar, 0, now.row);
+        if (loads) tma_load_2d(ring + stage * S::STAGE + is_v * S::TILE + sub * 16 * D, map, bar, 0, now.row);
         __syncwarp();
         if (++stage == S::STAGES) {
           stage = 0;
@@ -652,7 +670,9 @@ struct AttnConsumer {
   using S = AttnSmem<D, NR, WR>;
   static constexpr int RT = 8 * NR * WR, KG = CT_WARPS / WR, MT = D / 16;
   static constexpr int STEPS = WR <= 2 ? 1 : WR / 2;  // of 32 keys, per warp and tile
-  QueryRows<D, NR> q;
+  const uint2* frag;                                  // this warp's rows
+  float factor[NR][2];                                // of rows 2t and 2t + 1 of each block
+  int32_t limit[NR][2], least, most;                  // least, most: limits of the first and the last row that exist
   float o[NR][MT][4];                                 // O^T: block j of 16 columns: columns g MT*2 + 2j (| + 1) x rows 2t (| + 1)
   float ref[NR][2], l[NR][2];                         // weights are 2^(a - ref); their sum over the value scale
 
@@ -660,12 +680,11 @@ struct AttnConsumer {
   __device__ __forceinline__ void step(const uint8_t* ktile, const uint8_t* vtile, int at, int key, const float4 (&about)[2], int lane) {
     const int g = lane >> 2, t = lane & 3;
     float s[2][NR][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) scores<D, KIND, NR>(q, ktile, at + 16 * h, lane, s[h]);
+    scores<D, KIND, 2, NR>(frag, ktile, at, lane, s);
     // a = score in log2 units plus log2 of the value scale, so that 2^(a - ref) are the weights of the value codes, and the sum
     // of the probabilities is that of the weights over the value scale.  ref follows the largest a from 8 below it and is left
     // alone until a weight would pass 2^15: a half holds weights down to 2^-24, 2^-32 of the largest and less.
-    const bool edge = key + 32 > q.least || about[0].x == 0.f || about[1].x == 0.f;
+    const bool edge = key + 32 > least || about[0].x == 0.f || about[1].x == 0.f;
     float top[NR][2];
     bool high = false;
 #pragma unroll
@@ -674,13 +693,13 @@ struct AttnConsumer {
       for (int r = 0; r < 2; ++r) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float f = q.factor[i][r] * about[h].x;
+          const float f = factor[i][r] * about[h].x;
           float &x = s[h][i][r], &y = s[h][i][r + 2];
           x = fmaf(x, f, about[h].y);
           y = fmaf(y, f, about[h].y);
           if (edge) {
-            if (about[h].x == 0.f || key + 16 * h + g >= q.limit[i][r]) x = -INFINITY;
-            if (about[h].x == 0.f || key + 16 * h + g + 8 >= q.limit[i][r]) y = -INFINITY;
+            if (about[h].x == 0.f || key + 16 * h + g >= limit[i][r]) x = -INFINITY;
+            if (about[h].x == 0.f || key + 16 * h + g + 8 >= limit[i][r]) y = -INFINITY;
           }
         }
         top[i][r] = fmaxf(fmaxf(s[0][i][r], s[0][i][r + 2]), fmaxf(s[1][i][r], s[1][i][r + 2]));
@@ -733,51 +752,48 @@ struct AttnConsumer {
           v[i][1] = x.y;
         }
       }
-      bool careful = false;
       if (edge) {
-        // what lies behind the last key that any row sees is whatever the page held: it must not meet a zero weight
-        bool nan = false;
+        // What lies behind the last key that any row sees is whatever the page held, and a NaN of a new token must reach the
+        // rows that see it and no other: neither may meet a zero weight.
+        bool any = false;
+        uint32_t nan[4][D / 32];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const bool past = about[h].x == 0.f || key + 16 * h + 2 * t + (i & 1) + 8 * (i >> 1) >= q.most;
+          const bool past = about[h].x == 0.f || key + 16 * h + 2 * t + (i & 1) + 8 * (i >> 1) >= most;
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
             if (past) v[i][c] = 0;
-            if (KIND == FCP_CACHE_E4M3) nan |= __vcmpeq4(v[i][c] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
-          }
-        }
-        careful = KIND == FCP_CACHE_E4M3 && __any_sync(0xffffffffu, nan);
-      }
-      if (KIND == FCP_CACHE_E4M3 && careful) {
-        // a NaN that only some of the rows see: key by key, and only into the rows that see it
-#pragma unroll 1
-        for (int k = 0; k < 16; ++k) {
-          const bool mine = t == ((k & 7) >> 1), odd = k & 1, high8 = k >> 3;
-          const uint32_t keep = mine ? (odd ? 0xffff0000u : 0x0000ffffu) : 0u;
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = mine && (i & 1) == odd && (i >> 1) == high8 ? v[i][c] : 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t b0 = __byte_perm(x[0], x[1], e ? 0x7362 : 0x5140), b1 = __byte_perm(x[2], x[3], e ? 0x7362 : 0x5140);
-#pragma unroll
-              for (int i = 0; i < NR; ++i) {
-                float d[4] = {0.f, 0.f, 0.f, 0.f};
-                mma_f16(d, halves_lo<KIND>(b0), halves_hi<KIND>(b0), halves_lo<KIND>(b1), halves_hi<KIND>(b1), high8 ? 0 : p[h][i][0] & keep,
-                        high8 ? p[h][i][1] & keep : 0);
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-                  if (key + 16 * h + k < q.limit[i][r]) {
-                    o[i][2 * c + e][r] += d[r];
-                    o[i][2 * c + e][r + 2] += d[r + 2];
-                  }
-              }
+            if (KIND == FCP_CACHE_E4M3) {
+              nan[i][c] = __vcmpeq4(v[i][c] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+              any |= nan[i][c] != 0;
+              v[i][c] &= ~nan[i][c];
             }
           }
         }
-        continue;
+        if (KIND == FCP_CACHE_E4M3 && __any_sync(0xffffffffu, any)) {
+          // ones where a value is NaN times ones where a row sees the key: NaN where the product is not 0
+#pragma unroll
+          for (int i = 0; i < NR; ++i) {
+            uint32_t sees[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int pos = key + 16 * h + g + 8 * k;
+              sees[k] = transpose8(pack_half(pos < limit[i][0] ? 1.f : 0.f, pos < limit[i][1] ? 1.f : 0.f));
+            }
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t b0 = __byte_perm(nan[0][c], nan[1][c], e ? 0x7362 : 0x5140) & 0x38383838u;
+                const uint32_t b1 = __byte_perm(nan[2][c], nan[3][c], e ? 0x7362 : 0x5140) & 0x38383838u;
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(d, halves_lo<KIND>(b0), halves_hi<KIND>(b0), halves_lo<KIND>(b1), halves_hi<KIND>(b1), sees[0], sees[1]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  if (d[r] != 0.f) o[i][2 * c + e][r] = __int_as_float(0x7fffffff);
+              }
+          }
+        }
       }
 #pragma unroll
       for (int c = 0; c < D / 32; ++c)
@@ -801,7 +817,7 @@ struct AttnConsumer {
   // The end of a group's tiles on this CTA: joins the warps and writes the rows, or their partial result.
   __device__ __forceinline__ void finish(const AttnArgs& A, const StageMeta& meta, float4* join, float2* stats, int warp, int lane) {
     const int g = lane >> 2, t = lane & 3, tid = warp * 32 + lane;
-    asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory");       // the join area's last readers are done
+    consumer_sync();                                  // the join area's last readers are done
     float4* mine = join + warp * 8 * NR * (D / 4);
     const int n_rows = min(RT, meta.n * A.group - meta.row_tile * RT);
 #pragma unroll
@@ -818,7 +834,7 @@ struct AttnConsumer {
         for (int c = 0; c < D / 32; ++c)
           mine[join_slot(row, g * (D / 32) + c)] = make_float4(o[i][2 * c][r], o[i][2 * c][r + 2], o[i][2 * c + 1][r], o[i][2 * c + 1][r + 2]);
       }
-    asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory");
+    consumer_sync();
     for (int e = tid; e < n_rows * (D / 4); e += CT_WARPS * 32) {
       const int r = e / (D / 4), f = e % (D / 4), wr = r / (8 * NR), row = r % (8 * NR);
       float top = -3e38f;
@@ -849,20 +865,32 @@ struct AttnConsumer {
     }
   }
 
-  __device__ __forceinline__ void run(const AttnArgs& A, const uint8_t* ring, const uint8_t* queries, const StageMeta* metas, float4* join, float2* stats,
+  __device__ __forceinline__ void run(const AttnArgs& A, const uint8_t* ring, const uint8_t* queries, const QueryArea<D>& area, const StageMeta* metas, float4* join, float2* stats,
                                       uint32_t full, uint32_t empty, const WaitCtx& ctx) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, kg = warp / WR;
     const int turn = WR == 1 ? kg >> 2 : 0, first = (WR == 1 ? kg & 3 : kg) * STEPS;       // which tiles, which 32 keys of them
     int stage = 0, tile = 0;
     uint32_t phase = 0;
+    frag = area.frag + wr * NR * (D / 16) * 32;
     while (mbar_wait_warp(full + stage * 8, phase, ctx, 921)) {
       const StageMeta& meta = metas[stage];
       const int flags = meta.flags;
       if (flags & ST_END) break;
       if (flags & ST_FIRST) {
-        q.fill(A, meta, meta.row_tile * RT + wr * 8 * NR, lane, S::QUERY_BYTES ? queries + stage * S::QUERY_BYTES : nullptr);
+        area.template fill<false>(A, meta, meta.row_tile * RT, S::BLOCKS, S::QUERY_BYTES ? queries + stage * S::QUERY_BYTES : nullptr, warp, lane);
+        consumer_sync();
+        const int first_row = meta.row_tile * RT + wr * 8 * NR, n_rows = meta.n * A.group;
+        const int last_row = min(first_row + 8 * NR, n_rows) - 1;
+        least = meta.length - meta.n + first_row / A.group + 1;
+        most = first_row < n_rows ? meta.length - meta.n + last_row / A.group + 1 : 0;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const RowInfo x = area.row[(wr * NR + i) * 8 + 2 * (lane & 3) + r];
+            factor[i][r] = x.factor;
+            limit[i][r] = x.limit;
+          }
           ref[i][0] = ref[i][1] = -3e38f;
           l[i][0] = l[i][1] = 0.f;
 #pragma unroll
@@ -870,12 +898,12 @@ struct AttnConsumer {
         }
       }
       if (WR > 1 || (tile & 1) == turn) {
-        const uint8_t* ktile = ring + stage * 2 * S::TILE;
+        const uint8_t* ktile = ring + stage * S::STAGE;
 #pragma unroll 1
         for (int i = first; i < first + STEPS; ++i) {
           const int key = meta.key0 + i * CT_STEP;
           const float4 about[2] = {meta.sub[2 * i], meta.sub[2 * i + 1]};
-          if (key < q.most && (about[0].x != 0.f || about[1].x != 0.f)) step(ktile, ktile + S::TILE, i * CT_STEP, key, about, lane);
+          if (key < most && (about[0].x != 0.f || about[1].x != 0.f)) step(ktile, ktile + S::TILE, i * CT_STEP, key, about, lane);
         }
       }
       if (flags & ST_LAST) finish(A, meta, join, stats, warp, lane);
@@ -891,52 +919,66 @@ struct AttnConsumer {
 };
 
 // Weights of the cached keys: the scores once more, against the finished log-sum-exps.  A warp holds 16 keys and goes over the
-// rows in blocks of 8 (32 rows stay in registers), so that a key's sum is taken by four threads in a fixed order.
+// rows in blocks of 8, NR blocks in shared memory at a time, so that a key's sum is taken by four threads in a fixed order.
 template <int D, int KIND, int NR>
-__device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t* ring, const StageMeta* metas, uint32_t full,
-                                                uint32_t empty, const WaitCtx& ctx) {
+__device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t* ring, const QueryArea<D>& area, const StageMeta* metas,
+                                                uint32_t full, uint32_t empty, const WaitCtx& ctx) {
   using S = AttnSmem<D, NR, 0>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int stage = 0;
   uint32_t phase = 0;
-  QueryRows<D, NR> q;
-  float lse2[NR][2];
   while (mbar_wait_warp(full + stage * 8, phase, ctx, 931)) {
     const StageMeta& meta = metas[stage];
     if (meta.flags & ST_END) break;
     const int key = meta.key0 + warp * 16, n_rows = meta.n * A.group;
     const float4 about = meta.sub[warp];
-    auto rows_from = [&](int r0) {
-      q.fill(A, meta, r0, lane, nullptr);
-#pragma unroll
-      for (int i = 0; i < NR; ++i)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int r = r0 + 8 * i + 2 * t + c, j = r / A.group;
-          lse2[i][c] = r < n_rows ? ld_f32(A.lse + (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + r - j * A.group) * 1.4426950408889634f : INFINITY;
-        }
-    };
-    if (n_rows <= 8 * NR && (meta.flags & ST_FIRST)) rows_from(0);
-    if (key < meta.length && about.x != 0.f) {
-      float sum[2] = {0.f, 0.f};                      // of keys g and g + 8
+    float sum[2] = {0.f, 0.f};                        // of keys g and g + 8
 #pragma unroll 1
-      for (int r = 0; r < n_rows; r += 8 * NR) {
-        if (n_rows > 8 * NR) rows_from(r);
-        float s[NR][4];
-        scores<D, KIND, NR>(q, ring + stage * 2 * S::TILE, warp * 16, lane, s);
-#pragma unroll
-        for (int i = 0; i < NR; ++i)
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (key + g + 8 * (c >> 1) < q.limit[i][c & 1])
-              sum[c >> 1] += exp2_approx(fmaf(s[i][c], q.factor[i][c & 1] * about.x, -lse2[i][c & 1]));
+    for (int r0 = 0; r0 < n_rows; r0 += 8 * NR) {
+      const int blocks = min(NR, (n_rows - r0 + 7) / 8);
+      if (n_rows > 8 * NR || (meta.flags & ST_FIRST)) {
+        consumer_sync();                              // the rows before have been read
+        area.template fill<true>(A, meta, r0, blocks, nullptr, warp, lane);
+        consumer_sync();
       }
+      if (key >= meta.length || about.x == 0.f) continue;
+      uint32_t a[D / 16][4];                          // the keys as operands
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        uint32_t lo[4], hi[4];
+        words(tile_at<D>(ring + stage * S::STAGE, warp * 16 + g, t * (D / 64) + c), lo);
+        words(tile_at<D>(ring + stage * S::STAGE, warp * 16 + g + 8, t * (D / 64) + c), hi);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          a[4 * c + k][0] = halves_lo<KIND>(lo[k]);
+          a[4 * c + k][1] = halves_lo<KIND>(hi[k]);
+          a[4 * c + k][2] = halves_hi<KIND>(lo[k]);
+          a[4 * c + k][3] = halves_hi<KIND>(hi[k]);
+        }
+      }
+#pragma unroll 2
+      for (int i = 0; i < blocks; ++i) {
+        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};          // two chains
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint2 x = area.frag[(i * (D / 16) + k) * 32 + lane];
+          mma_f16(s[k & 1], a[k][0], a[k][1], a[k][2], a[k][3], x.x, x.y);
+        }
+        const RowInfo rows[2] = {area.row[8 * i + 2 * t], area.row[8 * i + 2 * t + 1]};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (key + g + 8 * (c >> 1) < rows[c & 1].limit)
+            sum[c >> 1] += exp2_approx(fmaf(s[0][c] + s[1][c], rows[c & 1].factor * about.x, -rows[c & 1].lse2));
+      }
+    }
+    if (key < meta.length && about.x != 0.f) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 1);
         sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], 2);
       }
-      if (t < 2 && key + g + 8 * t < meta.length) A.c.weight[(int64_t)__float_as_int(about.w) + g + 8 * t] += sum[t];
+      // one addition per place and call, so the result does not depend on any order; as an atomic it is not waited for
+      if (t < 2 && key + g + 8 * t < meta.length) atomicAdd(A.c.weight + (int64_t)__float_as_int(about.w) + g + 8 * t, t ? sum[1] : sum[0]);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(empty + stage * 8);
@@ -956,6 +998,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   __shared__ __align__(8) uint64_t bars[2 * S::STAGES];
   __shared__ __align__(16) StageMeta metas[S::STAGES];
   __shared__ float2 stats[WR ? CT_WARPS * 8 * NR : 1];
+  __shared__ __align__(16) RowInfo rows[S::ROWS];
   __shared__ int64_t scratch[16];
   __shared__ int abort_flag;
   const int warp = threadIdx.x >> 5;
@@ -964,6 +1007,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   const uint32_t skip = (1024u - (smem_u32(smem) & 1023u)) & 1023u;
   uint8_t* ring = smem + skip;
   uint8_t* queries = ring + S::RING;
+  const QueryArea<D> area = {reinterpret_cast<uint2*>(queries + S::STAGES * S::QUERY_BYTES), rows};
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < S::STAGES; ++i) {
@@ -983,10 +1027,10 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
     AttnProducer<D, NR, WR> producer(A, order, range);
     if (warp == CT_WARPS || WR > 0) producer.run(warp == CT_WARPS ? &tk : &tv, warp - CT_WARPS, smem_u32(ring), smem_u32(queries), metas, full, empty, ctx);
   } else if constexpr (WR == 0) {
-    weight_consumer<D, KIND, NR>(A, ring, metas, full, empty, ctx);
+    weight_consumer<D, KIND, NR>(A, ring, area, metas, full, empty, ctx);
   } else {
     AttnConsumer<D, KIND, NR, WR> consumer;
-    consumer.run(A, ring, queries, metas, reinterpret_cast<float4*>(queries + S::STAGES * S::QUERY_BYTES), stats, full, empty, ctx);
+    consumer.run(A, ring, queries, area, metas, reinterpret_cast<float4*>(queries + S::STAGES * S::QUERY_BYTES + S::FRAGS), stats, full, empty, ctx);
   }
   __syncthreads();
   wait_teardown(ctx);
