@@ -57,6 +57,7 @@ BatchView view(const fcp_cache_config& c, const fcp_cache_batch& b) {
   v.page_table = b.page_table;
   v.length = b.length;
   v.row_offset = b.row_offset;
+  v.only = nullptr;
   return v;
 }
 
@@ -176,17 +177,45 @@ int ready(const char* call, const fcp_cache* cache) {
   return FCP_OK;
 }
 
-// Workspace of fcp_cache_attn: partial outputs and log-sum-exps of two groups per CTA, and what each CTA shares.
+// Whether a call goes through bf16 copies and tcgen05: chunks of a tile of new tokens and more, while the copies stay below
+// half of the device's memory or so.  TODO
+constexpr int kChunkTokens = 128;
+constexpr int64_t kChunkBytes = int64_t(64) << 30;
+int64_t chunk_stride(const fcp_cache_config& c, const fcp_cache_batch& b) {
+  return ((int64_t)b.table_width * c.page_tokens + CT_KEYS - 1) / CT_KEYS * CT_KEYS;
+}
+bool in_chunks(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq) {
+  const int64_t tokens = b.B * chunk_stride(c, b), units = (int64_t)b.B * ((b.max_new + FCP_FWD_UNIT_ROWS - 1) / FCP_FWD_UNIT_ROWS);
+  return b.max_new >= kChunkTokens && b.B <= 65535 && tokens < (int64_t(1) << 31) - CT_KEYS && tokens * c.hkv * c.head_dim * 4 <= kChunkBytes &&
+         2 * units * hq < int64_t(1) << 31;
+}
+
+// Workspace of fcp_cache_attn: partial outputs and log-sum-exps of two groups per CTA, and what each CTA shares; for chunks also
+// the copies and the tables of the units.
 struct AttnSpace {
-  int64_t o, lse, split, bytes;
+  int64_t o, lse, split, k, v, careful, units, groups, row_limit, bytes;
+  int32_t units_per_seq;
 };
-AttnSpace attn_space(RowTile t, int D) {
+AttnSpace attn_space(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq, RowTile t) {
+  AttnSpace s = {};
+  auto take = [&s](int64_t bytes) {
+    const int64_t at = s.bytes;
+    s.bytes += (bytes + 255) / 256 * 256;
+    return at;
+  };
   const int64_t parts = 2 * (int64_t)FCP_PLAN_SMS * t.rows();
-  AttnSpace s;
-  s.o = 0;
-  s.lse = parts * D * 4;
-  s.split = s.lse + (parts * 4 + 255) / 256 * 256;
-  s.bytes = s.split + (FCP_PLAN_SMS * SP_W * 4 + 255) / 256 * 256;
+  s.o = take(parts * c.head_dim * 4);
+  s.lse = take(parts * 4);
+  s.split = take(FCP_PLAN_SMS * SP_W * 4);
+  if (!in_chunks(c, b, hq)) return s;
+  const int64_t copy = b.B * chunk_stride(c, b) * c.hkv * c.head_dim * 2;
+  s.units_per_seq = (b.max_new + FCP_FWD_UNIT_ROWS - 1) / FCP_FWD_UNIT_ROWS;
+  s.k = take(copy);
+  s.v = take(copy);
+  s.careful = take((int64_t)b.B * 4);
+  s.units = take((int64_t)b.B * s.units_per_seq * FCP_FWD_UNIT_W * 4);
+  s.groups = take(FCP_WORK_GROUP_W * 4 + 4);
+  s.row_limit = take((int64_t)b.rows * 4);
   return s;
 }
 
@@ -304,9 +333,46 @@ extern "C" int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_
   int rc = check_batch(call, cache, batch, true);
   if (rc == FCP_OK) rc = check_heads(call, cache->config, hq);
   if (rc != FCP_OK) return rc;
-  *bytes = attn_space(row_tile((int64_t)batch->max_new * (hq / cache->config.hkv)), cache->config.head_dim).bytes;
+  *bytes = attn_space(cache->config, *batch, hq, row_tile((int64_t)batch->max_new * (hq / cache->config.hkv))).bytes;
   return FCP_OK;
 }
+
+namespace {
+int attn_in_chunks(const fcp_cache* cache, const fcp_cache_batch& batch, const AttnArgs& a, const AttnSpace& space, char* ws, cudaStream_t st) {
+  const fcp_cache_config& c = cache->config;
+  ChunkArgs x;
+  x.c = a.c;
+  x.s = a.s;
+  x.k = (__nv_bfloat16*)(ws + space.k);
+  x.v = (__nv_bfloat16*)(ws + space.v);
+  x.stride = (int32_t)chunk_stride(c, batch);
+  x.careful = (int32_t*)(ws + space.careful);
+  x.units = (int32_t*)(ws + space.units);
+  x.groups = (int32_t*)(ws + space.groups);
+  x.counter = x.groups + FCP_WORK_GROUP_W;
+  x.row_limit = (int32_t*)(ws + space.row_limit);
+  x.units_per_seq = space.units_per_seq;
+  FCP_CUDA_CHECK(cudaMemsetAsync(x.careful, 0, (size_t)batch.B * 4, st));
+  const dim3 grid((unsigned)(x.stride / CT_KEYS), (unsigned)c.hkv, (unsigned)batch.B);
+  void (*unpack)(const ChunkArgs) = c.head_dim == 128 ? (c.kind == FCP_CACHE_E4M3 ? cache_unpack_kernel<128, FCP_CACHE_E4M3> : cache_unpack_kernel<128, FCP_CACHE_INT8>)
+                                                      : (c.kind == FCP_CACHE_E4M3 ? cache_unpack_kernel<64, FCP_CACHE_E4M3> : cache_unpack_kernel<64, FCP_CACHE_INT8>);
+  FCP_CUDA_CHECK(launch(unpack, grid, UNPACK_THREADS, 0, st, x));
+  FCP_CUDA_CHECK(launch(cache_chunk_kernel, dim3((unsigned)space.units_per_seq, (unsigned)batch.B), CHUNK_THREADS, 0, st, x));
+  FwdTables t;
+  t.units = x.units;
+  t.groups = x.groups;
+  t.row_limit = x.row_limit;
+  t.counter = x.counter;
+  t.status = c.status;
+  t.n_units = batch.B * space.units_per_seq;
+  fcp_params p;
+  p.hq = a.hq;
+  p.hkv = c.hkv;
+  p.head_dim = c.head_dim;
+  p.scale = a.scale_log2 * 0.69314718055994531f;
+  return launch_fwd_tables(t, p, a.q, a.q_stride, batch.rows, x.k, x.v, (int64_t)batch.B * x.stride, a.o, a.lse, st);
+}
+}  // namespace
 
 extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const void* q, int64_t q_stride, int32_t hq,
                               float scale, void* o, float* lse, int32_t accumulate, void* workspace, int64_t workspace_bytes,
@@ -336,7 +402,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
     return FCP_ERR_INVALID_ARG;
   }
   const RowTile tile = row_tile((int64_t)batch->max_new * group);
-  const AttnSpace space = attn_space(tile, c.head_dim);
+  const AttnSpace space = attn_space(c, *batch, hq, tile);
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < space.bytes) {
     fcp_set_error("%s: workspace of %lld bytes (aligned to 256) needed, %lld given", call, (long long)space.bytes, (long long)workspace_bytes);
     return FCP_ERR_WORKSPACE;
@@ -358,9 +424,15 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
   a.split = (int32_t*)((char*)workspace + space.split);
   cudaStream_t st = (cudaStream_t)stream;
   const int grid = cache->sm_count;
+  const BatchView all = a.s;
+  if (space.units_per_seq > 0) {
+    if ((rc = attn_in_chunks(cache, *batch, a, space, (char*)workspace, st)) != FCP_OK) return rc;
+    a.s.only = (const int32_t*)((char*)workspace + space.careful);       // what is left
+  }
   FCP_CUDA_CHECK(launch(attn_kernel(c, tile), grid, CT_THREADS, attn_smem(c, tile), st, cache->k_map, cache->v_map, a));
   if (c.head_dim == 128) FCP_CUDA_CHECK(launch(cache_merge_kernel<128>, grid, MERGE_THREADS, 0, st, a, tile.rows()));
   else FCP_CUDA_CHECK(launch(cache_merge_kernel<64>, grid, MERGE_THREADS, 0, st, a, tile.rows()));
+  a.s = all;
   if (accumulate)
     FCP_CUDA_CHECK(launch(attn_kernel(c, kWeights), grid, CT_THREADS, attn_smem(c, kWeights), st, cache->k_map, cache->v_map, a));
   return FCP_OK;

@@ -21,6 +21,7 @@ struct CacheView {
 struct BatchView {
   int32_t B, rows, max_new, table_width, capacity;     // capacity: tokens that a row of the page table can name
   const int32_t *page_table, *length, *row_offset;
+  const int32_t* only;                                 // NULL, or one word per sequence: the others count as without new tokens
 };
 
 __device__ __forceinline__ int32_t ld_i32(const int32_t* p) {
@@ -35,7 +36,9 @@ __device__ __forceinline__ void mark_bad(int32_t* status, int32_t code, int32_t 
   }
 }
 __device__ __forceinline__ SeqView load_seq(const BatchView& s, int b) {
-  return seq_view(ld_i32(s.row_offset + b), ld_i32(s.row_offset + b + 1), ld_i32(s.length + b), s.rows, s.max_new, s.capacity);
+  SeqView v = seq_view(ld_i32(s.row_offset + b), ld_i32(s.row_offset + b + 1), ld_i32(s.length + b), s.rows, s.max_new, s.capacity);
+  if (s.only && ld_i32(s.only + b) == 0) v.n = 0;
+  return v;
 }
 __device__ __forceinline__ bool usable_scale(float x) { return x >= FCP_CACHE_MIN_SCALE && x <= FCP_CACHE_MAX_SCALE; }
 
@@ -1066,6 +1069,138 @@ __global__ void __launch_bounds__(MERGE_THREADS) cache_merge_kernel(const __grid
     const int64_t out = (int64_t)(row0 + j) * A.hq + head * A.group + gr - j * A.group;
     *reinterpret_cast<uint2*>(A.o + out * D + f * 4) = make_uint2(pack_bf16(x.x * inverse, x.y * inverse), pack_bf16(x.z * inverse, x.w * inverse));
     if (f == 0) A.lse[out] = z == 0.f ? -INFINITY : (ref + __log2f(z)) * 0.69314718055994531f;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention of long chunks of new tokens
+// ---------------------------------------------------------------------------------------------
+// With many new tokens the products decide, and those of whole tiles of 128 tokens belong to tcgen05: the cached keys and values
+// are written out as bf16 once (exactly, where the scale is a power of two), [sequence][capacity][hkv][D], and the packed
+// attention of this library (fcp_fwd_kernel) runs over them, with work units and row limits made on the device.
+//
+// Sequences that this cannot serve exactly are marked and left to cache_attn_kernel: tokens on pages that do not exist, more new rows
+// than tokens, a NaN value among the new tokens (it would meet zero weights of rows that do not see it).
+struct ChunkArgs {
+  CacheView c;
+  BatchView s;
+  __nv_bfloat16 *k, *v;                               // [B * stride][hkv][D]
+  int32_t stride;                                     // rows per sequence: the capacity in whole tiles
+  int32_t* careful;                                   // [B], zero before
+  int32_t *units, *groups, *row_limit, *counter;      // [B * units_per_seq][FCP_FWD_UNIT_W], [4], [rows], the grid's work counter
+  int32_t units_per_seq;
+};
+
+constexpr int UNPACK_THREADS = 256;
+// 16 codes -> 16 bf16
+template <int KIND>
+__device__ __forceinline__ void unpack16(const uint4& x, float scale, uint4 (&out)[2]) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t y[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = halves_lo<KIND>(w[i]), hi = halves_hi<KIND>(w[i]);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    y[2 * i] = pack_bf16(a.x * scale, a.y * scale);
+    y[2 * i + 1] = pack_bf16(b.x * scale, b.y * scale);
+  }
+  out[0] = make_uint4(y[0], y[1], y[2], y[3]);
+  out[1] = make_uint4(y[4], y[5], y[6], y[7]);
+}
+// One block per (128 tokens, KV head, sequence).  The rest of a sequence's last tile is zeroed: its probabilities are zero, and a
+// product with them must not meet what the memory held.
+template <int D, int KIND>
+__global__ void __launch_bounds__(UNPACK_THREADS) cache_unpack_kernel(const __grid_constant__ ChunkArgs a) {
+  __shared__ int32_t rows[CT_KEYS];
+  __shared__ float scales[2][CT_KEYS];
+  grid_begin();
+  const int b = blockIdx.z, h = blockIdx.y, t0 = blockIdx.x * CT_KEYS, tid = threadIdx.x;
+  const SeqView s = load_seq(a.s, b);
+  if (s.n == 0 || t0 >= s.length) {
+    if (tid == 0 && s.n > s.length) a.careful[b] = 1;
+    return;
+  }
+  bool careful = s.n > s.length;
+  if (tid < CT_KEYS) {
+    const int pos = t0 + tid;
+    int32_t row = -2;
+    float ks = 0.f, vs = 0.f;
+    if (pos < s.length) {
+      const int32_t page = ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + (pos >> a.c.page_shift));
+      row = page_row(page, a.c.n_pages, a.c.hkv, h, a.c.page_tokens);
+      if (row >= 0) {
+        ks = ld_f32(a.c.k_scale + page * a.c.hkv + h);
+        vs = ld_f32(a.c.v_scale + page * a.c.hkv + h);
+        row += pos & (a.c.page_tokens - 1);
+      }
+      if (row < 0 || !usable_scale(ks) || !usable_scale(vs)) {
+        row = -2;
+        careful = true;
+      }
+    }
+    rows[tid] = row;
+    scales[0][tid] = ks;
+    scales[1][tid] = vs;
+  }
+  __syncthreads();
+  constexpr int C = D / 16, N = 2 * CT_KEYS * C / UNPACK_THREADS;
+  uint4 x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = i * UNPACK_THREADS + tid, which = e / (CT_KEYS * C), t = e / C % CT_KEYS, c = e % C;
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (rows[t] >= 0) x[i] = ld_v4((which ? a.c.v : a.c.k) + (int64_t)rows[t] * D + c * 16);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = i * UNPACK_THREADS + tid, which = e / (CT_KEYS * C), t = e / C % CT_KEYS, c = e % C;
+    if (KIND == FCP_CACHE_E4M3 && which && t0 + t >= s.length - s.n) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) careful |= __vcmpeq4(w[j] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+    }
+    uint4 y[2];
+    unpack16<KIND>(x[i], scales[which][t], y);
+    __nv_bfloat16* out = (which ? a.v : a.k) + (((int64_t)b * a.stride + t0 + t) * a.c.hkv + h) * D + c * 16;
+    *reinterpret_cast<uint4*>(out) = y[0];
+    *reinterpret_cast<uint4*>(out + 8) = y[1];
+  }
+  if (careful) a.careful[b] = 1;
+}
+
+// The work units of fcp_fwd_kernel (pairs of tiles of 128 new tokens), the one work group, the row limits.
+constexpr int CHUNK_THREADS = 256;
+__global__ void __launch_bounds__(CHUNK_THREADS) cache_chunk_kernel(const __grid_constant__ ChunkArgs a) {
+  grid_begin();
+  const int b = blockIdx.y, u = blockIdx.x, tid = threadIdx.x;
+  const SeqView s = load_seq(a.s, b);
+  const bool serves = ld_i32(a.careful + b) == 0;
+  const int first = u * FCP_FWD_UNIT_ROWS, n = serves ? max(0, min(FCP_FWD_UNIT_ROWS, s.n - first)) : 0;
+  const int seen = s.length - s.n + first + 1;        // keys that the unit's first row sees
+  if (tid < n) a.row_limit[s.row0 + first + tid] = b * a.stride + seen + tid;
+  if (tid < FCP_FWD_UNIT_W) {
+    auto tiles = [&](int rows) { return (seen + rows - 1 + FCP_TILE - 1) / FCP_TILE; };        // of keys, for the first `rows` rows
+    int x = 0;
+    switch (tid) {
+      case FU_Q_ROW0: x = s.row0 + first; break;
+      case FU_Q_ROWS: x = n; break;
+      case FU_N_RANGES: x = 1; break;
+      case FU_KV0_BEGIN: x = b * a.stride; break;
+      case FU_KV0_END: x = b * a.stride + seen + n - 1; break;
+      case FU_KV0_DIAG: x = 1; break;
+      case FU_NT_STAGE0: x = n > 0 ? tiles(min(n, FCP_TILE)) : 0; break;
+      case FU_NT_STAGE1: x = n > FCP_TILE ? tiles(n) : 0; break;
+      case FU_NT_RANGE0: x = 0x7fffffff; break;       // no second range
+      case FU_SINGLE_SLOT: x = 1; break;
+    }
+    a.units[((int64_t)b * a.units_per_seq + u) * FCP_FWD_UNIT_W + tid] = x;
+  }
+  if (b == 0 && u == 0 && tid == 0) {
+    *a.counter = 0;
+    a.groups[WG_FIRST] = 0;
+    a.groups[WG_N_UNITS] = (int32_t)(gridDim.x * gridDim.y);
+    a.groups[WG_HEADS] = a.c.hkv;
+    a.groups[WG_RSV] = 0;
   }
 }
 

@@ -21,7 +21,8 @@ using namespace fcp;
 namespace {
 
 // bf16 tensor [T][H][D]; box = 64 columns x 1 head x `box_rows` tokens, 128-byte swizzle, zero fill.
-int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int D, int box_rows) {
+// `stride`: elements from one token to the next.
+int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int D, int box_rows, int64_t stride) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) {
     fcp_set_error("cuTensorMapEncodeTiled is not available from the driver");
@@ -32,7 +33,7 @@ int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int D, int 
     return FCP_ERR_INVALID_ARG;
   }
   const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)T};
-  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)H * D * 2};
+  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
   const cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
   const cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
@@ -43,6 +44,10 @@ int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int D, int 
     return FCP_ERR_CUDA;
   }
   return FCP_OK;
+}
+
+int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int D, int box_rows) {
+  return make_thd_map(m, base, T, H, D, box_rows, (int64_t)H * D);
 }
 
 // Records an event pair around a kernel launch when the plan is in profiling mode.
@@ -680,6 +685,46 @@ int launch_fwd(const fcp_plan* plan, const void* q, const void* k, const void* v
   return FCP_OK;
 }
 
+}  // namespace
+
+int fcp::launch_fwd_tables(const FwdTables& t, const fcp_params& P, const void* q, int64_t q_stride, int64_t rows, const void* k,
+                           const void* v, int64_t kv_rows, void* o, float* lse, cudaStream_t st) {
+  PlanPool* pool = nullptr;
+  int rc = current_pool(&pool);
+  if (rc != FCP_OK) return rc;
+  {
+    std::lock_guard<std::mutex> lock(pool->mu);
+    if ((rc = pool_setup(*pool)) != FCP_OK) return rc;
+  }
+  CUtensorMap tq, tk, tv;
+  if ((rc = make_thd_map(&tq, q, rows, P.hq, P.head_dim, 128, q_stride)) != FCP_OK) return rc;
+  if ((rc = make_thd_map(&tk, k, kv_rows, P.hkv, P.head_dim, 128)) != FCP_OK) return rc;
+  if ((rc = make_thd_map(&tv, v, kv_rows, P.hkv, P.head_dim, 128)) != FCP_OK) return rc;
+  FwdArgs a = {};
+  a.units = t.units;
+  a.n_units = t.n_units;
+  a.groups = t.groups;
+  a.head_count = a.hq = P.hq;
+  a.hkv = P.hkv;
+  a.head_group = P.hq / P.hkv;
+  a.scale_log2 = P.scale * 1.4426950408889634f;
+  a.o_direct = (__nv_bfloat16*)o;
+  a.lse_direct = lse;
+  a.row_limit = t.row_limit;
+  a.status = t.status;
+  a.work_counter = t.counter;
+  // the second tile of a unit runs beside the first at little cost, unless SMs would have no unit at all
+  a.split = (int64_t)t.n_units * P.hq < pool->sm_count ? 1 : 0;
+  const int grid = (int)std::min<int64_t>((int64_t)t.n_units * P.hq << a.split, pool->sm_count);
+  // not early: the kernel reads its tables through the read-only path, which wants them complete before it begins
+  if (P.head_dim == 128)
+    FCP_CUDA_CHECK(launch_when(false, fcp_fwd_kernel<128>, grid, FWD_THREADS, FwdSmem<128>::DYN_BYTES, st, tq, tk, tv, a));
+  else
+    FCP_CUDA_CHECK(launch_when(false, fcp_fwd_kernel<64>, grid, FWD_THREADS, FwdSmem<64>::DYN_BYTES, st, tq, tk, tv, a));
+  return FCP_OK;
+}
+
+namespace {
 int launch_merge(const fcp_plan* plan, const float* o_partial, const float* lse_partial, int32_t head_begin,
                  int32_t head_count, void* o, float* o_f32, float* lse, int n_units, void* stream) {
   const fcp_params& P = plan->params;

@@ -72,4 +72,14 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cu
   return launch_when(true, kernel, grid, threads, smem, st, args...);
 }
 
+// The fused forward kernel over work units, one work group and row limits that a kernel before it on the stream has written
+// (fcp_kernels.cu).  q [rows][hq][D] with q_stride elements between rows; k, v [kv_rows][hkv][D].
+struct FwdTables {
+  const int32_t *units, *groups, *row_limit;
+  int32_t *counter, *status;                          // counter: zero
+  int32_t n_units;
+};
+int launch_fwd_tables(const FwdTables& t, const fcp_params& p, const void* q, int64_t q_stride, int64_t rows, const void* k, const void* v,
+                      int64_t kv_rows, void* o, float* lse, cudaStream_t st);
+
 }  // namespace fcp

@@ -276,9 +276,9 @@ def test_append_scales_that_are_no_powers_of_two():
         assert np.abs(now[n] - state[n]).max() <= 1 and (now[n] != state[n]).mean() < 1e-3
 
 
-def check_attn(w, state, r, o, lse, rows):
-    """Against the definition: the rounding of the weights to halves (2^-11), of o to bf16 (2^-8), and the fp32 sums of the scores
-    (D products of size at most `size` in all, each sum truncated at 2^-23)."""
+def check_attn(w, state, r, o, lse, rows, weight=HALF):
+    """Against the definition: the rounding of the weights (to halves 2^-11; in chunks of 128 new tokens and more to bf16, 2^-8), of o
+    to bf16 (2^-8), and the fp32 sums of the scores (D products of size at most `size` in all, each sum truncated at 2^-23)."""
     off = w.off
     for name, x in (("o", o), ("lse", lse)):
         assert x.shape[0] >= rows
@@ -288,8 +288,8 @@ def check_attn(w, state, r, o, lse, rows):
     assert np.array_equal(dead, got_lse == -np.inf)
     assert np.all(got[dead] == 0)
     live = ~dead
-    assert np.all(np.abs(got_lse - r["lse"])[live] <= (score + 4 * F32 * np.abs(np.where(live, r["lse"], 0)))[live])
-    bound = BF16 * np.abs(r["o"]) + (HALF + 2 * score[..., None]) * r["spread"] * (1 + BF16) + 1e-30
+    assert np.all(np.abs(got_lse[live] - r["lse"][live]) <= (score + 4 * F32 * np.abs(np.where(live, r["lse"], 0)))[live])
+    bound = BF16 * np.abs(r["o"]) + (weight + 2 * score[..., None]) * r["spread"] * (1 + BF16) + 1e-30
     assert np.all(np.abs(got - r["o"]) <= bound), np.max(np.abs(got - r["o"]) / bound)
     assert off[-1] == rows
 
@@ -359,6 +359,90 @@ def test_long_ragged_batch_is_split_and_joined():
     w.rng = np.random.default_rng(99)
     q2, o2, lse2, _ = attend(w, new, 8)
     assert torch.equal(o1, o2) and torch.equal(lse1, lse2) and not torch.equal(o1, a)
+
+
+@pytest.mark.parametrize("kind,page,hkv,d", CASES)
+@pytest.mark.parametrize("group,new,before", [(1, [128], [0]), (2, [129, 0, 1], [70, 300, 5]), (3, [300, 40, 257], [129, 0, 700])])
+def test_attention_of_long_chunks(kind, page, hkv, d, group, new, before):
+    w = World(71, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    q, o, lse, rows = attend(w, new, hkv * group, stride_heads=1, accumulate=True)
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    check_attn(w, None, r, o, lse, rows, weight=BF16)
+    assert w.cache.device_status().tolist() == [0, 0, 0, 0]
+    assert math.isclose(float(w.w.double().sum()) - float(w.weight.astype(np.float64).sum()), rows * hkv * group, rel_tol=1e-4)
+    w.rng = np.random.default_rng(5)
+    q1, o1, lse1, _ = attend(w, new, hkv * group)
+    w.rng = np.random.default_rng(5)
+    q2, o2, lse2, _ = attend(w, new, hkv * group)
+    assert torch.equal(o1, o2) and torch.equal(lse1, lse2)
+
+
+def test_chunk_of_a_wide_table_is_captured_and_replayed():
+    """Lengths of a captured chunk change; the table is far wider than the sequences."""
+    w = World(72, "e4m3", 32, 2, 64, [500, 400], width=64).fill().up()
+    hq, rows = 4, 300
+    length, off = dev([0, 0]), dev([0, 0, 0])
+    q = torch.zeros(rows, hq, 64, dtype=torch.bfloat16, device="cuda")
+    o, lse = torch.zeros_like(q), torch.zeros(rows, hq, device="cuda")
+    batch = fcp.CacheBatch(dev(w.table), length, off, rows=rows, max_new=260)
+    n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, hq)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    step = lambda: fcp.fcp_cache_attn(w.cache, batch, q, o, lse, ws, n, stream=stream())
+    with torch.cuda.stream(torch.cuda.Stream()):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for lengths, new in [([500, 400], [130, 170]), ([260, 0], [260, 0]), ([3, 399], [3, 1])]:
+        xq = bf16(w.rng, rows, hq, 64)
+        q.copy_(xq), o.fill_(3.0)
+        w.off = np.concatenate([[0], np.cumsum(new)])
+        length.copy_(dev(lengths)), off.copy_(dev(w.off))
+        graph.replay()
+        torch.cuda.synchronize()
+        m = int(w.off[-1])
+        r = R.attention(w.state(), w.table, lengths, w.off, f64(xq)[:m])
+        check_attn(w, None, r, o[:m], lse[:m], m, weight=BF16)
+        assert bool((o[m:] == 3).all())
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_chunks_with_sequences_that_need_care(kind):
+    """In one call with ordinary sequences: a NaN among the new values, more rows than tokens, a page that does not exist, lengths
+    that make no sense."""
+    new = [140, 150, 133, 20, 200]
+    w = World(73, kind, 16, 1, 64, [300, 90, 200, 100, 260]).fill()
+    place = lambda b, p: (w.table[b][p // 16], 0, p % 16)
+    if kind == "e4m3":
+        w.codes["v"][place(0, 290)][7] = 0xff
+    good = w.state()
+    table = w.table.copy()
+    w.table[2, 1] = w.n_pages + 5
+    w.up()
+    w.length[4] = 10 ** 6
+    q, o, lse, rows = attend(w, new, 2, spare=0)
+    w.length[4] = 260
+    off = w.off
+    r = R.attention(good, table, w.length, off, f64(q)[:rows])
+    got, got_lse = f64(o), f64(lse)
+    st = w.cache.device_status().tolist()
+    assert st[0] == fcp.FCP_ERR_INVALID_ARG and st[1:3] in ([fcp.FCP_CACHE_BAD_LENGTH, 4], [fcp.FCP_CACHE_BAD_PAGE, 2])
+    assert np.all(got[off[4]:] == 3) and np.all(got_lse[off[4]:] == 5)
+    # sequence 2 without its tokens 16..31
+    k = R.gather(good, "k", np.asarray(table[2][:13], dtype=np.int64), 200, 0)
+    for j in (0, 70, 132):
+        for head in range(2):
+            seen = [p for p in range(200 - 133 + j + 1) if not 16 <= p < 32]
+            s = k[seen] @ f64(q)[off[2] + j, head] / 8
+            assert abs(got_lse[off[2] + j, head] - np.log(np.exp(s).sum())) < 1e-3
+    for b in (0, 1, 3):
+        for row in range(off[b], off[b + 1]):
+            bad = np.isnan(r["o"][row])
+            assert np.array_equal(np.isnan(got[row]), bad), (b, row)
+            ok = ~bad
+            assert np.all(np.abs(got[row] - r["o"][row])[ok] <= (2 * BF16 * np.abs(r["o"][row]) + 2 * BF16 * r["spread"][row])[ok])
+    assert np.isneginf(got_lse[off[1]:off[1] + 60]).all() and np.all(got[off[1]:off[1] + 60] == 0)
 
 
 def test_many_sequences():
