@@ -122,15 +122,15 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
   const int w = blockIdx.x, h = blockIdx.y >> 1, tid = threadIdx.x;
   const bool is_v = blockIdx.y & 1;
   const int page_tokens = a.c.page_tokens;
-  int b = 0;
-  if (a.s.max_new == 1) {                            // one token, one page: a slot per sequence
-    b = w;
-  } else {                                           // the last b whose first slot is at most w
+  int b = w;                                         // one token, one page: a slot per sequence
+  if (a.s.max_new != 1) {
+    // the last b whose first slot is at most w, by all threads: APPEND_THREADS sequences a round
     int lo = 0, hi = a.s.B - 1;
     while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (append_slot(ld_i32(a.s.row_offset + mid), mid, page_tokens) <= w) lo = mid;
-      else hi = mid - 1;
+      const int step = (hi - lo + APPEND_THREADS - 1) / APPEND_THREADS, at = lo + (tid + 1) * step;
+      const int below = __syncthreads_count(at <= hi && append_slot(ld_i32(a.s.row_offset + min(at, a.s.B - 1)), min(at, a.s.B - 1), page_tokens) <= w);
+      lo += below * step;
+      hi = min(hi, lo + step - 1);
     }
     b = lo;
   }
@@ -144,11 +144,6 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
   const AppendSpan sp = append_span(sv, slot, page_tokens);
   if (sp.lo >= sp.hi || sp.page >= a.s.table_width) return;
   const int32_t page = ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + sp.page);
-  const int32_t row = page_row(page, a.c.n_pages, a.c.hkv, h, page_tokens);
-  if (row < 0) {
-    if (tid == 0) mark_bad(a.c.status, FCP_CACHE_BAD_PAGE, b);
-    return;
-  }
   const int held = sp.lo - sp.page * page_tokens, filled = sp.hi - sp.page * page_tokens;      // slots [held, filled) are new
   constexpr int C = D / 16;
   const __nv_bfloat16* x = (is_v ? a.v : a.k) + h * D;
@@ -166,6 +161,15 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
       r[i][1] = ld_v4(p + 8);
     }
   }
+  const int32_t row = page_row(page, a.c.n_pages, a.c.hkv, h, page_tokens);
+  const int32_t cell = page * a.c.hkv + h;
+  float* scales = is_v ? a.c.v_scale : a.c.k_scale;
+  float old = 0.f;
+  if (row < 0) {
+    if (tid == 0) mark_bad(a.c.status, FCP_CACHE_BAD_PAGE, b);
+    return;
+  }
+  if (held > 0) old = ld_f32(scales + cell);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const uint32_t* u = reinterpret_cast<const uint32_t*>(r[i]);
@@ -177,15 +181,9 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < APPEND_THREADS / 32; ++i) most = max(most, warp_max[i]);
-  const int32_t cell = page * a.c.hkv + h;
-  float* scales = is_v ? a.c.v_scale : a.c.k_scale;
   uint8_t* codes = (is_v ? a.c.v : a.c.k) + (int64_t)row * D;
-  float scale = fresh_scale<KIND>(most), old = 0.f;
-  if (held > 0) {
-    old = ld_f32(scales + cell);
-    scale = fmaxf(old, scale);
-  }
-  __syncthreads();                                   // every thread has read the old scale
+  float scale = fresh_scale<KIND>(most);
+  if (held > 0) scale = fmaxf(old, scale);           // every thread has read the old scale before the barrier above
   if (tid == 0 && !(held > 0 && scale == old)) scales[cell] = scale;
   const float inverse = 1.f / scale;                 // exact for powers of two; x / scale otherwise below
   const bool exact = (__float_as_uint(scale) & 0x7fffffu) == 0;
@@ -941,7 +939,7 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
       const int blocks = min(NR, (n_rows - r0 + 7) / 8);
       if (n_rows > 8 * NR || (meta.flags & ST_FIRST)) {
         consumer_sync();                              // the rows before have been read
-        area.template fill<true>(A, meta, r0, blocks, nullptr, warp, lane);
+        area.template fill<true>(A, meta, r0, (blocks + 3) / 4 * 4, nullptr, warp, lane);
         consumer_sync();
       }
       if (key >= meta.length || about.x == 0.f) continue;
@@ -959,19 +957,28 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
           a[4 * c + k][3] = halves_hi<KIND>(hi[k]);
         }
       }
-#pragma unroll 2
-      for (int i = 0; i < blocks; ++i) {
-        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};          // two chains
+      // four blocks side by side, so that a product need not wait for the one before it (blocks behind the last hold no rows)
+#pragma unroll 1
+      for (int i0 = 0; i0 < blocks; i0 += 4) {
+        float s[4][4];
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint2 x = area.frag[(i * (D / 16) + k) * 32 + lane];
-          mma_f16(s[k & 1], a[k][0], a[k][1], a[k][2], a[k][3], x.x, x.y);
+        for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint2 x = area.frag[((i0 + i) * (D / 16) + k) * 32 + lane];
+            mma_f16(s[i], a[k][0], a[k][1], a[k][2], a[k][3], x.x, x.y);
+          }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i0 + i >= blocks) break;
+          const RowInfo rows[2] = {area.row[8 * (i0 + i) + 2 * t], area.row[8 * (i0 + i) + 2 * t + 1]};
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (key + g + 8 * (c >> 1) < rows[c & 1].limit)
+              sum[c >> 1] += exp2_approx(fmaf(s[i][c], rows[c & 1].factor * about.x, -rows[c & 1].lse2));
         }
-        const RowInfo rows[2] = {area.row[8 * i + 2 * t], area.row[8 * i + 2 * t + 1]};
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (key + g + 8 * (c >> 1) < rows[c & 1].limit)
-            sum[c >> 1] += exp2_approx(fmaf(s[0][c] + s[1][c], rows[c & 1].factor * about.x, -rows[c & 1].lse2));
       }
     }
     if (key < meta.length && about.x != 0.f) {

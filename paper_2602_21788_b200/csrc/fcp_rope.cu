@@ -98,10 +98,6 @@ __device__ __forceinline__ void turn_pair(float& x, float& y, float2 cs) {
 __device__ __forceinline__ float2 unpack(uint32_t w) {
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&p);
-}
 
 // HBM bound.  A block takes a few tokens: one sine and cosine per (token, pair), shared by all heads through shared memory,
 // then slots of 16 columns, heads fastest, so that neighbouring threads move neighbouring bytes.
@@ -115,6 +111,41 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   grid_begin();
   const int t0 = blockIdx.x * a.tokens, n = min(a.tokens, a.T - t0);
   const int tid = threadIdx.x;
+  const int pairs = a.rotary / 2, turned = a.rotary / 16;
+  const int heads = a.hq + a.hkv, slots = WIDE ? a.D / 16 : a.D / 2, total = n * heads * slots;
+  auto place = [&](int i, const __nv_bfloat16*& src, __nv_bfloat16*& dst, int& t, int& s) {
+    const int row = i / slots;
+    s = i - row * slots;
+    t = row / heads;
+    const int h = row - t * heads;
+    const int64_t tok = t0 + t;
+    if (h < a.hq) {
+      src = a.q + tok * a.q_stride + h * a.D;
+      dst = a.q_out + tok * a.q_out_stride + h * a.D;
+    } else {
+      src = a.k + tok * a.k_stride + (h - a.hq) * a.D;
+      dst = a.k_out + tok * a.k_out_stride + (h - a.hq) * a.D;
+    }
+  };
+  constexpr int U = 2;                               // wide slots in flight per thread
+  uint4 x[U], y[U];
+  __nv_bfloat16* dst[U];
+  int t[U], s[U], cx[U], cy[U];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * ROPE_THREADS;
+      if (i >= total) continue;
+      const __nv_bfloat16* src;
+      place(i, src, dst[u], t[u], s[u]);
+      const bool half = LAYOUT == FCP_ROPE_HALF && s[u] < turned;      // columns of the two pieces
+      cx[u] = half ? s[u] * 8 : s[u] * 16;
+      cy[u] = half ? pairs + s[u] * 8 : s[u] * 16 + 8;
+      x[u] = ld_v4(src + cx[u]);
+      y[u] = ld_v4(src + cy[u]);
+    }
+  };
+  if (WIDE) fetch(tid);                              // the first values travel while positions and angles are found
   if (a.positions) {
     if (tid < n) {
       pos[tid] = ld_i32(a.positions + t0 + tid);
@@ -141,57 +172,20 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
     }
   }
   __syncthreads();
-  const int pairs = a.rotary / 2;
   for (int i = tid; i < n * pairs; i += ROPE_THREADS) {
     const int t = i / pairs, p = i - t * pairs;
     const int32_t part = (int32_t)(((uint64_t)pos[t] * a.turn[p]) >> 32);      // fraction of a turn, two's complement
     float s, c;
     sincospif((float)part * 0x1p-31f, &s, &c);
-    // wide slots read their 8 pairs in a row
     cs[t * 64 + p] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
   }
   __syncthreads();
-  const int heads = a.hq + a.hkv, slots = WIDE ? a.D / 16 : a.D / 2, total = n * heads * slots;
-  auto place = [&](int i, const __nv_bfloat16*& src, __nv_bfloat16*& dst, int& t, int& s) {
-    const int row = i / slots;
-    s = i - row * slots;
-    t = row / heads;
-    const int h = row - t * heads;
-    const int64_t tok = t0 + t;
-    if (h < a.hq) {
-      src = a.q + tok * a.q_stride + h * a.D;
-      dst = a.q_out + tok * a.q_out_stride + h * a.D;
-    } else {
-      src = a.k + tok * a.k_stride + (h - a.hq) * a.D;
-      dst = a.k_out + tok * a.k_out_stride + (h - a.hq) * a.D;
-    }
-    return ok[t] != 0;
-  };
   if (WIDE) {
-    const int turned = a.rotary / 16;
-    constexpr int U = 2;                             // slots in flight per thread
     for (int i0 = tid; i0 < total; i0 += U * ROPE_THREADS) {
-      uint4 x[U], y[U];
-      __nv_bfloat16* dst[U];
-      int t[U], s[U], cx[U], cy[U];
-      bool live[U];
+      if (i0 != tid) fetch(i0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * ROPE_THREADS;
-        const __nv_bfloat16* src = nullptr;
-        live[u] = i < total && place(i, src, dst[u], t[u], s[u]);
-        if (live[u]) {
-          // columns of the two pieces
-          const bool half = LAYOUT == FCP_ROPE_HALF && s[u] < turned;
-          cx[u] = half ? s[u] * 8 : s[u] * 16;
-          cy[u] = half ? pairs + s[u] * 8 : s[u] * 16 + 8;
-          x[u] = ld_v4(src + cx[u]);
-          y[u] = ld_v4(src + cy[u]);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!live[u]) continue;
+        if (i0 + u * ROPE_THREADS >= total || !ok[t[u]]) continue;
         if (s[u] < turned) {
           uint32_t wx[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, wy[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
           const float4* c4 = reinterpret_cast<const float4*>(cs + t[u] * 64 + s[u] * 8);
@@ -202,15 +196,15 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
               float2 u2 = unpack(wx[j]), v2 = unpack(wy[j]);
               turn_pair(u2.x, v2.x, make_float2(c.x, c.y));
               turn_pair(u2.y, v2.y, make_float2(c.z, c.w));
-              wx[j] = pack(u2.x, u2.y);
-              wy[j] = pack(v2.x, v2.y);
+              wx[j] = pack_bf16(u2.x, u2.y);
+              wy[j] = pack_bf16(v2.x, v2.y);
             } else {                                 // word j of a piece is a pair
               const float4 c = c4[j >> 1], d = c4[2 + (j >> 1)];
               float2 u2 = unpack(wx[j]), v2 = unpack(wy[j]);
               turn_pair(u2.x, u2.y, j & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y));
               turn_pair(v2.x, v2.y, j & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y));
-              wx[j] = pack(u2.x, u2.y);
-              wy[j] = pack(v2.x, v2.y);
+              wx[j] = pack_bf16(u2.x, u2.y);
+              wy[j] = pack_bf16(v2.x, v2.y);
             }
           }
           x[u] = make_uint4(wx[0], wx[1], wx[2], wx[3]);
@@ -223,22 +217,22 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   } else {
     for (int i = tid; i < total; i += ROPE_THREADS) {
       const __nv_bfloat16* src;
-      __nv_bfloat16* dst;
-      int t, s;
-      if (!place(i, src, dst, t, s)) continue;
-      const bool half = LAYOUT == FCP_ROPE_HALF && s < pairs;
-      const int cx = half ? s : 2 * s, cy = half ? s + pairs : 2 * s + 1;
-      const volatile __nv_bfloat16* vs = src;
-      const uint16_t bx = *reinterpret_cast<const volatile uint16_t*>(vs + cx), by = *reinterpret_cast<const volatile uint16_t*>(vs + cy);
-      uint16_t ox = bx, oy = by;
-      if (s < pairs) {
-        float x = __uint_as_float((uint32_t)bx << 16), y = __uint_as_float((uint32_t)by << 16);
-        turn_pair(x, y, cs[t * 64 + s]);
-        ox = __bfloat16_as_ushort(__float2bfloat16_rn(x));
-        oy = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+      __nv_bfloat16* to;
+      int tok, slot;
+      place(i, src, to, tok, slot);
+      if (!ok[tok]) continue;
+      const bool half = LAYOUT == FCP_ROPE_HALF && slot < pairs;
+      const int c0 = half ? slot : 2 * slot, c1 = half ? slot + pairs : 2 * slot + 1;
+      const volatile uint16_t* bits = reinterpret_cast<const volatile uint16_t*>(src);
+      uint16_t o0 = bits[c0], o1 = bits[c1];
+      if (slot < pairs) {
+        float u = __uint_as_float((uint32_t)o0 << 16), v = __uint_as_float((uint32_t)o1 << 16);
+        turn_pair(u, v, cs[tok * 64 + slot]);
+        o0 = __bfloat16_as_ushort(__float2bfloat16_rn(u));
+        o1 = __bfloat16_as_ushort(__float2bfloat16_rn(v));
       }
-      *reinterpret_cast<uint16_t*>(dst + cx) = ox;
-      *reinterpret_cast<uint16_t*>(dst + cy) = oy;
+      reinterpret_cast<uint16_t*>(to)[c0] = o0;
+      reinterpret_cast<uint16_t*>(to)[c1] = o1;
     }
   }
 }
@@ -247,7 +241,7 @@ int rope(const char* call, float sign, const fcp_rope_table* table, int64_t T, c
          const void* k, int64_t k_stride, int32_t hkv, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
          const int32_t* positions, const int32_t* row_offset, const int32_t* length, int32_t B, void* stream) {
   if (!table || T < 0 || T >= (int64_t(1) << 31) - 8 || hq < 0 || hkv < 0 || B < 0 || (int64_t)hq + hkv > 65536 ||
-      (hq > 0 && (!q || !q_out)) || (hkv > 0 && (!k || !k_out)) || (!positions && !row_offset)) {
+      (T > 0 && ((hq > 0 && (!q || !q_out)) || (hkv > 0 && (!k || !k_out)) || (!positions && !row_offset)))) {
     fcp_set_error("%s: NULL buffer or invalid size", call);
     return FCP_ERR_INVALID_ARG;
   }

@@ -335,7 +335,7 @@ class RopeTable:
                                float(high), float(magnitude))
         self.struct = FcpRopeTable()
         _check(lib().fcp_rope_init(C.byref(config), C.byref(self.struct)))
-        self.ref = C.byref(self.struct)
+        self.ref, self.head_dim = C.byref(self.struct), self.struct.head_dim
 
     def frequencies(self) -> np.ndarray:
         """Radians per token of each pair, as the table holds them."""
@@ -352,40 +352,42 @@ def _named(names: dict, value) -> int:
     return int(value)
 
 
+# The checks below stand in front of kernels of a few microseconds: one look at shape and strides per tensor, no conversions.
 def _heads(x, head_dim, name):
-    """Rows, heads and row stride of a tensor [rows][heads][head_dim] whose heads are contiguous; None has no heads."""
-    if x is None:
-        return None, 0, 0
+    """Rows, heads, row stride and address of a tensor [rows][heads][head_dim] whose heads are contiguous."""
     rows, heads, d = x.shape
     s0, s1, s2 = x.stride()
-    if x.dtype.itemsize != 2 or d != head_dim or (s2 != 1 and d > 1) or (s1 != head_dim and heads > 1):
+    if d != head_dim or s2 != 1 or (s1 != d and heads > 1) or x.element_size() != 2:
         raise ValueError(f"{name}: a bf16 tensor [rows][heads][{head_dim}] with contiguous heads is wanted")
-    return rows, heads, s0 if rows > 1 else heads * head_dim
+    return rows, heads, s0 if rows > 1 else heads * d, x.data_ptr()
+
+
+_NO_HEADS = (None, 0, 0, None)
 
 
 def _i32_ptr(x, n, name):
     """Address of a contiguous int32 device tensor of n entries (None: NULL)."""
     if x is None:
         return None
-    if x.dtype.itemsize != 4 or x.is_floating_point() or not x.is_contiguous() or x.numel() != n:
+    if x.element_size() != 4 or x.numel() != n or x.is_floating_point() or not x.is_contiguous():
         raise ValueError(f"{name}: a contiguous int32 tensor of {n} entries is wanted")
     return x.data_ptr()
 
 
 def _rope(call, table, q, k, q_out, k_out, positions, row_offset, length, stream):
-    d = table.struct.head_dim
-    rows, hq, qs = _heads(q, d, "q")
-    k_rows, hkv, ks = _heads(k, d, "k")
-    T = rows if rows is not None else k_rows if k_rows is not None else 0
-    q_out_rows, hq_out, qos = _heads(q_out, d, "q_out")
-    k_out_rows, hkv_out, kos = _heads(k_out, d, "k_out")
-    if (hq_out, hkv_out) != (hq, hkv) or any(r not in (None, T) for r in (k_rows, q_out_rows, k_out_rows)):
+    d = table.head_dim
+    rows, hq, qs, qp = _NO_HEADS if q is None else _heads(q, d, "q")
+    k_rows, hkv, ks, kp = _NO_HEADS if k is None else _heads(k, d, "k")
+    q_out_rows, hq_out, qos, qop = _NO_HEADS if q_out is None else _heads(q_out, d, "q_out")
+    k_out_rows, hkv_out, kos, kop = _NO_HEADS if k_out is None else _heads(k_out, d, "k_out")
+    if hq_out != hq or hkv_out != hkv or q_out_rows != rows or k_out_rows != k_rows or (q is not None and k is not None and k_rows != rows):
         raise ValueError("q, k, q_out, k_out differ in rows or heads")
+    T = rows or k_rows or 0
     B = 0 if row_offset is None else row_offset.numel() - 1
-    _check(call(table.ref, T, q.data_ptr() if hq else None, qs, hq, k.data_ptr() if hkv else None, ks, hkv,
-                q_out.data_ptr() if hq else None, qos, k_out.data_ptr() if hkv else None, kos,
-                _i32_ptr(positions, T, "positions"), _i32_ptr(row_offset, B + 1, "row_offset"), _i32_ptr(length, B, "length"),
-                B, stream))
+    rc = call(table.ref, T, qp, qs, hq, kp, ks, hkv, qop, qos, kop, kos, _i32_ptr(positions, T, "positions"),
+              _i32_ptr(row_offset, B + 1, "row_offset"), _i32_ptr(length, B, "length"), B, stream)
+    if rc:
+        _check(rc)
 
 
 def fcp_rope_fwd(table: RopeTable, q, k, q_out, k_out, positions=None, row_offset=None, length=None, stream=0):
@@ -446,23 +448,21 @@ class CacheBatch:
     def __init__(self, page_table, length, row_offset=None, rows=0, max_new=None):
         B, width = page_table.shape
         self.tensors = (page_table, length, row_offset)
-        self.struct = FcpCacheBatch(B, int(rows), int(rows if max_new is None else max_new), width,
+        self.B, self.rows = B, int(rows)
+        self.struct = FcpCacheBatch(B, self.rows, int(rows if max_new is None else max_new), width,
                                     _i32_ptr(page_table, B * width, "page_table"), _i32_ptr(length, B, "length"),
                                     _i32_ptr(row_offset, B + 1, "row_offset"))
         self.ref = C.byref(self.struct)
 
 
-def _rows(x, batch, heads, head_dim, name):
-    rows, h, stride = _heads(x, head_dim, name)
-    if rows != batch.struct.rows or h != heads:
-        raise ValueError(f"{name}: {rows} rows of {h} heads, the batch has {batch.struct.rows} rows of {heads}")
-    return x.data_ptr(), stride
-
-
 def fcp_cache_append(cache: Cache, batch: CacheBatch, k, v, stream=0):
-    kp, ks = _rows(k, batch, cache.hkv, cache.head_dim, "k")
-    vp, vs = _rows(v, batch, cache.hkv, cache.head_dim, "v")
-    _check(lib().fcp_cache_append(cache.handle, batch.ref, kp, ks, vp, vs, stream))
+    k_rows, k_heads, ks, kp = _heads(k, cache.head_dim, "k")
+    v_rows, v_heads, vs, vp = _heads(v, cache.head_dim, "v")
+    if k_rows != batch.rows or v_rows != batch.rows or k_heads != cache.hkv or v_heads != cache.hkv:
+        raise ValueError(f"k, v: {batch.rows} rows of {cache.hkv} heads are wanted")
+    rc = lib().fcp_cache_append(cache.handle, batch.ref, kp, ks, vp, vs, stream)
+    if rc:
+        _check(rc)
 
 
 def fcp_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, hq) -> int:
@@ -472,19 +472,21 @@ def fcp_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, hq) -> int:
 
 
 def fcp_cache_attn(cache: Cache, batch: CacheBatch, q, o, lse, workspace, workspace_bytes, scale=0.0, accumulate=False, stream=0):
-    hq = q.shape[1]
-    qp, qs = _rows(q, batch, hq, cache.head_dim, "q")
-    if o.shape != q.shape or o.dtype.itemsize != 2 or not o.is_contiguous():
-        raise ValueError("o: a contiguous bf16 tensor of q's shape is wanted")
-    if tuple(lse.shape) != (q.shape[0], hq) or lse.dtype.itemsize != 4 or not lse.is_contiguous():
+    rows, hq, qs, qp = _heads(q, cache.head_dim, "q")
+    o_rows, o_heads, _, op = _heads(o, cache.head_dim, "o")
+    if rows != batch.rows or o_rows != rows or o_heads != hq or not o.is_contiguous():
+        raise ValueError(f"q, o: {batch.rows} rows of the same heads are wanted, o contiguous")
+    if lse.numel() != rows * hq or lse.element_size() != 4 or not lse.is_contiguous():
         raise ValueError("lse: a contiguous fp32 tensor [rows][hq] is wanted")
-    _check(lib().fcp_cache_attn(cache.handle, batch.ref, qp, qs, hq, float(scale), o.data_ptr(), lse.data_ptr(), int(bool(accumulate)),
-                                _ptr(workspace), int(workspace_bytes), stream))
+    rc = lib().fcp_cache_attn(cache.handle, batch.ref, qp, qs, hq, scale, op, lse.data_ptr(), 1 if accumulate else 0,
+                              None if workspace is None else workspace.data_ptr(), workspace_bytes, stream)
+    if rc:
+        _check(rc)
 
 
 def fcp_cache_evict(cache: Cache, batch: CacheBatch, n_sink, n_heavy, n_recent, dst_table, new_length, kept, stream=0):
     B, width = dst_table.shape
-    if B != batch.struct.B:
+    if B != batch.B:
         raise ValueError("dst_table and the batch differ in their number of sequences")
     keep = int(n_sink) + int(n_heavy) + int(n_recent)
     _check(lib().fcp_cache_evict(cache.handle, batch.ref, int(n_sink), int(n_heavy), int(n_recent),

@@ -74,7 +74,7 @@ def test_rope_calls_that_are_refused():
         for more in bad:
             assert call(f=f, **more) == fcp.FCP_ERR_INVALID_ARG, more
             assert fcp.lib().fcp_last_error_message()
-        for nothing in (dict(T=0), dict(hq=0, hkv=0), dict(pos=None, off=p, B=0)):       # nothing to do: no GPU is asked for
+        for nothing in (dict(T=0), dict(T=0, q=None, k=None, qo=None, ko=None, pos=None), dict(hq=0, hkv=0), dict(pos=None, off=p, B=0)):       # nothing to do: no GPU is asked for
             assert call(f=f, **nothing) == fcp.FCP_OK
     blank = fcp.FcpRopeTable()
     assert call(table=C.byref(blank)) == fcp.FCP_ERR_INVALID_ARG
@@ -269,7 +269,7 @@ def test_every_kernel_waits_for_the_one_before_it(name):
     """Kernels become resident while the one before them still writes: each one waits in front of its first access."""
     code = re.sub(r"/\*.*?\*/|//[^\n]*", "", open(os.path.join(CSRC, name)).read(), flags=re.S)
     bodies = re.findall(r"__global__[^{;]*\)\s*\{(.*?)\n\}", code, flags=re.S)
-    assert len(bodies) == {"fcp_rope.cu": 1, "fcp_cache.cuh": 5}[name]
+    assert len(bodies) == {"fcp_rope.cu": 1, "fcp_cache.cuh": 7}[name]
     for body in bodies:
         wait = re.search(r"grid_(begin|wait)\(\)", body)
         assert wait and not re.search(r"\bld_|tma_load", body[:wait.start()])
