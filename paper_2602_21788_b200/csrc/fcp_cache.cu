@@ -290,11 +290,19 @@ extern "C" int fcp_cache_device_status(const fcp_cache* cache, int32_t* status) 
 // ---------------------------------------------------------------------------------------------
 namespace {
 typedef void (*AppendKernel)(const AppendArgs);
+constexpr int kPieces = 4;                            // of 16 values per thread: 32 registers
 template <int D, int KIND>
-AppendKernel append_kernel(int page_tokens) {
-  const int n = page_tokens * D / (16 * APPEND_THREADS);
-  return n <= 1 ? cache_append_kernel<D, KIND, 1> : n == 2 ? cache_append_kernel<D, KIND, 2>
-         : n == 4 ? cache_append_kernel<D, KIND, 4> : cache_append_kernel<D, KIND, 8>;
+AppendKernel append_kernel(int warps) {
+  switch (warps) {
+    case 1: return cache_append_kernel<D, KIND, kPieces, 1>;
+    case 2: return cache_append_kernel<D, KIND, kPieces, 2>;
+    case 4: return cache_append_kernel<D, KIND, kPieces, 4>;
+    default: return cache_append_kernel<D, KIND, kPieces, 8>;
+  }
+}
+AppendKernel append_kernel(const fcp_cache_config& c, int warps) {
+  if (c.head_dim == 128) return c.kind == FCP_CACHE_E4M3 ? append_kernel<128, FCP_CACHE_E4M3>(warps) : append_kernel<128, FCP_CACHE_INT8>(warps);
+  return c.kind == FCP_CACHE_E4M3 ? append_kernel<64, FCP_CACHE_E4M3>(warps) : append_kernel<64, FCP_CACHE_INT8>(warps);
 }
 }  // namespace
 
@@ -316,11 +324,9 @@ extern "C" int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* b
   a.k_stride = k_stride;
   a.v_stride = v_stride;
   a.slots = batch->max_new == 1 ? batch->B : append_slot(batch->rows, batch->B, c.page_tokens);
-  AppendKernel kernel = c.head_dim == 128 ? (c.kind == FCP_CACHE_E4M3 ? append_kernel<128, FCP_CACHE_E4M3>(c.page_tokens)
-                                                                       : append_kernel<128, FCP_CACHE_INT8>(c.page_tokens))
-                                          : (c.kind == FCP_CACHE_E4M3 ? append_kernel<64, FCP_CACHE_E4M3>(c.page_tokens)
-                                                                      : append_kernel<64, FCP_CACHE_INT8>(c.page_tokens));
-  FCP_CUDA_CHECK(launch(kernel, dim3((unsigned)a.slots, (unsigned)(2 * c.hkv)), APPEND_THREADS, 0, (cudaStream_t)stream, a));
+  const int warps = append_warps(c.page_tokens, c.head_dim, kPieces), threads = append_threads(warps), parts = threads / (32 * warps);
+  const dim3 grid((unsigned)a.slots, (unsigned)((2 * c.hkv + parts - 1) / parts));
+  FCP_CUDA_CHECK(launch(append_kernel(c, warps), grid, threads, 0, (cudaStream_t)stream, a));
   return FCP_OK;
 }
 

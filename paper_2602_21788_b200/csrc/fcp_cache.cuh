@@ -79,6 +79,16 @@ __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d)
   auto one = [](float x) { return (uint32_t)min(127, max(-127, __float2int_rn(x))) & 0xffu; };       // NaN: 0
   return one(a) | (one(b) << 8) | (one(c) << 16) | (one(d) << 24);
 }
+// The same for finite values within the range of the codes, times the inverse of a power of two.  int8: added to 1.5 * 2^23 a value
+// is rounded to an integer, ties to even, which the low byte holds; limits, shifts and conversions took 19 instructions a value.
+template <int KIND>
+__device__ __forceinline__ uint32_t small_codes(const float4& f, float inverse) {
+  if (KIND == FCP_CACHE_E4M3) return to_codes<KIND>(f.x * inverse, f.y * inverse, f.z * inverse, f.w * inverse);
+  const float magic = 12582912.f;
+  const uint32_t a = __float_as_uint(fmaf(f.x, inverse, magic)), b = __float_as_uint(fmaf(f.y, inverse, magic));
+  const uint32_t c = __float_as_uint(fmaf(f.z, inverse, magic)), d = __float_as_uint(fmaf(f.w, inverse, magic));
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
 template <int KIND>
 __device__ __forceinline__ uint32_t rescale_codes(uint32_t w, float ratio) {
   const uint32_t lo = halves_lo<KIND>(w), hi = halves_hi<KIND>(w);
@@ -113,27 +123,31 @@ struct AppendArgs {
   int32_t slots;
 };
 
-// One block per (page touched, head, K or V): the page's new values stay in registers between the maximum and the codes.
-constexpr int APPEND_THREADS = 128;
-template <int D, int KIND, int N>                    // N: pieces of 16 values per thread
-__global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __grid_constant__ AppendArgs a) {
-  __shared__ uint32_t warp_max[APPEND_THREADS / 32];
+// One piece of work per (page touched, head, K or V), for as many warps as give a thread N pieces of 16 values, which stay in
+// registers between the maximum and the codes.  HBM bound: 64K tokens of 8 heads, pages of 64, int8: TODO.
+constexpr int append_warps(int page_tokens, int D, int N) { return page_tokens * D / (512 * N) < 1 ? 1 : page_tokens * D / (512 * N); }
+__host__ __device__ constexpr int append_threads(int warps) { return 32 * (warps < 4 ? 4 : warps); }
+template <int D, int KIND, int N, int WARPS>
+__global__ void __launch_bounds__(append_threads(WARPS)) cache_append_kernel(const __grid_constant__ AppendArgs a) {
+  constexpr int THREADS = append_threads(WARPS), GROUP = 32 * WARPS;        // of the block, of a piece of work
+  __shared__ uint32_t warp_max[THREADS / 32];
   grid_begin();
-  const int w = blockIdx.x, h = blockIdx.y >> 1, tid = threadIdx.x;
-  const bool is_v = blockIdx.y & 1;
+  const int w = blockIdx.x, part = blockIdx.y * (THREADS / GROUP) + threadIdx.x / GROUP, h = part >> 1, tid = threadIdx.x % GROUP;
+  const bool is_v = part & 1;
   const int page_tokens = a.c.page_tokens;
   int b = w;                                         // one token, one page: a slot per sequence
   if (a.s.max_new != 1) {
-    // the last b whose first slot is at most w, by all threads: APPEND_THREADS sequences a round
+    // the last b whose first slot is at most w, by all threads: THREADS sequences a round
     int lo = 0, hi = a.s.B - 1;
     while (lo < hi) {
-      const int step = (hi - lo + APPEND_THREADS - 1) / APPEND_THREADS, at = lo + (tid + 1) * step;
+      const int step = (hi - lo + THREADS - 1) / THREADS, at = lo + ((int)threadIdx.x + 1) * step;
       const int below = __syncthreads_count(at <= hi && append_slot(ld_i32(a.s.row_offset + min(at, a.s.B - 1)), min(at, a.s.B - 1), page_tokens) <= w);
       lo += below * step;
       hi = min(hi, lo + step - 1);
     }
     b = lo;
   }
+  if (h >= a.c.hkv) return;
   const SeqView sv = load_seq(a.s, b);
   const int slot = a.s.max_new == 1 ? 0 : w - append_slot(sv.row0, b, page_tokens);
   if (sv.bad) {
@@ -153,7 +167,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
   uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int e = i * APPEND_THREADS + tid, s = e / C, c = e % C;
+    const int e = i * GROUP + tid, s = e / C, c = e % C;
     r[i][0] = r[i][1] = make_uint4(0, 0, 0, 0);
     if (s >= held && s < filled) {
       const __nv_bfloat16* p = x + (first + s) * stride + c * 16;
@@ -170,36 +184,63 @@ __global__ void __launch_bounds__(APPEND_THREADS) cache_append_kernel(const __gr
     return;
   }
   if (held > 0) old = ld_f32(scales + cell);
+  auto group_sync = [&] {                            // also: every thread has read the old scale before one writes it
+    // barrier numbers that the compiler sees: with one in a register a block takes all 16, which leaves room for few blocks (64K
+    // tokens 98 us instead of 69)
+    if (WARPS == 1) __syncwarp();
+    else if (WARPS >= 4) __syncthreads();
+    else if (threadIdx.x < GROUP) asm volatile("bar.sync 1, %0;" ::"n"(GROUP) : "memory");
+    else asm volatile("bar.sync 2, %0;" ::"n"(GROUP) : "memory");
+  };
+  auto group_max = [&](uint32_t x) {
+    x = __reduce_max_sync(0xffffffffu, x);
+    if (WARPS == 1) return x;
+    if ((tid & 31) == 0) warp_max[threadIdx.x >> 5] = x;
+    group_sync();
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) x = max(x, warp_max[threadIdx.x / GROUP * WARPS + i]);
+    return x;
+  };
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const uint32_t* u = reinterpret_cast<const uint32_t*>(r[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) most = max(most, max(abs_bits(u[j]), abs_bits(u[j] >> 16)));
+    for (int j = 0; j < 8; ++j) most = __vmaxu2(most, u[j] & 0x7fff7fffu);
   }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if ((tid & 31) == 0) warp_max[tid >> 5] = most;
-  __syncthreads();
+  most = group_max(max(most & 0xffffu, most >> 16));
+  const bool odd = most >= 0x7f80u;                  // an infinity or a NaN on this page: again, with care
+  if (odd) {
+    most = 0;
 #pragma unroll
-  for (int i = 0; i < APPEND_THREADS / 32; ++i) most = max(most, warp_max[i]);
+    for (int i = 0; i < N; ++i) {
+      const uint32_t* u = reinterpret_cast<const uint32_t*>(r[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = max(most, max(abs_bits(u[j]), abs_bits(u[j] >> 16)));
+    }
+    group_sync();
+    most = group_max(most);
+  }
   uint8_t* codes = (is_v ? a.c.v : a.c.k) + (int64_t)row * D;
   float scale = fresh_scale<KIND>(most);
-  if (held > 0) scale = fmaxf(old, scale);           // every thread has read the old scale before the barrier above
+  if (held > 0) scale = fmaxf(old, scale);
+  if (WARPS == 1) __syncwarp();
   if (tid == 0 && !(held > 0 && scale == old)) scales[cell] = scale;
   const float inverse = 1.f / scale;                 // exact for powers of two; x / scale otherwise below
   const bool exact = (__float_as_uint(scale) & 0x7fffffu) == 0;
   if (!is_v && a.c.weight)
-    for (int s = held + tid; s < filled; s += APPEND_THREADS) a.c.weight[(int64_t)row + s] = 0.f;
+    for (int s = held + tid; s < filled; s += GROUP) a.c.weight[(int64_t)row + s] = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int e = i * APPEND_THREADS + tid, s = e / C, c = e % C;
+    const int e = i * GROUP + tid, s = e / C, c = e % C;
     if (s >= held && s < filled) {
       const uint32_t* u = reinterpret_cast<const uint32_t*>(r[i]);
       uint32_t out[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float4 f = make_float4(bf_lo(u[2 * j]), bf_hi(u[2 * j]), bf_lo(u[2 * j + 1]), bf_hi(u[2 * j + 1]));
-        out[j] = exact ? to_codes<KIND>(f.x * inverse, f.y * inverse, f.z * inverse, f.w * inverse)
-                       : to_codes<KIND>(__fdiv_rn(f.x, scale), __fdiv_rn(f.y, scale), __fdiv_rn(f.z, scale), __fdiv_rn(f.w, scale));
+        out[j] = exact && !odd ? small_codes<KIND>(f, inverse)
+                 : exact       ? to_codes<KIND>(f.x * inverse, f.y * inverse, f.z * inverse, f.w * inverse)
+                               : to_codes<KIND>(__fdiv_rn(f.x, scale), __fdiv_rn(f.y, scale), __fdiv_rn(f.z, scale), __fdiv_rn(f.w, scale));
       }
       *reinterpret_cast<uint4*>(codes + s * D + c * 16) = make_uint4(out[0], out[1], out[2], out[3]);
     } else if (s < held && scale != old) {

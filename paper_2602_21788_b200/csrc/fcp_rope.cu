@@ -1,4 +1,5 @@
 // Rotary positions: table (host) and the kernel behind fcp_rope_fwd and fcp_rope_bwd.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -72,7 +73,8 @@ extern "C" int fcp_rope_init(const fcp_rope_config* c, fcp_rope_table* t) {
 namespace {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_TOKENS = 4;           // most tokens of one block
+constexpr int ROPE_TOKENS = 16;          // most tokens of one block
+constexpr int ROPE_SLOTS = 1280;         // slots of a block, where it may choose: 5 per thread
 
 struct RopeArgs {
   const __nv_bfloat16 *q, *k;
@@ -112,12 +114,18 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   const int t0 = blockIdx.x * a.tokens, n = min(a.tokens, a.T - t0);
   const int tid = threadIdx.x;
   const int pairs = a.rotary / 2, turned = a.rotary / 16;
-  const int heads = a.hq + a.hkv, slots = WIDE ? a.D / 16 : a.D / 2, total = n * heads * slots;
-  auto place = [&](int i, const __nv_bfloat16*& src, __nv_bfloat16*& dst, int& t, int& s) {
-    const int row = i / slots;
-    s = i - row * slots;
-    t = row / heads;
-    const int h = row - t * heads;
+  // slots of a head's row: a power of two, so that a thread keeps its slot and steps over rows
+  const int heads = a.hq + a.hkv, slots = WIDE ? a.D / 16 : a.D / 2;
+  const int s = tid & (slots - 1), stride = ROPE_THREADS / slots;
+  int t = 0, h = tid / slots;                        // token and head of the row to be fetched next
+  auto settle = [&] {
+    while (h >= heads) {
+      h -= heads;
+      ++t;
+    }
+  };
+  settle();
+  auto row = [&](const __nv_bfloat16*& src, __nv_bfloat16*& dst) {
     const int64_t tok = t0 + t;
     if (h < a.hq) {
       src = a.q + tok * a.q_stride + h * a.D;
@@ -127,25 +135,29 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
       dst = a.k_out + tok * a.k_out_stride + (h - a.hq) * a.D;
     }
   };
+  // columns of a wide slot's two pieces
+  const bool half = LAYOUT == FCP_ROPE_HALF && s < turned;
+  const int cx = half ? s * 8 : s * 16, cy = half ? pairs + s * 8 : s * 16 + 8;
   constexpr int U = 2;                               // wide slots in flight per thread
   uint4 x[U], y[U];
   __nv_bfloat16* dst[U];
-  int t[U], s[U], cx[U], cy[U];
-  auto fetch = [&](int i0) {
+  int at[U];                                         // token; -1: none
+  auto fetch = [&] {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * ROPE_THREADS;
-      if (i >= total) continue;
-      const __nv_bfloat16* src;
-      place(i, src, dst[u], t[u], s[u]);
-      const bool half = LAYOUT == FCP_ROPE_HALF && s[u] < turned;      // columns of the two pieces
-      cx[u] = half ? s[u] * 8 : s[u] * 16;
-      cy[u] = half ? pairs + s[u] * 8 : s[u] * 16 + 8;
-      x[u] = ld_v4(src + cx[u]);
-      y[u] = ld_v4(src + cy[u]);
+      at[u] = -1;
+      if (t < n) {
+        const __nv_bfloat16* src;
+        row(src, dst[u]);
+        at[u] = t;
+        x[u] = ld_v4(src + cx);
+        y[u] = ld_v4(src + cy);
+        h += stride;
+        settle();
+      }
     }
   };
-  if (WIDE) fetch(tid);                              // the first values travel while positions and angles are found
+  if (WIDE) fetch();                                 // the first values travel while positions and angles are found
   if (a.positions) {
     if (tid < n) {
       pos[tid] = ld_i32(a.positions + t0 + tid);
@@ -175,20 +187,19 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   for (int i = tid; i < n * pairs; i += ROPE_THREADS) {
     const int t = i / pairs, p = i - t * pairs;
     const int32_t part = (int32_t)(((uint64_t)pos[t] * a.turn[p]) >> 32);      // fraction of a turn, two's complement
-    float s, c;
-    sincospif((float)part * 0x1p-31f, &s, &c);
-    cs[t * 64 + p] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
+    float sine, cosine;
+    sincospif((float)part * 0x1p-31f, &sine, &cosine);
+    cs[t * 64 + p] = make_float2(cosine * a.magnitude, sine * a.magnitude * a.sign);
   }
   __syncthreads();
   if (WIDE) {
-    for (int i0 = tid; i0 < total; i0 += U * ROPE_THREADS) {
-      if (i0 != tid) fetch(i0);
+    while (at[0] >= 0) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (i0 + u * ROPE_THREADS >= total || !ok[t[u]]) continue;
-        if (s[u] < turned) {
+        if (at[u] < 0 || !ok[at[u]]) continue;
+        if (s < turned) {
           uint32_t wx[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, wy[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
-          const float4* c4 = reinterpret_cast<const float4*>(cs + t[u] * 64 + s[u] * 8);
+          const float4* c4 = reinterpret_cast<const float4*>(cs + at[u] * 64 + s * 8);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if (LAYOUT == FCP_ROPE_HALF) {           // words j of both pieces: pairs 2j, 2j + 1
@@ -210,24 +221,23 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
           x[u] = make_uint4(wx[0], wx[1], wx[2], wx[3]);
           y[u] = make_uint4(wy[0], wy[1], wy[2], wy[3]);
         }
-        *reinterpret_cast<uint4*>(dst[u] + cx[u]) = x[u];
-        *reinterpret_cast<uint4*>(dst[u] + cy[u]) = y[u];
+        *reinterpret_cast<uint4*>(dst[u] + cx) = x[u];
+        *reinterpret_cast<uint4*>(dst[u] + cy) = y[u];
       }
+      fetch();
     }
   } else {
-    for (int i = tid; i < total; i += ROPE_THREADS) {
+    const int c0 = LAYOUT == FCP_ROPE_HALF && s < pairs ? s : 2 * s, c1 = LAYOUT == FCP_ROPE_HALF && s < pairs ? s + pairs : 2 * s + 1;
+    for (; t < n; h += stride, settle()) {
       const __nv_bfloat16* src;
       __nv_bfloat16* to;
-      int tok, slot;
-      place(i, src, to, tok, slot);
-      if (!ok[tok]) continue;
-      const bool half = LAYOUT == FCP_ROPE_HALF && slot < pairs;
-      const int c0 = half ? slot : 2 * slot, c1 = half ? slot + pairs : 2 * slot + 1;
+      row(src, to);
+      if (!ok[t]) continue;
       const volatile uint16_t* bits = reinterpret_cast<const volatile uint16_t*>(src);
       uint16_t o0 = bits[c0], o1 = bits[c1];
-      if (slot < pairs) {
+      if (s < pairs) {
         float u = __uint_as_float((uint32_t)o0 << 16), v = __uint_as_float((uint32_t)o1 << 16);
-        turn_pair(u, v, cs[tok * 64 + slot]);
+        turn_pair(u, v, cs[t * 64 + s]);
         o0 = __bfloat16_as_ushort(__float2bfloat16_rn(u));
         o1 = __bfloat16_as_ushort(__float2bfloat16_rn(v));
       }
@@ -284,8 +294,10 @@ int rope(const char* call, float sign, const fcp_rope_table* table, int64_t T, c
   const uintptr_t bases = (uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out;
   const int64_t strides = a.q_stride | a.k_stride | a.q_out_stride | a.k_out_stride;
   const bool wide = a.rotary % 16 == 0 && (bases & 15) == 0 && strides % 8 == 0;
-  // one token per block while that leaves SMs without a block, else four (one sine and cosine per thread)
-  a.tokens = T <= 4 * FCP_PLAN_SMS ? 1 : ROPE_TOKENS;
+  // As many tokens per block as make ROPE_SLOTS slots, because finding the sequence and the angles costs a thread as much as three
+  // slots; fewer where SMs would be left without a block.
+  const int per_token = (hq + hkv) * (wide ? a.D / 16 : a.D / 2);
+  a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({ROPE_TOKENS, ROPE_SLOTS / per_token, T / (2 * FCP_PLAN_SMS)}));
   const unsigned grid = (unsigned)((T + a.tokens - 1) / a.tokens);
   cudaStream_t st = (cudaStream_t)stream;
   const bool half = table->layout == FCP_ROPE_HALF;
