@@ -432,7 +432,7 @@ int fcp_rope_bwd(const fcp_rope_table* table, int64_t T, const void* dq, int64_t
 typedef struct fcp_cache fcp_cache;
 typedef struct fcp_cache_config {
   void    *k, *v;                    /* 16-byte aligned                                        */
-  float   *k_scale, *v_scale, *weight;
+  float   *k_scale, *v_scale, *weight;   /* weight: 16-byte aligned                            */
   int32_t *status;
   int32_t n_pages;                   /* n_pages * hkv * page_tokens < 2^31                     */
   int32_t page_tokens;               /* 16, 32, 64 or 128                                      */

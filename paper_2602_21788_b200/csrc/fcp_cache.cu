@@ -239,7 +239,7 @@ extern "C" int fcp_cache_create(const fcp_cache_config* c, fcp_cache** cache) {
   }
   *cache = nullptr;
   if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->status || (((uintptr_t)c->k | (uintptr_t)c->v) & 15) != 0 ||
-      (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale | (uintptr_t)c->weight | (uintptr_t)c->status) & 3) != 0) {
+      ((uintptr_t)c->weight & 15) != 0 || (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale | (uintptr_t)c->status) & 3) != 0) {
     fcp_set_error("fcp_cache_create: a buffer is NULL or not aligned");
     return FCP_ERR_INVALID_ARG;
   }
@@ -483,7 +483,7 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const fcp_cache_batch* ba
   cudaStream_t st = (cudaStream_t)stream;
   // about 8 candidates per thread, as far as eight blocks go
   const int cluster = a.s.capacity > 32768 ? 8 : a.s.capacity > 16384 ? 4 : a.s.capacity > 8192 ? 2 : 1;
-  const size_t smem = (size_t)std::min(SELECT_KEYS, (a.s.capacity + cluster - 1) / cluster) * 4;
+  const size_t smem = (size_t)std::min(SELECT_KEYS, (a.s.capacity + cluster - 1) / cluster + 8) * 4;        // whole fours at both ends
   FCP_CUDA_CHECK(launch_clusters(cluster, cache_select_kernel, dim3((unsigned)(c.hkv * cluster), (unsigned)batch->B), SELECT_THREADS, smem, st, a));
   const dim3 grid((unsigned)((keep + MOVE_TOKENS - 1) / MOVE_TOKENS), (unsigned)c.hkv, (unsigned)batch->B);
   if (c.head_dim == 128) {

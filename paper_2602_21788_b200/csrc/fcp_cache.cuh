@@ -95,6 +95,29 @@ __device__ __forceinline__ uint32_t rescale_codes(uint32_t w, float ratio) {
   const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
   return to_codes<KIND>(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio);
 }
+// The same for a power of two of at most 1, in halves.  A code times it is exact, or below 2^-14, where e4m3 has nothing but 0; an
+// int8 code times it plus 1.5 * 2^10 is rounded to an integer, which the low byte holds.
+template <int KIND>
+__device__ __forceinline__ uint32_t shrink_codes(uint32_t w, __half2 ratio) {
+  const uint32_t lo = halves_lo<KIND>(w), hi = halves_hi<KIND>(w);
+  const __half2 a = *reinterpret_cast<const __half2*>(&lo), b = *reinterpret_cast<const __half2*>(&hi);
+  if (KIND == FCP_CACHE_E4M3) {
+    const __half2 x = __hmul2(a, ratio), y = __hmul2(b, ratio);
+    return (uint32_t)__nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&x), __NV_SATFINITE, __NV_E4M3) |
+           (uint32_t)__nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&y), __NV_SATFINITE, __NV_E4M3) << 16;
+  }
+  const __half2 magic = __float2half2_rn(1536.f);
+  return __byte_perm(h2_bits(__hfma2(a, ratio, magic)), h2_bits(__hfma2(b, ratio, magic)), 0x6420);
+}
+template <int KIND>
+__device__ __forceinline__ uint4 moved_codes(const uint4& x, float ratio) {
+  if (ratio == 1.f) return x;
+  if ((__float_as_uint(ratio) & 0x7fffffu) == 0 && ratio < 1.f) {
+    const __half2 r = __float2half2_rn(ratio);        // below 2^-24: 0, and so are the codes
+    return make_uint4(shrink_codes<KIND>(x.x, r), shrink_codes<KIND>(x.y, r), shrink_codes<KIND>(x.z, r), shrink_codes<KIND>(x.w, r));
+  }
+  return make_uint4(rescale_codes<KIND>(x.x, ratio), rescale_codes<KIND>(x.y, ratio), rescale_codes<KIND>(x.z, ratio), rescale_codes<KIND>(x.w, ratio));
+}
 // |x| of a bf16 as ordered bits; infinities count as the largest finite value, NaN as 0
 __device__ __forceinline__ uint32_t abs_bits(uint32_t h) {
   h &= 0x7fffu;
@@ -246,8 +269,7 @@ __global__ void __launch_bounds__(append_threads(WARPS)) cache_append_kernel(con
     } else if (s < held && scale != old) {
       const float ratio = __fdiv_rn(old, scale);
       const uint4 u = ld_v4(codes + s * D + c * 16);
-      *reinterpret_cast<uint4*>(codes + s * D + c * 16) =
-          make_uint4(rescale_codes<KIND>(u.x, ratio), rescale_codes<KIND>(u.y, ratio), rescale_codes<KIND>(u.z, ratio), rescale_codes<KIND>(u.w, ratio));
+      *reinterpret_cast<uint4*>(codes + s * D + c * 16) = moved_codes<KIND>(u, ratio);
     }
   }
 }
@@ -1269,9 +1291,9 @@ __device__ __forceinline__ int32_t usable_length(const BatchView& s, int b) {
   return n < 0 || n > s.capacity ? -1 : n;
 }
 
-// Weights as unsigned keys of the same order; NaN and what lies on a page that does not exist come last.
+// Weights as unsigned keys of the same order; NaN and what lies on a page that does not exist come last.  0 is no candidate.
 __device__ __forceinline__ uint32_t weight_key(float x) {
-  if (x != x) return 0u;
+  if (x != x) return 1u;
   const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);
   return u >> 31 ? ~u : u | 0x80000000u;
 }
@@ -1279,12 +1301,14 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
 // Which tokens of a head stay: one cluster of blocks per (KV head, sequence), each with its slice of the candidates.  The n_heavy
 // largest weights by three counting passes over 11, 11 and 10 bits of the keys, from the top, the counts added up over the cluster;
 // then one pass writes the kept positions in order.
+// Keys go four at a time: they lie side by side in a page, and one place in the page table, one load and one address serve them
+// (key by key the kernel was bound by its instructions, 120 000 warp instructions per block).
 constexpr int SELECT_THREADS = 1024;
 constexpr int SELECT_KEYS = 49152;                    // as many keys of a slice stay in shared memory
 constexpr int SELECT_BINS = 2048;
 constexpr int SELECT_BLOCKS = 8;                      // most blocks of a cluster
 __global__ void __launch_bounds__(SELECT_THREADS, 2) cache_select_kernel(const __grid_constant__ EvictArgs a) {
-  extern __shared__ uint32_t keys[];
+  extern __shared__ __align__(16) uint4 keys[];
   __shared__ __align__(8) uint32_t sums[2][SELECT_BINS];       // of this block, read by the others: one per pass in turn
   __shared__ uint32_t warp_count[32][2];
   __shared__ uint32_t share[2];                       // kept and equal keys of this block, read by the others
@@ -1304,40 +1328,38 @@ __global__ void __launch_bounds__(SELECT_THREADS, 2) cache_select_kernel(const _
     for (int i = first; i < keep; i += stride) kept[i] = i < length ? i : -1;
     return;
   }
-  const int page_tokens = a.c.page_tokens, end = length - a.n_recent, n_all = end - a.n_sink;  // candidates [n_sink, end)
+  const int page_tokens = a.c.page_tokens, end = length - a.n_recent;          // candidates: positions [n_sink, end)
   for (int i = first; i < a.n_sink; i += stride) kept[i] = i;
   for (int i = first; i < a.n_recent; i += stride) kept[a.n_sink + a.n_heavy + i] = end + i;
   if (a.n_heavy == 0) return;
-  const int per = (n_all + blocks - 1) / blocks, from = a.n_sink + min(n_all, rank * per), n = min(n_all, rank * per + per) - min(n_all, rank * per);
-  auto key_at = [&](int i) {
-    const int pos = from + i;
-    const int32_t row = page_row(ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + (pos >> a.c.page_shift)), a.c.n_pages, a.c.hkv, h, page_tokens);
-    return row < 0 ? 0u : weight_key(ld_f32(a.c.weight + (int64_t)row + (pos & (page_tokens - 1))));
+  // fours of positions, and this block's share of them
+  const int q_begin = a.n_sink >> 2, q_all = ((end + 3) >> 2) - q_begin, per = (q_all + blocks - 1) / blocks;
+  const int from = q_begin + min(q_all, rank * per), n = q_begin + min(q_all, rank * per + per) - from;
+  auto page_of = [&](int i) { return ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + (((from + i) * 4) >> a.c.page_shift)); };
+  auto keys_of = [&](int i, int32_t page) {
+    const int pos = (from + i) * 4;
+    const int32_t row = page_row(page, a.c.n_pages, a.c.hkv, h, page_tokens);
+    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row >= 0) {
+      const uint4 x = ld_v4(a.c.weight + (int64_t)row + (pos & (page_tokens - 1)));
+      w = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
+    }
+    auto key = [&](float x, int p) { return p < a.n_sink || p >= end ? 0u : row < 0 ? 1u : weight_key(x); };
+    return make_uint4(key(w.x, pos), key(w.y, pos + 1), key(w.z, pos + 2), key(w.w, pos + 3));
   };
-  const bool in_smem = n <= SELECT_KEYS;
+  const bool in_smem = 4 * n <= SELECT_KEYS;
   if (in_smem) {
-    constexpr int U = 4;                              // page entries, then weights, in flight per thread
+    constexpr int U = 4;                              // places in the page table in flight per thread
     for (int i0 = tid; i0 < n; i0 += U * SELECT_THREADS) {
-      int32_t row[U];
-      float w[U];
+      int32_t page[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * SELECT_THREADS;
-        row[u] = i < n ? ld_i32(a.s.page_table + (int64_t)b * a.s.table_width + ((from + i) >> a.c.page_shift)) : -1;
-      }
+      for (int u = 0; u < U; ++u) page[u] = i0 + u * SELECT_THREADS < n ? page_of(i0 + u * SELECT_THREADS) : -1;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int pos = from + i0 + u * SELECT_THREADS;
-        row[u] = page_row(row[u], a.c.n_pages, a.c.hkv, h, page_tokens);
-        w[u] = row[u] < 0 ? __int_as_float(0x7fffffff) : ld_f32(a.c.weight + (int64_t)row[u] + (pos & (page_tokens - 1)));
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * SELECT_THREADS;
-        if (i < n) keys[i] = weight_key(w[u]);
-      }
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * SELECT_THREADS < n) keys[i0 + u * SELECT_THREADS] = keys_of(i0 + u * SELECT_THREADS, page[u]);
     }
   }
+  auto four = [&](int i) { return in_smem ? keys[i] : keys_of(i, page_of(i)); };
   uint32_t prefix = 0, wanted = (uint32_t)a.n_heavy;
   for (int pass = 0; pass < 3; ++pass) {              // 11, 11 and 10 bits
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
@@ -1346,8 +1368,14 @@ __global__ void __launch_bounds__(SELECT_THREADS, 2) cache_select_kernel(const _
     for (int i = tid; i < SELECT_BINS; i += SELECT_THREADS) mine[i] = 0;
     __syncthreads();
     for (int i = tid; i < n; i += SELECT_THREADS) {
-      const uint32_t k = in_smem ? keys[i] : key_at(i);
-      if (pass == 0 || k >> (shift + bits) == prefix) atomicAdd(&mine[(k >> shift) & mask], 1u);
+      const uint4 k = four(i);
+      auto count = [&](uint32_t x) {
+        if (x != 0u && (pass == 0 || x >> (shift + bits) == prefix)) atomicAdd(&mine[(x >> shift) & mask], 1u);
+      };
+      count(k.x);
+      count(k.y);
+      count(k.z);
+      count(k.w);
     }
     if (blocks > 1) cluster.sync();
     else __syncthreads();
@@ -1392,11 +1420,13 @@ __global__ void __launch_bounds__(SELECT_THREADS, 2) cache_select_kernel(const _
   // prefix is the smallest kept key, `wanted` of its equals are kept: the first ones
   // every warp takes a run of the keys, so that only its first place needs the others
   const int run = (n + SELECT_THREADS - 1) / SELECT_THREADS * 32, w0 = min(n, warp * run), w1 = min(n, w0 + run);
+  auto above_in = [&](const uint4& k) { return (uint32_t)(k.x > prefix) + (k.y > prefix) + (k.z > prefix) + (k.w > prefix); };
+  auto equal_in = [&](const uint4& k) { return (uint32_t)(k.x == prefix) + (k.y == prefix) + (k.z == prefix) + (k.w == prefix); };
   uint32_t above_n = 0, equal_n = 0;
   for (int i = w0 + lane; i < w1; i += 32) {
-    const uint32_t k = in_smem ? keys[i] : key_at(i);
-    above_n += k > prefix;
-    equal_n += k == prefix;
+    const uint4 k = four(i);
+    above_n += above_in(k);
+    equal_n += equal_in(k);
   }
   above_n = __reduce_add_sync(0xffffffffu, above_n);
   equal_n = __reduce_add_sync(0xffffffffu, equal_n);
@@ -1425,13 +1455,29 @@ __global__ void __launch_bounds__(SELECT_THREADS, 2) cache_select_kernel(const _
   e_base = __reduce_add_sync(0xffffffffu, e_base);
   for (int i0 = w0; i0 < w1; i0 += 32) {
     const int i = i0 + lane;
-    const uint32_t k = i < w1 ? (in_smem ? keys[i] : key_at(i)) : 0u;
-    const bool above = i < w1 && k > prefix, equal = i < w1 && k == prefix;
-    const uint32_t am = __ballot_sync(0xffffffffu, above), em = __ballot_sync(0xffffffffu, equal), below = (1u << lane) - 1u;
-    const uint32_t a_before = a_base + __popc(am & below), e_before = e_base + __popc(em & below);
-    if (above || (equal && e_before < wanted)) kept[a.n_sink + a_before + min(e_before, wanted)] = from + i;
-    a_base += __popc(am);
-    e_base += __popc(em);
+    const uint4 k = i < w1 ? four(i) : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t upto = above_in(k) | equal_in(k) << 16;  // at most 128 of each in a trip
+    const uint32_t own = upto;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    uint32_t a_before = a_base + ((upto - own) & 0xffffu), e_before = e_base + ((upto - own) >> 16);
+    auto put = [&](uint32_t x, int pos) {
+      const bool above = x > prefix, equal = x == prefix;
+      if (above || (equal && e_before < wanted)) kept[a.n_sink + a_before + min(e_before, wanted)] = pos;
+      a_before += above;
+      e_before += equal;
+    };
+    const int pos = (from + i) * 4;
+    put(k.x, pos);
+    put(k.y, pos + 1);
+    put(k.z, pos + 2);
+    put(k.w, pos + 3);
+    const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
+    a_base += total & 0xffffu;
+    e_base += total >> 16;
   }
   cluster.sync();                                     // no block leaves while another reads its shares
 }
@@ -1503,29 +1549,23 @@ __global__ void __launch_bounds__(MOVE_THREADS) cache_move_kernel(const __grid_c
     if (s % 16 == 0) top[which][s / 16] = m;
   }
   __syncthreads();
-  const int pieces = page_tokens / 16;
-  auto page_top = [&](int which, int s) {
+  {
+    // what a token's codes are multiplied by: 256 threads, the keys' and the values' of 128 tokens
+    const int which = tid / MOVE_TOKENS, s = tid % MOVE_TOKENS, pieces = page_tokens / 16, p = (s / 16) & ~(pieces - 1);
     float m = 0.f;
-    const int p = s / 16 / pieces * pieces;
     for (int i = 0; i < pieces; ++i) m = fmaxf(m, top[which][p + i]);
-    return m;
-  };
-  if (tid < MOVE_TOKENS && tid % page_tokens == 0 && dst >= 0) {
-    a.c.k_scale[dst_page * a.c.hkv + h] = page_top(0, tid);
-    a.c.v_scale[dst_page * a.c.hkv + h] = page_top(1, tid);
+    if (dst_row[s] >= 0) {
+      if ((s & (page_tokens - 1)) == 0) (which ? a.c.v_scale : a.c.k_scale)[(dst_row[s] >> a.c.page_shift)] = m;
+      src_scale[which][s] = __fdiv_rn(src_scale[which][s], m);
+    }
   }
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int e = i * MOVE_THREADS + tid, which = e / (MOVE_TOKENS * C), s = e / C % MOVE_TOKENS, c = e % C;
     if (dst_row[s] < 0) continue;
-    const float from = src_scale[which][s], to = page_top(which, s);
-    if (from == 0.f) {
-      x[i] = make_uint4(0, 0, 0, 0);
-    } else if (from != to) {
-      const float ratio = __fdiv_rn(from, to);
-      x[i] = make_uint4(rescale_codes<KIND>(x[i].x, ratio), rescale_codes<KIND>(x[i].y, ratio), rescale_codes<KIND>(x[i].z, ratio), rescale_codes<KIND>(x[i].w, ratio));
-    }
-    *reinterpret_cast<uint4*>((which ? a.c.v : a.c.k) + (int64_t)dst_row[s] * D + c * 16) = x[i];
+    const float ratio = src_scale[which][s];
+    *reinterpret_cast<uint4*>((which ? a.c.v : a.c.k) + (int64_t)dst_row[s] * D + c * 16) = ratio == 0.f ? make_uint4(0, 0, 0, 0) : moved_codes<KIND>(x[i], ratio);
   }
 }
 
