@@ -440,7 +440,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
   else FCP_CUDA_CHECK(launch(cache_merge_kernel<64>, grid, MERGE_THREADS, 0, st, a, tile.rows()));
   a.s = all;
   if (accumulate)
-    FCP_CUDA_CHECK(launch(attn_kernel(c, kWeights), grid, CT_THREADS, attn_smem(c, kWeights), st, cache->k_map, cache->v_map, a));
+    FCP_CUDA_CHECK(launch(attn_kernel(c, kWeights), WEIGHT_CTAS * grid, CT_THREADS, attn_smem(c, kWeights), st, cache->k_map, cache->v_map, a));
   return FCP_OK;
 }
 

@@ -290,6 +290,7 @@ constexpr int CT_KEYS = 128;                          // keys of a tile
 constexpr int CT_STEP = 32;                           // keys that a warp takes at a time
 constexpr int CT_WARPS = 8;                           // consumer warps; two more load keys and values
 constexpr int CT_THREADS = (CT_WARPS + 2) * 32;
+constexpr int WEIGHT_CTAS = 2;                        // per SM, of the kernel that adds up weights
 
 struct AttnArgs {
   CacheView c;
@@ -321,7 +322,7 @@ struct AttnSmem {
   static constexpr int BLOCKS = NR * (WR ? WR : 1), ROWS = 8 * BLOCKS;
   static constexpr int TILE = CT_KEYS * D;            // bytes of K or of V
   static constexpr int STAGE = WR ? 2 * TILE : TILE;
-  static constexpr int STAGES = D == 64 || WR == 0 ? 8 : WR == 8 ? 3 : NR == 2 ? 4 : 5;
+  static constexpr int STAGES = WR == 0 ? 4 : D == 64 ? 8 : WR == 8 ? 3 : NR == 2 ? 4 : 5;
   static constexpr int RING = STAGES * STAGE;
   // the queries of a group travel with its first tile where they are few; else the warps fetch them
   static constexpr int QUERY_BYTES = WR == 1 ? ROWS * D * 2 : 0;
@@ -999,7 +1000,7 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
     float sum[2] = {0.f, 0.f};                        // of keys g and g + 8
 #pragma unroll 1
     for (int r0 = 0; r0 < n_rows; r0 += 8 * NR) {
-      const int blocks = min(NR, (n_rows - r0 + 7) / 8);
+      const int blocks = min(NR, (n_rows - r0 + 7) / 8), least = meta.length - meta.n + r0 / A.group + 1;
       if (n_rows > 8 * NR || (meta.flags & ST_FIRST)) {
         consumer_sync();                              // the rows before have been read
         area.template fill<true>(A, meta, r0, (blocks + 3) / 4 * 4, nullptr, warp, lane);
@@ -1037,10 +1038,16 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
         for (int i = 0; i < 4; ++i) {
           if (i0 + i >= blocks) break;
           const RowInfo rows[2] = {area.row[8 * (i0 + i) + 2 * t], area.row[8 * (i0 + i) + 2 * t + 1]};
+          const float f[2] = {rows[0].factor * about.x, rows[1].factor * about.x};
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (key + g + 8 * (c >> 1) < rows[c & 1].limit)
-              sum[c >> 1] += exp2_approx(fmaf(s[i][c], rows[c & 1].factor * about.x, -rows[c & 1].lse2));
+          for (int c = 0; c < 4; ++c) s[i][c] = fmaf(s[i][c], f[c & 1], -rows[c & 1].lse2);
+          if (key + 16 > least) {                     // some row may not see some key
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (key + g + 8 * (c >> 1) >= rows[c & 1].limit) s[i][c] = -INFINITY;
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) sum[c >> 1] += exp2_approx(s[i][c]);
         }
       }
     }
@@ -1064,7 +1071,7 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
 
 // WR = 0: the weights, of NR blocks of rows at a time.
 template <int D, int KIND, int NR, int WR>
-__global__ void __launch_bounds__(CT_THREADS, 1)
+__global__ void __launch_bounds__(CT_THREADS, WR == 0 ? WEIGHT_CTAS : 1)
 cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ AttnArgs A) {
   using S = AttnSmem<D, NR, WR>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -1122,17 +1129,34 @@ __global__ void __launch_bounds__(MERGE_THREADS) cache_merge_kernel(const __grid
   auto part = [&](int i) { return i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i); };
   for (int e = threadIdx.x; e < n_rows * (D / 4); e += MERGE_THREADS) {
     const int r = e / (D / 4), f = e % (D / 4);
-    float top = -INFINITY;
-    for (int i = 0; i <= count; ++i) top = fmaxf(top, ld_f32(A.part_lse + (int64_t)part(i) * rows_per_tile + r));
-    const float ref = top == -INFINITY ? 0.f : top;
-    float z = 0.f;
+    float ref = -3e38f, z = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i <= count; ++i) {
-      const int64_t at = (int64_t)part(i) * rows_per_tile + r;
-      const float w = exp2_approx(ld_f32(A.part_lse + at) - ref);
-      const float4 y = ld_stream_f4(A.part_o + at * D + f * 4);
-      z += w;
-      x.x = fmaf(y.x, w, x.x); x.y = fmaf(y.y, w, x.y); x.z = fmaf(y.z, w, x.z); x.w = fmaf(y.w, w, x.w);
+    constexpr int U = 4;                              // partial results in flight
+    for (int i0 = 0; i0 <= count; i0 += U) {
+      float l[U], top = ref;
+      float4 y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = (int64_t)part(min(i0 + u, count)) * rows_per_tile + r;
+        l[u] = ld_f32(A.part_lse + at);
+        y[u] = ld_stream_f4(A.part_o + at * D + f * 4);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i0 + u > count) l[u] = -INFINITY;
+        top = fmaxf(top, l[u]);
+      }
+      const float shrink = exp2_approx(ref - top);
+      ref = top;
+      z *= shrink;
+      x.x *= shrink; x.y *= shrink; x.z *= shrink; x.w *= shrink;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float w = exp2_approx(l[u] - ref);
+        if (i0 + u > count) continue;                 // a repeated one, whose values may be NaN
+        z += w;
+        x.x = fmaf(y[u].x, w, x.x); x.y = fmaf(y[u].y, w, x.y); x.z = fmaf(y[u].z, w, x.z); x.w = fmaf(y[u].w, w, x.w);
+      }
     }
     const float inverse = z == 0.f ? 0.f : 1.f / z;
     const int gr = first + r, j = gr / A.group;

@@ -74,7 +74,8 @@ namespace {
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_TOKENS = 16;          // most tokens of one block
-constexpr int ROPE_SLOTS = 1280;         // slots of a block, where it may choose: 5 per thread
+constexpr int ROPE_SLOTS = 1280;         // most slots of a block: 5 per thread
+constexpr int ROPE_RESIDENT = 8;         // blocks of an SM
 
 struct RopeArgs {
   const __nv_bfloat16 *q, *k;
@@ -106,7 +107,7 @@ __device__ __forceinline__ float2 unpack(uint32_t w) {
 // WIDE: rotary_dim is a multiple of 16 and everything 16-byte aligned; a slot is 8 pairs in two 16-byte pieces (or 16 copied
 // columns).  Otherwise a slot is one pair, moved as two values.
 template <bool WIDE, int LAYOUT>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(ROPE_THREADS, ROPE_RESIDENT) rope_kernel(const __grid_constant__ RopeArgs a) {
   __shared__ __align__(16) float2 cs[ROPE_TOKENS * 64];
   __shared__ int64_t pos[ROPE_TOKENS];
   __shared__ int32_t ok[ROPE_TOKENS];
@@ -138,23 +139,19 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   // columns of a wide slot's two pieces
   const bool half = LAYOUT == FCP_ROPE_HALF && s < turned;
   const int cx = half ? s * 8 : s * 16, cy = half ? pairs + s * 8 : s * 16 + 8;
-  constexpr int U = 2;                               // wide slots in flight per thread
-  uint4 x[U], y[U];
-  __nv_bfloat16* dst[U];
-  int at[U];                                         // token; -1: none
+  uint4 x, y;
+  __nv_bfloat16* dst;
+  int at;                                            // token of the slot that was fetched; -1: none
   auto fetch = [&] {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      at[u] = -1;
-      if (t < n) {
-        const __nv_bfloat16* src;
-        row(src, dst[u]);
-        at[u] = t;
-        x[u] = ld_v4(src + cx);
-        y[u] = ld_v4(src + cy);
-        h += stride;
-        settle();
-      }
+    at = -1;
+    if (t < n) {
+      const __nv_bfloat16* src;
+      row(src, dst);
+      at = t;
+      x = ld_v4(src + cx);
+      y = ld_v4(src + cy);
+      h += stride;
+      settle();
     }
   };
   if (WIDE) fetch();                                 // the first values travel while positions and angles are found
@@ -193,38 +190,31 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   }
   __syncthreads();
   if (WIDE) {
-    while (at[0] >= 0) {
+    for (; at >= 0; fetch()) {
+      if (!ok[at]) continue;
+      if (s < turned) {
+        uint32_t wx[4] = {x.x, x.y, x.z, x.w}, wy[4] = {y.x, y.y, y.z, y.w};
+        const float4* c4 = reinterpret_cast<const float4*>(cs + at * 64 + s * 8);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (at[u] < 0 || !ok[at[u]]) continue;
-        if (s < turned) {
-          uint32_t wx[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, wy[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
-          const float4* c4 = reinterpret_cast<const float4*>(cs + at[u] * 64 + s * 8);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (LAYOUT == FCP_ROPE_HALF) {           // words j of both pieces: pairs 2j, 2j + 1
-              const float4 c = c4[j];
-              float2 u2 = unpack(wx[j]), v2 = unpack(wy[j]);
-              turn_pair(u2.x, v2.x, make_float2(c.x, c.y));
-              turn_pair(u2.y, v2.y, make_float2(c.z, c.w));
-              wx[j] = pack_bf16(u2.x, u2.y);
-              wy[j] = pack_bf16(v2.x, v2.y);
-            } else {                                 // word j of a piece is a pair
-              const float4 c = c4[j >> 1], d = c4[2 + (j >> 1)];
-              float2 u2 = unpack(wx[j]), v2 = unpack(wy[j]);
-              turn_pair(u2.x, u2.y, j & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y));
-              turn_pair(v2.x, v2.y, j & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y));
-              wx[j] = pack_bf16(u2.x, u2.y);
-              wy[j] = pack_bf16(v2.x, v2.y);
-            }
+        for (int j = 0; j < 4; ++j) {
+          float2 u = unpack(wx[j]), v = unpack(wy[j]);
+          if (LAYOUT == FCP_ROPE_HALF) {             // words j of both pieces: pairs 2j, 2j + 1
+            const float4 c = c4[j];
+            turn_pair(u.x, v.x, make_float2(c.x, c.y));
+            turn_pair(u.y, v.y, make_float2(c.z, c.w));
+          } else {                                   // word j of a piece is a pair
+            const float4 c = c4[j >> 1], d = c4[2 + (j >> 1)];
+            turn_pair(u.x, u.y, j & 1 ? make_float2(c.z, c.w) : make_float2(c.x, c.y));
+            turn_pair(v.x, v.y, j & 1 ? make_float2(d.z, d.w) : make_float2(d.x, d.y));
           }
-          x[u] = make_uint4(wx[0], wx[1], wx[2], wx[3]);
-          y[u] = make_uint4(wy[0], wy[1], wy[2], wy[3]);
+          wx[j] = pack_bf16(u.x, u.y);
+          wy[j] = pack_bf16(v.x, v.y);
         }
-        *reinterpret_cast<uint4*>(dst[u] + cx) = x[u];
-        *reinterpret_cast<uint4*>(dst[u] + cy) = y[u];
+        x = make_uint4(wx[0], wx[1], wx[2], wx[3]);
+        y = make_uint4(wy[0], wy[1], wy[2], wy[3]);
       }
-      fetch();
+      *reinterpret_cast<uint4*>(dst + cx) = x;
+      *reinterpret_cast<uint4*>(dst + cy) = y;
     }
   } else {
     const int c0 = LAYOUT == FCP_ROPE_HALF && s < pairs ? s : 2 * s, c1 = LAYOUT == FCP_ROPE_HALF && s < pairs ? s + pairs : 2 * s + 1;
@@ -294,10 +284,11 @@ int rope(const char* call, float sign, const fcp_rope_table* table, int64_t T, c
   const uintptr_t bases = (uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out;
   const int64_t strides = a.q_stride | a.k_stride | a.q_out_stride | a.k_out_stride;
   const bool wide = a.rotary % 16 == 0 && (bases & 15) == 0 && strides % 8 == 0;
-  // As many tokens per block as make ROPE_SLOTS slots, because finding the sequence and the angles costs a thread as much as three
-  // slots; fewer where SMs would be left without a block.
-  const int per_token = (hq + hkv) * (wide ? a.D / 16 : a.D / 2);
-  a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({ROPE_TOKENS, ROPE_SLOTS / per_token, T / (2 * FCP_PLAN_SMS)}));
+  // As many tokens per block as let all blocks run at once, up to ROPE_SLOTS slots: finding the sequence and the angles costs a
+  // thread as much as three slots.  16K tokens of 12/4 heads of 64: 14 tokens 15.4 us, 10 16.4, 16 (1.4 rounds) 17.1; 4000: 4
+  // tokens 6.4, 13 9.2; 64K tokens of 32/8 heads of 128: 4 tokens 211, 1 token 284.
+  const int64_t per_token = (hq + hkv) * (wide ? a.D / 16 : a.D / 2), at_once = ROPE_RESIDENT * FCP_PLAN_SMS;
+  a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({ROPE_TOKENS, ROPE_SLOTS / per_token, (T + at_once - 1) / at_once}));
   const unsigned grid = (unsigned)((T + a.tokens - 1) / a.tokens);
   cudaStream_t st = (cudaStream_t)stream;
   const bool half = table->layout == FCP_ROPE_HALF;

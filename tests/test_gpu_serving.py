@@ -459,10 +459,12 @@ def test_many_sequences():
 
 def test_rows_that_see_nothing():
     w = World(25, "e4m3", 16, 2, 64, [0, 3, 0]).fill().up()
-    q, o, lse, rows = attend(w, [2, 5, 1], 4)                     # more new rows than tokens: the first ones are no tokens
+    q, o, lse, rows = attend(w, [2, 5, 1], 4, accumulate=True)    # more new rows than tokens: the first ones are no tokens
     r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
     assert np.isneginf(r["lse"]).sum() == 4 * 5
     check_attn(w, None, r, o, lse, rows)
+    added = f64(w.w) - w.weight
+    assert np.isfinite(added).all() and math.isclose(added.sum(), 4 * 3, rel_tol=1e-5)
 
 
 @pytest.mark.parametrize("new", [1, 6, 40])
