@@ -177,17 +177,24 @@ int ready(const char* call, const fcp_cache* cache) {
   return FCP_OK;
 }
 
-// Whether a call goes through bf16 copies and tcgen05: chunks of a tile of new tokens and more, while the copies stay below
-// half of the device's memory or so.  TODO
-constexpr int kChunkTokens = 128;
-constexpr int64_t kChunkBytes = int64_t(64) << 30;
 int64_t chunk_stride(const fcp_cache_config& c, const fcp_cache_batch& b) {
   return ((int64_t)b.table_width * c.page_tokens + CT_KEYS - 1) / CT_KEYS * CT_KEYS;
 }
+// Whether a call goes through bf16 copies and tcgen05: where that takes less time by what both were measured to take, in clk of
+// the device per tile of 128 keys.  cache_attn_kernel: 11500 per KV head and 128 rows, spread over all SMs.  The other way: 5900 per KV head for the
+// copies; fcp_fwd_kernel takes 1700 per query head and tile of 128 new tokens, 1270 where two run beside each other, and no item is
+// cut along the keys.  4 sequences of 6K to 12K tokens, 32/8 heads, us, copies against not: 512 new tokens 290, 1400; 256 231, 770;
+// 128 185, 399; one sequence, 128 162, 170; 8/8 heads, 4 x 128 182, 128.  The copies may take up to 8 GB.
+constexpr int64_t kChunkBytes = int64_t(8) << 30;
 bool in_chunks(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq) {
   const int64_t tokens = b.B * chunk_stride(c, b), units = (int64_t)b.B * ((b.max_new + FCP_FWD_UNIT_ROWS - 1) / FCP_FWD_UNIT_ROWS);
-  return b.max_new >= kChunkTokens && b.B <= 65535 && tokens < (int64_t(1) << 31) - CT_KEYS && tokens * c.hkv * c.head_dim * 4 <= kChunkBytes &&
-         2 * units * hq < int64_t(1) << 31;
+  if (b.B < 1 || b.max_new < 2 || b.B > 65535 || tokens >= (int64_t(1) << 31) - CT_KEYS || tokens * c.hkv * c.head_dim * 4 > kChunkBytes ||
+      2 * units * hq >= int64_t(1) << 31)
+    return false;
+  const int64_t rows = ((int64_t)b.max_new * (hq / c.hkv) + 127) / 128, items = b.B * ((b.max_new + 127) / 128) * (int64_t)hq;
+  const int64_t direct = b.B * (int64_t)c.hkv * rows * 11500 / FCP_PLAN_SMS;
+  const int64_t copied = std::max<int64_t>(1700, items * 1270 / FCP_PLAN_SMS) + b.B * (int64_t)c.hkv * 5900 / FCP_PLAN_SMS;
+  return copied < direct;
 }
 
 // Workspace of fcp_cache_attn: partial outputs and log-sum-exps of two groups per CTA, and what each CTA shares; for chunks also

@@ -1262,16 +1262,38 @@ __global__ void __launch_bounds__(UNPACK_THREADS) cache_unpack_kernel(const __gr
   if (careful) a.careful[b] = 1;
 }
 
-// The work units of fcp_fwd_kernel (pairs of tiles of 128 new tokens), the one work group, the row limits.
+// The work units of fcp_fwd_kernel (pairs of tiles of 128 new tokens), the one work group, the row limits.  The units go by their
+// number of key tiles, most first, so that the last ones to be handed out are short; up to CHUNK_SORT units, because every unit
+// looks at every other.
 constexpr int CHUNK_THREADS = 256;
+constexpr int CHUNK_SORT = 8192;
 __global__ void __launch_bounds__(CHUNK_THREADS) cache_chunk_kernel(const __grid_constant__ ChunkArgs a) {
+  __shared__ int32_t place;
   grid_begin();
-  const int b = blockIdx.y, u = blockIdx.x, tid = threadIdx.x;
+  const int b = blockIdx.y, u = blockIdx.x, tid = threadIdx.x, n_units = (int)(gridDim.x * gridDim.y), self = b * (int)gridDim.x + u;
   const SeqView s = load_seq(a.s, b);
   const bool serves = ld_i32(a.careful + b) == 0;
   const int first = u * FCP_FWD_UNIT_ROWS, n = serves ? max(0, min(FCP_FWD_UNIT_ROWS, s.n - first)) : 0;
   const int seen = s.length - s.n + first + 1;        // keys that the unit's first row sees
   if (tid < n) a.row_limit[s.row0 + first + tid] = b * a.stride + seen + tid;
+  if (tid == 0) place = 0;
+  __syncthreads();
+  if (n_units <= CHUNK_SORT) {
+    const int mine = n > 0 ? (seen + n - 1 + FCP_TILE - 1) / FCP_TILE : 0;
+    int before = 0;
+    for (int i = tid; i < n_units; i += CHUNK_THREADS) {
+      const int bi = i / (int)gridDim.x, fi = (i - bi * (int)gridDim.x) * FCP_FWD_UNIT_ROWS;
+      const SeqView x = load_seq(a.s, bi);
+      const int ni = ld_i32(a.careful + bi) == 0 ? max(0, min(FCP_FWD_UNIT_ROWS, x.n - fi)) : 0;
+      const int other = ni > 0 ? (x.length - x.n + fi + ni + FCP_TILE - 1) / FCP_TILE : 0;
+      before += other > mine || (other == mine && i < self);
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    if ((tid & 31) == 0) atomicAdd(&place, before);
+  } else if (tid == 0) {
+    place = self;
+  }
+  __syncthreads();
   if (tid < FCP_FWD_UNIT_W) {
     auto tiles = [&](int rows) { return (seen + rows - 1 + FCP_TILE - 1) / FCP_TILE; };        // of keys, for the first `rows` rows
     int x = 0;
@@ -1287,7 +1309,7 @@ __global__ void __launch_bounds__(CHUNK_THREADS) cache_chunk_kernel(const __grid
       case FU_NT_RANGE0: x = 0x7fffffff; break;       // no second range
       case FU_SINGLE_SLOT: x = 1; break;
     }
-    a.units[((int64_t)b * a.units_per_seq + u) * FCP_FWD_UNIT_W + tid] = x;
+    a.units[(int64_t)place * FCP_FWD_UNIT_W + tid] = x;
   }
   if (b == 0 && u == 0 && tid == 0) {
     *a.counter = 0;

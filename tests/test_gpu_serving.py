@@ -276,9 +276,16 @@ def test_append_scales_that_are_no_powers_of_two():
         assert np.abs(now[n] - state[n]).max() <= 1 and (now[n] != state[n]).mean() < 1e-3
 
 
+def goes_by_copies(w, new, hq):
+    """Whether a call with these new tokens asks for room for bf16 copies of all keys and values, besides the partial results."""
+    rows = max(new) * hq // w.hkv
+    tile = next((t for t in (8, 16, 32, 64) if rows <= t), 128)
+    partial, copies = 2 * 148 * tile * (w.d + 1) * 4, len(new) * w.width * w.page * w.hkv * w.d * 4
+    return fcp.fcp_cache_attn_workspace_bytes(w.cache, w.batch(new), hq) >= partial + copies
+
+
 def check_attn(w, state, r, o, lse, rows, weight=HALF):
-    """Against the definition: the rounding of the weights (to halves 2^-11; in chunks of 128 new tokens and more to bf16, 2^-8), of o
-    to bf16 (2^-8), and the fp32 sums of the scores (D products of size at most `size` in all, each sum truncated at 2^-23)."""
+    """Against the definition: the rounding of the weights (to halves 2^-11; in calls that go by copies to bf16, 2^-8), of o to bf16 (2^-8), and the fp32 sums of the scores (D products of size at most `size` in all, each sum truncated at 2^-23)."""
     off = w.off
     for name, x in (("o", o), ("lse", lse)):
         assert x.shape[0] >= rows
@@ -319,7 +326,7 @@ def test_attention_over_the_cache(kind, page, hkv, d, group, new, before):
     w = World(21, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
     q, o, lse, rows = attend(w, new, hkv * group, stride_heads=1)
     r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
-    check_attn(w, None, r, o, lse, rows)
+    check_attn(w, None, r, o, lse, rows, weight=BF16 if goes_by_copies(w, new, hkv * group) else HALF)
     assert w.cache.device_status().tolist() == [0, 0, 0, 0]
 
 
@@ -361,10 +368,11 @@ def test_long_ragged_batch_is_split_and_joined():
     assert torch.equal(o1, o2) and torch.equal(lse1, lse2) and not torch.equal(o1, a)
 
 
-@pytest.mark.parametrize("kind,page,hkv,d", CASES)
-@pytest.mark.parametrize("group,new,before", [(1, [128], [0]), (2, [129, 0, 1], [70, 300, 5]), (3, [300, 40, 257], [129, 0, 700])])
-def test_attention_of_long_chunks(kind, page, hkv, d, group, new, before):
+@pytest.mark.parametrize("kind,page,d", [("e4m3", 16, 64), ("int8", 16, 128), ("e4m3", 32, 128), ("int8", 64, 64), ("e4m3", 128, 128), ("int8", 128, 128)])
+@pytest.mark.parametrize("hkv,group,new,before", [(4, 8, [128], [0]), (4, 8, [129, 0, 1], [70, 300, 5]), (8, 3, [300, 40, 257], [129, 0, 700])])
+def test_attention_of_long_chunks(kind, page, d, hkv, group, new, before):
     w = World(71, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    assert goes_by_copies(w, new, hkv * group)
     q, o, lse, rows = attend(w, new, hkv * group, stride_heads=1, accumulate=True)
     r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
     check_attn(w, None, r, o, lse, rows, weight=BF16)
@@ -377,14 +385,24 @@ def test_attention_of_long_chunks(kind, page, hkv, d, group, new, before):
     assert torch.equal(o1, o2) and torch.equal(lse1, lse2)
 
 
+def test_many_rows_without_copies():
+    """More rows than a tile per KV head, few enough in all that no copies are made."""
+    w = World(74, "e4m3", 32, 1, 128, [700]).fill().up()
+    assert not goes_by_copies(w, [200], 2)
+    q, o, lse, rows = attend(w, [200], 2, accumulate=True)
+    r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
+    check_attn(w, None, r, o, lse, rows)
+
+
 def test_chunk_of_a_wide_table_is_captured_and_replayed():
     """Lengths of a captured chunk change; the table is far wider than the sequences."""
-    w = World(72, "e4m3", 32, 2, 64, [500, 400], width=64).fill().up()
-    hq, rows = 4, 300
+    w = World(72, "e4m3", 32, 4, 64, [500, 400], width=64).fill().up()
+    hq, rows = 16, 300
     length, off = dev([0, 0]), dev([0, 0, 0])
     q = torch.zeros(rows, hq, 64, dtype=torch.bfloat16, device="cuda")
     o, lse = torch.zeros_like(q), torch.zeros(rows, hq, device="cuda")
     batch = fcp.CacheBatch(dev(w.table), length, off, rows=rows, max_new=260)
+    assert goes_by_copies(w, [260, 40], hq)
     n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, hq)
     ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
     step = lambda: fcp.fcp_cache_attn(w.cache, batch, q, o, lse, ws, n, stream=stream())
@@ -411,28 +429,29 @@ def test_chunk_of_a_wide_table_is_captured_and_replayed():
 def test_chunks_with_sequences_that_need_care(kind):
     """In one call with ordinary sequences: a NaN among the new values, more rows than tokens, a page that does not exist, lengths
     that make no sense."""
-    new = [140, 150, 133, 20, 200]
-    w = World(73, kind, 16, 1, 64, [300, 90, 200, 100, 260]).fill()
-    place = lambda b, p: (w.table[b][p // 16], 0, p % 16)
+    new, hkv, group = [140, 150, 133, 20, 200], 4, 2
+    w = World(73, kind, 16, hkv, 64, [300, 90, 200, 100, 260]).fill()
     if kind == "e4m3":
-        w.codes["v"][place(0, 290)][7] = 0xff
+        w.codes["v"][w.table[0][290 // 16], 1, 290 % 16, 7] = 0xff
     good = w.state()
     table = w.table.copy()
     w.table[2, 1] = w.n_pages + 5
     w.up()
+    assert goes_by_copies(w, new, hkv * group)
     w.length[4] = 10 ** 6
-    q, o, lse, rows = attend(w, new, 2, spare=0)
+    q, o, lse, rows = attend(w, new, hkv * group, spare=0)
     w.length[4] = 260
     off = w.off
-    r = R.attention(good, table, w.length, off, f64(q)[:rows])
+    with np.errstate(invalid="ignore"):
+        r = R.attention(good, table, w.length, off, f64(q)[:rows])
     got, got_lse = f64(o), f64(lse)
     st = w.cache.device_status().tolist()
     assert st[0] == fcp.FCP_ERR_INVALID_ARG and st[1:3] in ([fcp.FCP_CACHE_BAD_LENGTH, 4], [fcp.FCP_CACHE_BAD_PAGE, 2])
     assert np.all(got[off[4]:] == 3) and np.all(got_lse[off[4]:] == 5)
     # sequence 2 without its tokens 16..31
-    k = R.gather(good, "k", np.asarray(table[2][:13], dtype=np.int64), 200, 0)
     for j in (0, 70, 132):
-        for head in range(2):
+        for head in range(hkv * group):
+            k = R.gather(good, "k", np.asarray(table[2][:13], dtype=np.int64), 200, head // group)
             seen = [p for p in range(200 - 133 + j + 1) if not 16 <= p < 32]
             s = k[seen] @ f64(q)[off[2] + j, head] / 8
             assert abs(got_lse[off[2] + j, head] - np.log(np.exp(s).sum())) < 1e-3
