@@ -417,8 +417,9 @@ int fcp_rope_bwd(const fcp_rope_table* table, int64_t T, const void* dq, int64_t
  * outside [0, n_pages) or, in fcp_cache_attn and fcp_cache_evict, on a page whose scale is not in
  * [FCP_CACHE_MIN_SCALE, FCP_CACHE_MAX_SCALE], count as absent.  status then holds FCP_ERR_INVALID_ARG, one of the
  * FCP_CACHE_BAD_* codes and the sequence (first failure, sticky); FCP_ERR_TIMEOUT as everywhere.
- * The calls write nothing but what is listed, wherever pages and offsets point inside their buffers.
- * Two calls on one cache must be stream-ordered if one of them writes what the other uses.
+ * The calls write nothing but what is listed, whatever the tables hold.
+ * Two calls on one cache must be stream-ordered if one of them writes what the other uses.  The device that holds the cache must be
+ * the current one.  The first compute call of a handle looks up the device and sets the kernels up; make it outside any capture.
  */
 #define FCP_CACHE_E4M3 0
 #define FCP_CACHE_INT8 1
@@ -473,10 +474,12 @@ int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const
  * q bf16 [rows][hq][D] with q_stride, o bf16 [rows][hq][D], lse fp32 [rows][hq]; hq % hkv == 0; scale <= 0 means
  * 1/sqrt(D).  A row that sees nothing gets o = 0 and lse = -infinity.  Pages may be shared by sequences.
  * accumulate != 0: weight of every cached token += its attention weight, summed over the sequence's new tokens and the
- * query heads of its KV head (what fcp_cache_evict goes by); then no page may appear twice among the call's tokens.
+ * query heads of its KV head (what fcp_cache_evict goes by).
  * workspace: device, 256-byte aligned, of at least fcp_cache_attn_workspace_bytes; its contents need not be initialised; two calls
  * that may overlap on the GPU, also two captured ones, need one each.
- * Results do not depend on the order in which blocks run.
+ * Scores, statistics and sums are fp32; the weights of the values are rounded to halves, and in calls with many new tokens, which go
+ * through bf16 copies of the codes in the workspace (up to 8 GB, where that is faster), to bf16, as is code * scale where a
+ * scale is no power of two.  The same call gives the same bits again, unless sequences of one call share a page and accumulate.
  */
 int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t hq, int64_t* bytes);
 int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const void* q, int64_t q_stride, int32_t hq,

@@ -404,7 +404,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
     return FCP_ERR_INVALID_ARG;
   }
   const int group = hq / c.hkv;
-  if ((int64_t)batch->max_new * group >= int64_t(1) << 31) {
+  if ((int64_t)batch->max_new * group >= int64_t(1) << 30) {
     fcp_set_error("%s: %d new tokens of %d heads each", call, batch->max_new, group);
     return FCP_ERR_INVALID_ARG;
   }

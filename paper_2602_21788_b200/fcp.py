@@ -415,9 +415,10 @@ class Cache:
 
     def __init__(self, k, v, k_scale, v_scale, status, weight=None, kind=None):
         n_pages, hkv, page_tokens, head_dim = k.shape
-        name = str(k.dtype)
         if kind is None:
-            kind = "int8" if name.endswith("int8") and not name.endswith("uint8") else "e4m3"
+            kind = {"torch.float8_e4m3fn": "e4m3", "torch.int8": "int8"}.get(str(k.dtype))
+            if kind is None:
+                raise ValueError(f"pages of {k.dtype}: say which kind of code they hold")
         for x, shape, size in ((k, k.shape, 1), (v, k.shape, 1), (k_scale, (n_pages, hkv), 4), (v_scale, (n_pages, hkv), 4),
                                (weight, (n_pages, hkv, page_tokens), 4), (status, (4,), 4)):
             if x is not None and (tuple(x.shape) != tuple(shape) or x.dtype.itemsize != size or not x.is_contiguous()):

@@ -172,9 +172,10 @@ def test_binding_checks_shapes():
     k, sc, st = z(3, 2, 16, 64, t=torch.int8), z(3, 2), z(4, t=torch.int32)
     cache = fcp.Cache(k, k.clone(), sc, sc.clone(), st)
     for args in [(k, k[:2], sc, sc, st), (k, k, sc[:2], sc, st), (k, k, sc, sc, st[:3]), (k, k, sc.double(), sc, st), (k, k, sc, sc, st, z(3, 2, 32)),
-                 (k.transpose(0, 1), k, sc, sc, st)]:
+                 (k.transpose(0, 1), k, sc, sc, st), (k.view(torch.uint8), k, sc, sc, st), (k.view(torch.float8_e5m2), k, sc, sc, st)]:
         with pytest.raises(ValueError):
             fcp.Cache(*args)
+    assert fcp.Cache(k.view(torch.uint8), k, sc, sc, st, kind="e4m3").handle.value and fcp.Cache(k.view(torch.float8_e4m3fn), k, sc, sc, st).handle.value
     table, length, off = z(2, 3, t=torch.int32), z(2, t=torch.int32), z(3, t=torch.int32)
     batch = fcp.CacheBatch(table, length, off, rows=2)
     for args in [(table, length[:1], off), (table, length, off[:2]), (table.long(), length, off)]:
