@@ -21,16 +21,12 @@ struct fcp_cache {
 
 namespace {
 
-// Row tiles: the smallest that holds a KV head's rows, because a block of 8 rows costs as much whether it is full or not, and
-// warps that stand side by side for more rows all convert the same codes.
-struct RowTile {
-  int blocks, warps;                                  // blocks of 8 rows per warp, warps side by side
-  int rows() const { return 8 * blocks * warps; }
-};
-constexpr RowTile kWeights = {16, 0};
-RowTile row_tile(int64_t rows) {
-  return rows <= 8 ? RowTile{1, 1} : rows <= 16 ? RowTile{2, 1} : rows <= 32 ? RowTile{2, 2} : rows <= 64 ? RowTile{2, 4} : RowTile{2, 8};
-}
+// Row tiles in blocks of 8 rows: the smallest that holds a KV head's rows.  1, 2 and 4 blocks go by cache_attn_kernel, whose time grows
+// with the rows, 16 by cache_tile_kernel, whose time does not.  16 sequences of 4K to 32K tokens, 40/8 heads, int8, us, the one against the
+// other: 15 rows per KV head 115, 250; 25 rows 183, 250; 35 rows (8 blocks) 323, 257; 100 rows (16 blocks) 599, 267.
+constexpr int kWeights = 0;
+int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 ? 4 : TILE_ROWS / 8; }
+
 int box_keys(const fcp_cache_config& c) { return std::min(c.page_tokens, CT_KEYS); }
 
 CacheView view(const fcp_cache_config& c) {
@@ -112,31 +108,22 @@ int cache_map(CUtensorMap* m, const fcp_cache_config& c, void* base) {
 }
 
 typedef void (*AttnKernel)(const CUtensorMap, const CUtensorMap, const AttnArgs);
+constexpr int kWeightBlocks = 16;
 template <int D, int KIND>
-AttnKernel attn_kernel(RowTile t) {
-  switch (t.warps) {
-    case 0: return cache_attn_kernel<D, KIND, kWeights.blocks, 0>;
-    case 1: return t.blocks == 1 ? cache_attn_kernel<D, KIND, 1, 1> : cache_attn_kernel<D, KIND, 2, 1>;
-    case 2: return cache_attn_kernel<D, KIND, 2, 2>;
-    case 4: return cache_attn_kernel<D, KIND, 2, 4>;
-    default: return cache_attn_kernel<D, KIND, 2, 8>;
-  }
+AttnKernel attn_kernel(int blocks) {
+  return blocks == kWeights ? cache_attn_kernel<D, KIND, kWeightBlocks, 0> : blocks == 1 ? cache_attn_kernel<D, KIND, 1, 1>
+         : blocks == 2 ? cache_attn_kernel<D, KIND, 2, 1> : blocks == 4 ? cache_attn_kernel<D, KIND, 2, 2> : cache_tile_kernel<D, KIND>;
 }
-AttnKernel attn_kernel(const fcp_cache_config& c, RowTile t) {
-  if (c.head_dim == 128) return c.kind == FCP_CACHE_E4M3 ? attn_kernel<128, FCP_CACHE_E4M3>(t) : attn_kernel<128, FCP_CACHE_INT8>(t);
-  return c.kind == FCP_CACHE_E4M3 ? attn_kernel<64, FCP_CACHE_E4M3>(t) : attn_kernel<64, FCP_CACHE_INT8>(t);
+AttnKernel attn_kernel(const fcp_cache_config& c, int blocks) {
+  if (c.head_dim == 128) return c.kind == FCP_CACHE_E4M3 ? attn_kernel<128, FCP_CACHE_E4M3>(blocks) : attn_kernel<128, FCP_CACHE_INT8>(blocks);
+  return c.kind == FCP_CACHE_E4M3 ? attn_kernel<64, FCP_CACHE_E4M3>(blocks) : attn_kernel<64, FCP_CACHE_INT8>(blocks);
 }
 template <int D>
-int attn_smem(RowTile t) {
-  switch (t.warps) {
-    case 0: return AttnSmem<D, kWeights.blocks, 0>::DYN_BYTES;
-    case 1: return t.blocks == 1 ? AttnSmem<D, 1, 1>::DYN_BYTES : AttnSmem<D, 2, 1>::DYN_BYTES;
-    case 2: return AttnSmem<D, 2, 2>::DYN_BYTES;
-    case 4: return AttnSmem<D, 2, 4>::DYN_BYTES;
-    default: return AttnSmem<D, 2, 8>::DYN_BYTES;
-  }
+int attn_smem(int blocks) {
+  return blocks == kWeights ? AttnSmem<D, kWeightBlocks, 0>::DYN_BYTES : blocks == 1 ? AttnSmem<D, 1, 1>::DYN_BYTES
+         : blocks == 2 ? AttnSmem<D, 2, 1>::DYN_BYTES : blocks == 4 ? AttnSmem<D, 2, 2>::DYN_BYTES : TileSmem<D>::DYN_BYTES;
 }
-int attn_smem(const fcp_cache_config& c, RowTile t) { return c.head_dim == 128 ? attn_smem<128>(t) : attn_smem<64>(t); }
+int attn_smem(const fcp_cache_config& c, int blocks) { return c.head_dim == 128 ? attn_smem<128>(blocks) : attn_smem<64>(blocks); }
 
 // The first compute call of a handle: device, kernel attributes, tensor maps.  Later ones: the device is still the current one.
 int ready(const char* call, const fcp_cache* cache) {
@@ -166,8 +153,8 @@ int ready(const char* call, const fcp_cache* cache) {
     return FCP_ERR_CUDA;
   }
   const fcp_cache_config& c = cache->config;
-  for (RowTile t : {kWeights, row_tile(8), row_tile(16), row_tile(32), row_tile(64), row_tile(128)})
-    FCP_CUDA_CHECK(cudaFuncSetAttribute(attn_kernel(c, t), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(c, t)));
+  for (int blocks : {kWeights, 1, 2, 4, TILE_ROWS / 8})
+    FCP_CUDA_CHECK(cudaFuncSetAttribute(attn_kernel(c, blocks), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(c, blocks)));
   FCP_CUDA_CHECK(cudaFuncSetAttribute(cache_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_KEYS * 4));
   int rc = cache_map(&cache->k_map, c, c.k);
   if (rc == FCP_OK) rc = cache_map(&cache->v_map, c, c.v);
@@ -180,11 +167,11 @@ int ready(const char* call, const fcp_cache* cache) {
 int64_t chunk_stride(const fcp_cache_config& c, const fcp_cache_batch& b) {
   return ((int64_t)b.table_width * c.page_tokens + CT_KEYS - 1) / CT_KEYS * CT_KEYS;
 }
-// Whether a call goes through bf16 copies and tcgen05: where that takes less time by what both were measured to take, in clk of
-// the device per tile of 128 keys.  cache_attn_kernel: 11500 per KV head and 128 rows, spread over all SMs.  The other way: 5900 per KV head for the
-// copies; fcp_fwd_kernel takes 1700 per query head and tile of 128 new tokens, 1270 where two run beside each other, and no item is
-// cut along the keys.  4 sequences of 6K to 12K tokens, 32/8 heads, us, copies against not: 512 new tokens 290, 1400; 256 231, 770;
-// 128 185, 399; one sequence, 128 162, 170; 8/8 heads, 4 x 128 182, 128.  The copies may take up to 8 GB.
+// Whether a call goes through bf16 copies and the packed attention: where that takes less time by a third by what both were measured to
+// take, in clk of the device per tile of 128 keys.  cache_tile_kernel: 4800 per KV head and 128 rows, spread over all SMs.  The other way:
+// 5900 per KV head for the copies; fcp_fwd_kernel takes 1700 per query head and tile of 128 new tokens, 1270 where two run beside
+// each other, and no item is cut along the keys.  4 sequences of 6K to 12K tokens, 32/8 heads, us, copies against not: 512 new
+// tokens 291, 535; 256 232, 290; 128 185, 172; 64 194, 110.  The copies may take up to 8 GB.
 constexpr int64_t kChunkBytes = int64_t(8) << 30;
 bool in_chunks(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq) {
   const int64_t tokens = b.B * chunk_stride(c, b), units = (int64_t)b.B * ((b.max_new + FCP_FWD_UNIT_ROWS - 1) / FCP_FWD_UNIT_ROWS);
@@ -192,9 +179,9 @@ bool in_chunks(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq) 
       2 * units * hq >= int64_t(1) << 31)
     return false;
   const int64_t rows = ((int64_t)b.max_new * (hq / c.hkv) + 127) / 128, items = b.B * ((b.max_new + 127) / 128) * (int64_t)hq;
-  const int64_t direct = b.B * (int64_t)c.hkv * rows * 11500 / FCP_PLAN_SMS;
+  const int64_t direct = b.B * (int64_t)c.hkv * rows * 4800 / FCP_PLAN_SMS;
   const int64_t copied = std::max<int64_t>(1700, items * 1270 / FCP_PLAN_SMS) + b.B * (int64_t)c.hkv * 5900 / FCP_PLAN_SMS;
-  return copied < direct;
+  return 3 * copied < 2 * direct;
 }
 
 // Workspace of fcp_cache_attn: partial outputs and log-sum-exps of two groups per CTA, and what each CTA shares; for chunks also
@@ -203,14 +190,14 @@ struct AttnSpace {
   int64_t o, lse, split, k, v, careful, units, groups, row_limit, bytes;
   int32_t units_per_seq;
 };
-AttnSpace attn_space(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq, RowTile t) {
+AttnSpace attn_space(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq) {
   AttnSpace s = {};
   auto take = [&s](int64_t bytes) {
     const int64_t at = s.bytes;
     s.bytes += (bytes + 255) / 256 * 256;
     return at;
   };
-  const int64_t parts = 2 * (int64_t)FCP_PLAN_SMS * t.rows();
+  const int64_t parts = 2 * (int64_t)FCP_PLAN_SMS * 8 * row_blocks((int64_t)b.max_new * (hq / c.hkv));
   s.o = take(parts * c.head_dim * 4);
   s.lse = take(parts * 4);
   s.split = take(FCP_PLAN_SMS * SP_W * 4);
@@ -346,7 +333,7 @@ extern "C" int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_
   int rc = check_batch(call, cache, batch, true);
   if (rc == FCP_OK) rc = check_heads(call, cache->config, hq);
   if (rc != FCP_OK) return rc;
-  *bytes = attn_space(cache->config, *batch, hq, row_tile((int64_t)batch->max_new * (hq / cache->config.hkv))).bytes;
+  *bytes = attn_space(cache->config, *batch, hq).bytes;
   return FCP_OK;
 }
 
@@ -414,8 +401,8 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
     fcp_set_error("%s: an output is NULL or not aligned", call);
     return FCP_ERR_INVALID_ARG;
   }
-  const RowTile tile = row_tile((int64_t)batch->max_new * group);
-  const AttnSpace space = attn_space(c, *batch, hq, tile);
+  const int blocks = row_blocks((int64_t)batch->max_new * group);
+  const AttnSpace space = attn_space(c, *batch, hq);
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < space.bytes) {
     fcp_set_error("%s: workspace of %lld bytes (aligned to 256) needed, %lld given", call, (long long)space.bytes, (long long)workspace_bytes);
     return FCP_ERR_WORKSPACE;
@@ -442,9 +429,9 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* bat
     if ((rc = attn_in_chunks(cache, *batch, a, space, (char*)workspace, st)) != FCP_OK) return rc;
     a.s.only = (const int32_t*)((char*)workspace + space.careful);       // what is left
   }
-  FCP_CUDA_CHECK(launch(attn_kernel(c, tile), grid, CT_THREADS, attn_smem(c, tile), st, cache->k_map, cache->v_map, a));
-  if (c.head_dim == 128) FCP_CUDA_CHECK(launch(cache_merge_kernel<128>, grid, MERGE_THREADS, 0, st, a, tile.rows()));
-  else FCP_CUDA_CHECK(launch(cache_merge_kernel<64>, grid, MERGE_THREADS, 0, st, a, tile.rows()));
+  FCP_CUDA_CHECK(launch(attn_kernel(c, blocks), grid, blocks > 4 ? TILE_THREADS : CT_THREADS, attn_smem(c, blocks), st, cache->k_map, cache->v_map, a));
+  if (c.head_dim == 128) FCP_CUDA_CHECK(launch(cache_merge_kernel<128>, grid, MERGE_THREADS, 0, st, a, 8 * blocks));
+  else FCP_CUDA_CHECK(launch(cache_merge_kernel<64>, grid, MERGE_THREADS, 0, st, a, 8 * blocks));
   a.s = all;
   if (accumulate)
     FCP_CUDA_CHECK(launch(attn_kernel(c, kWeights), WEIGHT_CTAS * grid, CT_THREADS, attn_smem(c, kWeights), st, cache->k_map, cache->v_map, a));

@@ -147,7 +147,8 @@ struct AppendArgs {
 };
 
 // One piece of work per (page touched, head, K or V), for as many warps as give a thread N pieces of 16 values, which stay in
-// registers between the maximum and the codes.  HBM bound: 64K tokens of 8 heads, pages of 64, int8: TODO.
+// registers between the maximum and the codes.  HBM bound: 64K tokens of 8 heads, pages of 64, int8: 70 us,
+// 5.8 TB/s (pages of 16, a warp each: 73 us).
 constexpr int append_warps(int page_tokens, int D, int N) { return page_tokens * D / (512 * N) < 1 ? 1 : page_tokens * D / (512 * N); }
 __host__ __device__ constexpr int append_threads(int warps) { return 32 * (warps < 4 ? 4 : warps); }
 template <int D, int KIND, int N, int WARPS>
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(append_threads(WARPS)) cache_append_kernel(con
 // of halves, which hold codes and probabilities exactly enough; a group that several CTAs share leaves one partial result
 // per CTA, joined by a second kernel in a fixed order.
 //
-// Products by mma.sync, not tcgen05: a decode step has 1 to 16 rows per KV head, tcgen05 wants 64 or 128, and codes
+// Products by mma.sync, not tcgen05, up to 32 rows: a decode step has 1 to 16 rows per KV head, tcgen05 wants 64 or 128, and codes
 // have to pass through registers to become halves anyway.  Keys and value columns are the 16-row operand, the rows the 8
 // columns: S^T = K Q^T, O^T = V^T P^T, so that 8 rows (one token of 8 query heads) fill a product.
 constexpr int CT_KEYS = 128;                          // keys of a tile
@@ -322,7 +323,7 @@ struct AttnSmem {
   static constexpr int BLOCKS = NR * (WR ? WR : 1), ROWS = 8 * BLOCKS;
   static constexpr int TILE = CT_KEYS * D;            // bytes of K or of V
   static constexpr int STAGE = WR ? 2 * TILE : TILE;
-  static constexpr int STAGES = WR == 0 ? 4 : D == 64 ? 8 : WR == 8 ? 3 : NR == 2 ? 4 : 5;
+  static constexpr int STAGES = WR == 0 ? 4 : D == 64 ? 8 : NR == 2 ? 4 : 5;
   static constexpr int RING = STAGES * STAGE;
   // the queries of a group travel with its first tile where they are few; else the warps fetch them
   static constexpr int QUERY_BYTES = WR == 1 ? ROWS * D * 2 : 0;
@@ -361,7 +362,8 @@ __device__ __forceinline__ float exp2_approx(float x) {
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
 
 // How the tiles of a batch lie in a row: sequence after sequence, its KV heads, their row tiles, their key tiles.
-// A group counts for GROUP_COST tiles more than it has, for what its queries and its end take: TODO
+// A group counts for GROUP_COST tiles more than it has, for what its queries and its end take.  64 sequences of 300 to 8K tokens, 8 KV heads,
+// us: 0 tiles 105, 1 tile 84, 2 tiles 73, 4 tiles 70 with pages of 128; 112, 92, 94, 99 with pages of 16.
 struct TileOrder {
   static constexpr int GROUP_COST = 2;
   int32_t rows_per_tile, group, hkv;
@@ -492,7 +494,17 @@ struct QueryArea {
     }
   }
 };
-__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(CT_WARPS * 32) : "memory"); }
+// A barrier of the eight consumer warps that gives up like every other wait: a warp that has left may not hold up the others.
+struct ConsumerSync {
+  uint32_t bar, phase;
+  __device__ __forceinline__ bool operator()(const WaitCtx& ctx, int lane, int where) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+    const bool ok = mbar_wait_warp(bar, phase, ctx, where);
+    phase ^= 1;
+    return ok;
+  }
+};
 
 // 16 bytes `chunk` of key `key` of a tile, as TMA has swizzled them.
 template <int D>
@@ -546,10 +558,9 @@ struct TileRun {
 
 // A loading warp walks the CTA's tiles.  Page numbers are fetched two runs ahead, the scales they lead to one run ahead, so that
 // the loop waits for neither; fetched when needed, the two in a row held the ring up for 1 to 2 us in every four tiles.
-template <int D, int NR, int WR>
+// S: the layout of shared memory (AttnSmem, TileSmem).
+template <int D, class S, bool WEIGHTS>
 struct AttnProducer {
-  using S = AttnSmem<D, NR, WR>;
-  static constexpr bool WEIGHTS = WR == 0;
   static constexpr int SUBS = CT_KEYS / 16;
   const AttnArgs& A;
   const TileOrder& order;
@@ -640,7 +651,7 @@ struct AttnProducer {
     r.vs = ld_f32(A.c.v_scale + r.page * A.c.hkv + r.head);
   }
 
-  // `map`: of the keys, or of the values (is_v); the keys' warp also describes the stages and fetches the queries.
+  // `map`, `ring`: of the keys, or of the values (is_v); the keys' warp also describes the stages and fetches the queries.
   __device__ __forceinline__ void run(const CUtensorMap* map, int is_v, uint32_t ring, uint32_t queries, StageMeta* meta, uint32_t full,
                                       uint32_t empty, const WaitCtx& ctx) {
     const int lane = threadIdx.x & 31, sub = lane & (SUBS - 1);
@@ -699,7 +710,7 @@ struct AttnProducer {
           bulk_load(queries + (stage * order.rows_per_tile + lane) * (2 * D),
                     A.q + (int64_t)(now.s.row0 + j) * A.q_stride + (now.head * A.group + row - j * A.group) * D, 2 * D, bar);
         }
-        if (loads) tma_load_2d(ring + stage * S::STAGE + is_v * S::TILE + sub * 16 * D, map, bar, 0, now.row);
+        if (loads) tma_load_2d(ring + stage * S::STAGE + sub * 16 * D, map, bar, 0, now.row);
         __syncwarp();
         if (++stage == S::STAGES) {
           stage = 0;
@@ -728,13 +739,12 @@ struct AttnProducer {
   }
 };
 
-// WR warps side by side hold the rows of a tile, 8 * NR each; the 8 / WR warps behind each other take different keys: 32 of a
-// tile (64, 128 with four, eight warps side by side), with one warp side by side of every second tile only.
+// WR warps side by side (1 or 2) hold the rows of a tile, 8 * NR each; the 8 / WR warps behind each other take 32 keys each: of
+// a tile, or with one warp side by side of every second tile.
 template <int D, int KIND, int NR, int WR>
 struct AttnConsumer {
   using S = AttnSmem<D, NR, WR>;
   static constexpr int RT = 8 * NR * WR, KG = CT_WARPS / WR, MT = D / 16;
-  static constexpr int STEPS = WR <= 2 ? 1 : WR / 2;  // of 32 keys, per warp and tile
   const uint2* frag;                                  // this warp's rows
   float factor[NR][2];                                // of rows 2t and 2t + 1 of each block
   int32_t limit[NR][2], least, most;                  // least, most: limits of the first and the last row that exist
@@ -880,9 +890,10 @@ struct AttnConsumer {
   }
 
   // The end of a group's tiles on this CTA: joins the warps and writes the rows, or their partial result.
-  __device__ __forceinline__ void finish(const AttnArgs& A, const StageMeta& meta, float4* join, float2* stats, int warp, int lane) {
+  __device__ __forceinline__ bool finish(const AttnArgs& A, const StageMeta& meta, float4* join, float2* stats, ConsumerSync& sync, const WaitCtx& ctx, int warp,
+                                         int lane) {
     const int g = lane >> 2, t = lane & 3, tid = warp * 32 + lane;
-    consumer_sync();                                  // the join area's last readers are done
+    if (!sync(ctx, lane, 923)) return false;          // the join area's last readers are done
     float4* mine = join + warp * 8 * NR * (D / 4);
     const int n_rows = min(RT, meta.n * A.group - meta.row_tile * RT);
 #pragma unroll
@@ -899,7 +910,7 @@ struct AttnConsumer {
         for (int c = 0; c < D / 32; ++c)
           mine[join_slot(row, g * (D / 32) + c)] = make_float4(o[i][2 * c][r], o[i][2 * c][r + 2], o[i][2 * c + 1][r], o[i][2 * c + 1][r + 2]);
       }
-    consumer_sync();
+    if (!sync(ctx, lane, 924)) return false;
     for (int e = tid; e < n_rows * (D / 4); e += CT_WARPS * 32) {
       const int r = e / (D / 4), f = e % (D / 4), wr = r / (8 * NR), row = r % (8 * NR);
       float top = -3e38f;
@@ -928,12 +939,13 @@ struct AttnConsumer {
         if (f == 0) A.part_lse[(int64_t)meta.part * RT + r] = lse2;
       }
     }
+    return true;
   }
 
   __device__ __forceinline__ void run(const AttnArgs& A, const uint8_t* ring, const uint8_t* queries, const QueryArea<D>& area, const StageMeta* metas, float4* join, float2* stats,
-                                      uint32_t full, uint32_t empty, const WaitCtx& ctx) {
+                                      uint32_t full, uint32_t empty, ConsumerSync sync, const WaitCtx& ctx) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, kg = warp / WR;
-    const int turn = WR == 1 ? kg >> 2 : 0, first = (WR == 1 ? kg & 3 : kg) * STEPS;       // which tiles, which 32 keys of them
+    const int turn = WR == 1 ? kg >> 2 : 0, i = WR == 1 ? kg & 3 : kg;       // which tiles, which 32 keys of them
     int stage = 0, tile = 0;
     uint32_t phase = 0;
     frag = area.frag + wr * NR * (D / 16) * 32;
@@ -943,7 +955,7 @@ struct AttnConsumer {
       if (flags & ST_END) break;
       if (flags & ST_FIRST) {
         area.template fill<false>(A, meta, meta.row_tile * RT, S::BLOCKS, S::QUERY_BYTES ? queries + stage * S::QUERY_BYTES : nullptr, warp, lane);
-        consumer_sync();
+        if (!sync(ctx, lane, 922)) break;
         const int first_row = meta.row_tile * RT + wr * 8 * NR, n_rows = meta.n * A.group;
         const int last_row = min(first_row + 8 * NR, n_rows) - 1;
         least = meta.length - meta.n + first_row / A.group + 1;
@@ -964,14 +976,11 @@ struct AttnConsumer {
       }
       if (WR > 1 || (tile & 1) == turn) {
         const uint8_t* ktile = ring + stage * S::STAGE;
-#pragma unroll 1
-        for (int i = first; i < first + STEPS; ++i) {
-          const int key = meta.key0 + i * CT_STEP;
-          const float4 about[2] = {meta.sub[2 * i], meta.sub[2 * i + 1]};
-          if (key < most && (about[0].x != 0.f || about[1].x != 0.f)) step(ktile, ktile + S::TILE, i * CT_STEP, key, about, lane);
-        }
+        const int key = meta.key0 + i * CT_STEP;
+        const float4 about[2] = {meta.sub[2 * i], meta.sub[2 * i + 1]};
+        if (key < most && (about[0].x != 0.f || about[1].x != 0.f)) step(ktile, ktile + S::TILE, i * CT_STEP, key, about, lane);
       }
-      if (flags & ST_LAST) finish(A, meta, join, stats, warp, lane);
+      if ((flags & ST_LAST) && !finish(A, meta, join, stats, sync, ctx, warp, lane)) break;
       __syncwarp();
       if (lane == 0) mbar_arrive(empty + stage * 8);
       ++tile;
@@ -987,7 +996,7 @@ struct AttnConsumer {
 // rows in blocks of 8, NR blocks in shared memory at a time, so that a key's sum is taken by four threads in a fixed order.
 template <int D, int KIND, int NR>
 __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t* ring, const QueryArea<D>& area, const StageMeta* metas,
-                                                uint32_t full, uint32_t empty, const WaitCtx& ctx) {
+                                                uint32_t full, uint32_t empty, ConsumerSync sync, const WaitCtx& ctx) {
   using S = AttnSmem<D, NR, 0>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int stage = 0;
@@ -1002,9 +1011,9 @@ __device__ __forceinline__ void weight_consumer(const AttnArgs& A, const uint8_t
     for (int r0 = 0; r0 < n_rows; r0 += 8 * NR) {
       const int blocks = min(NR, (n_rows - r0 + 7) / 8), least = meta.length - meta.n + r0 / A.group + 1;
       if (n_rows > 8 * NR || (meta.flags & ST_FIRST)) {
-        consumer_sync();                              // the rows before have been read
+        if (!sync(ctx, lane, 932)) return;            // the rows before have been read
         area.template fill<true>(A, meta, r0, (blocks + 3) / 4 * 4, nullptr, warp, lane);
-        consumer_sync();
+        if (!sync(ctx, lane, 933)) return;
       }
       if (key >= meta.length || about.x == 0.f) continue;
       uint32_t a[D / 16][4];                          // the keys as operands
@@ -1075,7 +1084,7 @@ __global__ void __launch_bounds__(CT_THREADS, WR == 0 ? WEIGHT_CTAS : 1)
 cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ AttnArgs A) {
   using S = AttnSmem<D, NR, WR>;
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t bars[2 * S::STAGES];
+  __shared__ __align__(8) uint64_t bars[2 * S::STAGES + 1];
   __shared__ __align__(16) StageMeta metas[S::STAGES];
   __shared__ float2 stats[WR ? CT_WARPS * 8 * NR : 1];
   __shared__ __align__(16) RowInfo rows[S::ROWS];
@@ -1083,6 +1092,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   __shared__ int abort_flag;
   const int warp = threadIdx.x >> 5;
   const uint32_t full = smem_u32(bars), empty = full + S::STAGES * 8;
+  const ConsumerSync sync = {empty + S::STAGES * 8, 0};
   // the swizzle pattern repeats every 1024 bytes of address
   const uint32_t skip = (1024u - (smem_u32(smem) & 1023u)) & 1023u;
   uint8_t* ring = smem + skip;
@@ -1094,6 +1104,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
       mbar_init(full + i * 8, WR ? 2 : 1);
       mbar_init(empty + i * 8, CT_WARPS);
     }
+    mbar_init(sync.bar, CT_WARPS);
     fence_mbar_init();
     prefetch_tmap(&tk);
     prefetch_tmap(&tv);
@@ -1104,16 +1115,458 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   const TileOrder order = {8 * NR * (WR ? WR : 1), A.group, A.c.hkv, WR == 0};
   const CtaRange range = cta_range(A.s, order, A.c.status, scratch);
   if (warp >= CT_WARPS) {
-    AttnProducer<D, NR, WR> producer(A, order, range);
-    if (warp == CT_WARPS || WR > 0) producer.run(warp == CT_WARPS ? &tk : &tv, warp - CT_WARPS, smem_u32(ring), smem_u32(queries), metas, full, empty, ctx);
+    AttnProducer<D, S, WR == 0> producer(A, order, range);
+    if (warp == CT_WARPS || WR > 0) producer.run(warp == CT_WARPS ? &tk : &tv, warp - CT_WARPS, smem_u32(ring) + (warp - CT_WARPS) * S::TILE, smem_u32(queries), metas, full, empty, ctx);
   } else if constexpr (WR == 0) {
-    weight_consumer<D, KIND, NR>(A, ring, area, metas, full, empty, ctx);
+    weight_consumer<D, KIND, NR>(A, ring, area, metas, full, empty, sync, ctx);
   } else {
     AttnConsumer<D, KIND, NR, WR> consumer;
-    consumer.run(A, ring, queries, area, metas, reinterpret_cast<float4*>(queries + S::STAGES * S::QUERY_BYTES + S::FRAGS), stats, full, empty, ctx);
+    consumer.run(A, ring, queries, area, metas, reinterpret_cast<float4*>(queries + S::STAGES * S::QUERY_BYTES + S::FRAGS), stats, full, empty, sync, ctx);
   }
   __syncthreads();
   wait_teardown(ctx);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention of tiles of up to 128 rows
+// ---------------------------------------------------------------------------------------------
+// From 33 rows per KV head on the products go to tcgen05: eight warps turn a tile's codes into halves in shared memory, once for
+// all rows, S = Q K^T and O += P V run on 128 rows whether they are all there or not (1024 clk per tile of 128 keys, D = 128), and
+// eight warps keep the softmax, half a row per thread, with P and O in tensor memory.  A tile takes 4400 to 5000 clk: bound by the chain
+// codes - halves - S - softmax - P - O with its hand-overs between warps and by shared memory (codes in, halves out, halves into the
+// products), not by the products.  16 sequences of 4K to 32K tokens, 40/8 heads, int8: 253 us for 35 rows, 270 us for 125 rows per KV head
+// (404 TFLOP/s); cache_attn_kernel took 323 and 602.  Four converting warps for K and four for V were slower than eight for both (142
+// against 111 us, 4 sequences, 64 new tokens); a second buffer for K's halves in place of a third stage changed nothing.
+//   warps 0..7    codes -> halves: queries at the start of a group, K of tile t, V of tile t - 1
+//   warps 8, 9    the loading warps above
+//   warp 10       issues the products: S of tile t, then O += P V of tile t - 1
+//   warps 12..19  softmax and output: two per quarter of the tensor memory's lanes, each with half of a tile's columns
+// Tensor memory: S of two tiles in turn | P of two tiles | O.
+constexpr int TILE_THREADS = 640;
+constexpr int TILE_ROWS = 128;
+constexpr int TILE_CONVERT = 8;                       // converting warps
+constexpr int TILE_RING = 8;                          // what goes with a tile: nobody is more than four behind; with a group: three
+constexpr int TILE_GROUPS = 4;
+template <int D>
+struct TileSmem {
+  // codes of K and of V in rings of their own; halves of a tile of K, one of V, and the queries
+  static constexpr int TILE = CT_KEYS * D, STAGE = TILE, STAGES = D == 64 ? 6 : 3, QUERY_BYTES = 0;
+  static constexpr int RING = STAGES * STAGE, HALVES = 128 * D * 2;
+  static constexpr int DYN_BYTES = 2 * RING + 3 * HALVES + 1024;
+};
+struct TileMeta {
+  int32_t flags, key0, row0, n, length, head, row_tile, part;
+  float4 sub[CT_KEYS / 16];                           // as in StageMeta
+};
+struct TileGroup {                                    // of a group's rows
+  float factor[TILE_ROWS];
+  int32_t limit[TILE_ROWS];
+  int32_t least, nan_any;
+};
+
+// Instruction descriptor like make_idesc, for halves.
+__host__ __device__ constexpr uint32_t make_idesc_f16(int M, int N, int b_mn_major) {
+  return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// 16 codes -> 32 bytes of halves at columns [16 c, 16 c + 16) of row r of a tile of [128][64]-element swizzled blocks.
+template <int D, int KIND>
+__device__ __forceinline__ void put_halves(uint8_t* tile, int r, int c, const uint32_t (&w)[4]) {
+  const uint4 lo = make_uint4(halves_lo<KIND>(w[0]), halves_hi<KIND>(w[0]), halves_lo<KIND>(w[1]), halves_hi<KIND>(w[1]));
+  const uint4 hi = make_uint4(halves_lo<KIND>(w[2]), halves_hi<KIND>(w[2]), halves_lo<KIND>(w[3]), halves_hi<KIND>(w[3]));
+  uint8_t* row = tile + (c >> 2) * 16384 + r * 128;
+  const int a = ((c & 3) * 2) ^ (r & 7);
+  // lanes of the second block write their upper half first, so that eight lanes cover all banks
+  const bool swap = c >> 2;
+  *reinterpret_cast<uint4*>(row + ((swap ? a ^ 1 : a) << 4)) = swap ? hi : lo;
+  *reinterpret_cast<uint4*>(row + ((swap ? a : a ^ 1) << 4)) = swap ? lo : hi;
+}
+
+template <int D, int KIND>
+__global__ void __launch_bounds__(TILE_THREADS, 1)
+cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ AttnArgs A) {
+  using S = TileSmem<D>;
+  constexpr uint32_t S_COL = 0, P_COL = 256, O_COL = 384;      // P: 64 columns for every other tile
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars[4 * S::STAGES + 18];
+  __shared__ __align__(16) StageMeta stages[S::STAGES];
+  __shared__ __align__(16) TileMeta tiles[TILE_RING];
+  __shared__ TileGroup groups[TILE_GROUPS];
+  constexpr bool NANS = KIND == FCP_CACHE_E4M3;
+  __shared__ uint16_t nans[NANS ? TILE_GROUPS : 1][NANS ? 128 : 1][D / 16];       // columns that are NaN in the keys from `least` on
+  __shared__ int64_t scratch[16];
+  __shared__ int abort_flag;
+  __shared__ float tops[2][2][TILE_ROWS], sums[2][TILE_ROWS];
+  __shared__ uint32_t tmem_slot;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t full = smem_u32(bars), empty = full + 2 * S::STAGES * 8, bar0 = empty + 2 * S::STAGES * 8;         // K's, then V's
+  // two of each but one, for even and odd tiles: a waiter may be two tiles behind, which one phase bit does not tell
+  const uint32_t v_full = bar0, k_full = bar0 + 8, k_free = bar0 + 24, s_full = bar0 + 40, s_free = bar0 + 56, p_full = bar0 + 72, pv_done = bar0 + 88;
+  ConsumerSync sync = {bar0 + 104, 0};
+  const uint32_t pair = bar0 + 112;                   // the two softmax warps of a quarter, four times
+  const uint32_t skip = (1024u - (smem_u32(smem) & 1023u)) & 1023u;
+  uint8_t* ring = smem + skip;
+  uint8_t* k16 = ring + 2 * S::RING;
+  uint8_t* v16 = k16 + S::HALVES;
+  uint8_t* q16 = v16 + S::HALVES;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < 2 * S::STAGES; ++i) {
+      mbar_init(full + i * 8, 1);
+      mbar_init(empty + i * 8, TILE_CONVERT);
+    }
+    mbar_init(v_full, TILE_CONVERT);
+    mbar_init(sync.bar, TILE_CONVERT);
+    for (int i = 0; i < 4; ++i) mbar_init(pair + i * 8, 2);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(k_full + i * 8, TILE_CONVERT);
+      mbar_init(k_free + i * 8, 1);
+      mbar_init(p_full + i * 8, 8);
+      mbar_init(pv_done + i * 8, 2);
+      mbar_init(s_full + i * 8, 2);
+      mbar_init(s_free + i * 8, 8);
+    }
+    fence_mbar_init();
+    prefetch_tmap(&tk);
+    prefetch_tmap(&tv);
+  }
+  if (warp == 10) {
+    tmem_alloc(smem_u32(&tmem_slot), 512);
+    tmem_relinquish();
+  }
+  grid_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const WaitCtx ctx = {&abort_flag, A.c.status, (uint32_t)FCP_WAIT_NS};
+  const TileOrder order = {TILE_ROWS, A.group, A.c.hkv, false};
+  const CtaRange range = cta_range(A.s, order, A.c.status, scratch);
+  if (warp < TILE_CONVERT) {
+    // ------------------------------------------------------------------ codes -> halves
+    // K of tile t comes before V of tile t - 1: its product does not wait for anything that V's does
+    int seg = -1, k_stage = 0, v_stage = 0, v_seg = 0, v_least = 0, v_most = 0, v_key0 = 0, next_least = 0, next_most = 0;
+    float v_scale = 0.f;                              // key scale of this warp's 16 keys of the tile whose V is next; 0: absent
+    uint32_t k_phase = 0, v_phase = 0;
+    constexpr int KEYS = CT_KEYS / TILE_CONVERT, C = D / 16, PER = KEYS * C / 32;        // pieces of 16 codes per lane and tile
+    for (int t = 0;; ++t) {
+      if (!mbar_wait_warp(full + k_stage * 8, k_phase, ctx, 941)) break;
+      const StageMeta& meta = stages[k_stage];
+      const int flags = meta.flags, key0 = meta.key0;
+      const float scale = meta.sub[warp].x;
+      if (t > 0 && !mbar_wait_warp(k_free + ((t - 1) & 1) * 8, ((t - 1) >> 1) & 1, ctx, 944)) break;
+      TileMeta& tile = tiles[t % TILE_RING];
+      if (warp == 0) {
+        if (lane < CT_KEYS / 16) tile.sub[lane] = meta.sub[lane];
+        if (lane == 0) {
+          tile.flags = flags; tile.key0 = meta.key0; tile.row0 = meta.row0; tile.n = meta.n; tile.length = meta.length;
+          tile.head = meta.head; tile.row_tile = meta.row_tile; tile.part = meta.part;
+        }
+      }
+      if (!(flags & ST_END)) {
+        if (flags & ST_FIRST) {
+          ++seg;
+          TileGroup& grp = groups[seg % TILE_GROUPS];
+          const int n_rows = meta.n * A.group, row0 = meta.row_tile * TILE_ROWS, last = min(row0 + TILE_ROWS, n_rows) - 1;
+          next_least = meta.length - meta.n + row0 / A.group + 1;
+          next_most = meta.length - meta.n + last / A.group + 1;
+          if (NANS) {
+            for (int i = threadIdx.x; i < 128 * C; i += TILE_CONVERT * 32) (&nans[seg % TILE_GROUPS][0][0])[i] = 0;
+            if (threadIdx.x == 0) {
+              grp.least = next_least;
+              grp.nan_any = 0;
+            }
+            if (!sync(ctx, lane, 946)) break;         // in front of any warp's values of this group
+          }
+          // a row at a time; times a power of two as in QueryArea
+#pragma unroll 4
+          for (int i = 0; i < TILE_ROWS / TILE_CONVERT; ++i) {
+            const int r = warp * (TILE_ROWS / TILE_CONVERT) + i, row = row0 + r, j = row / A.group;
+            uint2 x = make_uint2(0, 0);
+            if (row < n_rows) {
+              const __nv_bfloat16* p = A.q + (int64_t)(meta.row0 + j) * A.q_stride + (meta.head * A.group + row - j * A.group) * D;
+              if (D == 128) asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p + 4 * lane));
+              else asm volatile("ld.global.u32 %0, [%1];" : "=r"(x.x) : "l"(p + 2 * lane));
+            }
+            uint32_t top = max(max(x.x & 0x7fffu, (x.x >> 16) & 0x7fffu), max(x.y & 0x7fffu, (x.y >> 16) & 0x7fffu));
+            top = __reduce_max_sync(0xffffffffu, top);
+            const int e = max((int)(top >> 7), 20);
+            const float up = __uint_as_float((uint32_t)(262 - e) << 23);
+            if (lane == 0) {
+              grp.factor[r] = A.scale_log2 * __uint_as_float((uint32_t)(e - 8) << 23);
+              grp.limit[r] = row < n_rows ? meta.length - meta.n + j + 1 : 0;
+            }
+            const uint32_t h0 = pack_half(bf_lo(x.x) * up, bf_hi(x.x) * up), h1 = pack_half(bf_lo(x.y) * up, bf_hi(x.y) * up);
+            if (D == 128)
+              *reinterpret_cast<uint2*>(q16 + (lane >> 4) * 16384 + r * 128 + ((((lane & 15) >> 1) ^ (r & 7)) << 4) + (lane & 1) * 8) = make_uint2(h0, h1);
+            else
+              *reinterpret_cast<uint32_t*>(q16 + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) = h0;
+          }
+        }
+        const uint8_t* raw = ring + k_stage * S::STAGE;
+        uint32_t w[PER][4];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) words(tile_at<D>(raw, warp * KEYS + (i * 32 + lane) / C, lane % C), w[i]);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) put_halves<D, KIND>(k16, warp * KEYS + (i * 32 + lane) / C, lane % C, w[i]);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(k_full + (t & 1) * 8);
+        if (!(flags & ST_END)) mbar_arrive(empty + k_stage * 8);
+      }
+      if (t > 0) {
+        // V of the tile before
+        if (!mbar_wait_warp(full + (S::STAGES + v_stage) * 8, v_phase, ctx, 945)) break;
+        if (t > 1 && !mbar_wait_warp(pv_done + (t & 1) * 8, ((t - 2) >> 1) & 1, ctx, 943)) break;
+        const uint8_t* raw = ring + S::RING + v_stage * S::STAGE;
+        uint32_t all[PER][4];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) words(tile_at<D>(raw, warp * KEYS + (i * 32 + lane) / C, lane % C), all[i]);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int r = warp * KEYS + (i * 32 + lane) / C, c = lane % C, pos = v_key0 + r;
+          uint32_t (&w)[4] = all[i];
+          if (v_key0 + CT_KEYS <= v_least && v_scale != 0.f) {       // every row sees every key of the tile
+            put_halves<D, KIND>(v16, r, c, w);
+            continue;
+          }
+          // what no row sees is whatever the page held, and must not meet a zero weight; nor must a NaN that some rows see
+          if (pos >= v_most || v_scale == 0.f) w[0] = w[1] = w[2] = w[3] = 0;
+          if (NANS && pos >= v_least) {
+            uint32_t bits = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t m = __vcmpeq4(w[j] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+              w[j] &= ~m;
+              bits |= ((m & 1u) | (m >> 7 & 2u) | (m >> 14 & 4u) | (m >> 21 & 8u)) << (4 * j);
+            }
+            if (bits) {
+              nans[v_seg % TILE_GROUPS][pos - v_least][c] = (uint16_t)bits;
+              groups[v_seg % TILE_GROUPS].nan_any = 1;
+            }
+          }
+          put_halves<D, KIND>(v16, r, c, w);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(v_full);
+          mbar_arrive(empty + (S::STAGES + v_stage) * 8);
+        }
+        if (++v_stage == S::STAGES) {
+          v_stage = 0;
+          v_phase ^= 1;
+        }
+      }
+      if (flags & ST_END) break;
+      v_key0 = key0;
+      v_scale = scale;
+      v_seg = seg;
+      v_least = next_least;
+      v_most = next_most;
+      if (++k_stage == S::STAGES) {
+        k_stage = 0;
+        k_phase ^= 1;
+      }
+    }
+  } else if (warp < 10) {
+    AttnProducer<D, S, false> producer(A, order, range);
+    const uint32_t v = warp - 8;
+    producer.run(v ? &tv : &tk, v, smem_u32(ring) + v * S::RING, 0, stages, full + v * S::STAGES * 8, empty + v * S::STAGES * 8, ctx);
+  } else if (warp == 10) {
+    // ------------------------------------------------------------------ products
+    constexpr uint32_t IDESC_QK = make_idesc_f16(128, 128, 0), IDESC_PV = make_idesc_f16(128, D, 1);
+    int before = 0;                                   // flags of the tile before
+    for (int t = 0;; ++t) {
+      if (!mbar_wait_warp(k_full + (t & 1) * 8, (t >> 1) & 1, ctx, 951)) break;
+      const int flags = __shfl_sync(0xffffffffu, tiles[t % TILE_RING].flags, 0);
+      if (!(flags & ST_END)) {
+        if (!mbar_wait_warp(s_free + (t & 1) * 8, ((t >> 1) & 1) ^ 1, ctx, 952)) break;
+        tc_fence_after();
+        umma_loop_kk<0, D / 16>(tmem + S_COL + (t & 1) * 128, smem_u32(q16), smem_u32(k16), IDESC_QK);
+        tc_commit(s_full + (t & 1) * 8);
+        tc_commit(k_free + (t & 1) * 8);
+        if (lane == 0) mbar_arrive(s_full + (t & 1) * 8);      // passes on what the converting warps wrote about the tile
+      }
+      if (t > 0) {
+        if (!mbar_wait_warp(v_full, (t - 1) & 1, ctx, 954)) break;
+        if (!mbar_wait_warp(p_full + ((t - 1) & 1) * 8, ((t - 1) >> 1) & 1, ctx, 955)) break;
+        tc_fence_after();
+        umma_loop_ts<0, 8>(tmem + O_COL, tmem + P_COL + ((t - 1) & 1) * 64, false, smem_u32(v16), IDESC_PV, before & ST_FIRST ? 0u : 1u);
+        tc_commit(pv_done + ((t - 1) & 1) * 8);
+        if (lane == 0) mbar_arrive(pv_done + ((t - 1) & 1) * 8);
+      }
+      if (flags & ST_END) {
+        tc_commit(s_full + (t & 1) * 8);
+        if (lane == 0) mbar_arrive(s_full + (t & 1) * 8);
+        break;
+      }
+      before = flags;
+    }
+  } else if (warp >= 12) {
+    // ------------------------------------------------------------------ softmax
+    const int quarter = warp & 3, half = (warp - 12) >> 2, row = quarter * 32 + lane;
+    const uint32_t t_o = tmem_addr(tmem, quarter * 32, O_COL + half * (D / 2));
+    ConsumerSync both = {pair + quarter * 8, 0};
+    float factor = 0.f, ref = -3e38f, l = 0.f;
+    int limit = 0, seg = -1;
+    bool there = false, begun = false;                // these warps have rows; O holds something of this group
+    for (int t = 0;; ++t) {
+      if (!mbar_wait_warp(s_full + (t & 1) * 8, (t >> 1) & 1, ctx, 961)) break;
+      tc_fence_after();
+      const TileMeta& meta = tiles[t % TILE_RING];
+      const int flags = meta.flags;
+      if (flags & ST_END) break;
+      if (flags & ST_FIRST) {
+        ++seg;
+        factor = groups[seg % TILE_GROUPS].factor[row];
+        limit = groups[seg % TILE_GROUPS].limit[row];
+        there = meta.row_tile * TILE_ROWS + quarter * 32 < meta.n * A.group;
+        ref = -3e38f;
+        l = 0.f;
+        begun = false;
+      }
+      uint32_t x[64];                                 // this warp's half of the row's scores
+      float top = -INFINITY;
+      const int seen = limit - meta.key0 - 64 * half; // columns of the half that the row sees
+      const bool edge = __any_sync(0xffffffffu, seen < 64);
+      if (there) {
+        const uint32_t t_s = tmem_addr(tmem, quarter * 32, S_COL + (t & 1) * 128 + 64 * half);
+        tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(x));
+        tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(x + 32));
+        tc_wait_ld(x);
+        // a = score in log2 units plus log2 of the value scale, as in AttnConsumer
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const float4 about = meta.sub[4 * half + h];
+          if (edge || about.x == 0.f) {
+            const int n = about.x == 0.f ? 0 : seen - 16 * h;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (i >= n) x[16 * h + i] = 0xff800000u;
+          }
+          float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            m0 = max3(m0, __uint_as_float(x[16 * h + i]), __uint_as_float(x[16 * h + i + 1]));
+            m1 = max3(m1, __uint_as_float(x[16 * h + i + 2]), __uint_as_float(x[16 * h + i + 3]));
+          }
+          if (about.x != 0.f) top = fmaxf(top, fmaf(fmaxf(m0, m1), fmaxf(factor * about.x, 1.2e-38f), about.y));
+        }
+        tops[t & 1][half][row] = top;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_free + (t & 1) * 8);
+      // this tile's place for P is free.  Warps without rows wait too, so that none arrives twice in one phase of p_full.
+      if (t > 1 && !mbar_wait_warp(pv_done + (t & 1) * 8, ((t - 2) >> 1) & 1, ctx, 962)) break;
+      if (there) {
+        if (!both(ctx, lane, 965)) break;
+        top = fmaxf(top, tops[t & 1][half ^ 1][row]);
+        tc_fence_after();
+        if (__any_sync(0xffffffffu, top > ref + 15.f)) {       // the same in both warps
+          const float m = top > ref + 15.f ? top - 8.f : ref, shrink = exp2_approx(ref - m);
+          l *= shrink;
+          ref = m;
+          if (begun) {                                // O is at rest once the tile before is in it
+            if (!mbar_wait_warp(pv_done + ((t - 1) & 1) * 8, ((t - 1) >> 1) & 1, ctx, 963)) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[16];
+              tmem_ld16(t_o + 16 * c, o);
+              tc_wait_ld(o);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * shrink);
+              tmem_st16(t_o + 16 * c, o);
+            }
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t p[16];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float4 about = meta.sub[4 * half + 2 * c + h];
+            const bool is = about.x != 0.f;           // else the scores are -infinity whatever they are multiplied by
+            const float f = is ? fmaxf(factor * about.x, 1.2e-38f) : 1.f, shift = about.y - ref;      // not 0: times -infinity
+            float z0 = 0.f, z1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int e = 32 * c + 16 * h + 2 * i;
+              const float a = exp2_approx(fmaf(__uint_as_float(x[e]), f, shift)), b = exp2_approx(fmaf(__uint_as_float(x[e + 1]), f, shift));
+              z0 += a;
+              z1 += b;
+              p[8 * h + i] = pack_half(a, b);
+            }
+            l = fmaf(z0 + z1, about.z, l);
+          }
+          tmem_st16(tmem_addr(tmem, quarter * 32, P_COL + (t & 1) * 64 + half * 32 + 16 * c), p);
+        }
+        tc_wait_st();
+        begun = true;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + (t & 1) * 8);
+      if (flags & ST_LAST) {
+        if (there) {
+          sums[half][row] = l;
+          if (!both(ctx, lane, 966)) break;
+          const float z = sums[0][row] + sums[1][row];
+          if (!mbar_wait_warp(pv_done + (t & 1) * 8, (t >> 1) & 1, ctx, 964)) break;
+          tc_fence_after();
+          const int gr = meta.row_tile * TILE_ROWS + row, j = gr / A.group;
+          const bool is = gr < meta.n * A.group;
+          const float inverse = z == 0.f ? 0.f : 1.f / z, lse2 = z == 0.f ? -INFINITY : ref + __log2f(z);
+          const int64_t out = (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + gr - j * A.group, part = (int64_t)meta.part * TILE_ROWS + row;
+          const TileGroup& grp = groups[seg % TILE_GROUPS];
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {          // this warp's half of the columns
+            uint32_t o[16];
+            tmem_ld16(t_o + 16 * c, o);
+            tc_wait_ld(o);
+            const int col = half * (D / 32) + c;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(z == 0.f ? 0.f : __uint_as_float(o[i]) * inverse);
+            if (NANS && grp.nan_any) {
+              uint32_t bits = 0;
+              for (int k = 0; k < min(limit - grp.least, 128); ++k) bits |= nans[seg % TILE_GROUPS][k][col];
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (bits >> i & 1) o[i] = 0x7fffffffu;
+            }
+            if (!is) continue;
+            if (flags & ST_WHOLE) {
+              uint32_t y[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) y[i] = pack_bf16(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
+              uint4* dst = reinterpret_cast<uint4*>(A.o + out * D + 16 * col);
+              dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+              dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
+            } else {
+              uint4* dst = reinterpret_cast<uint4*>(A.part_o + part * D + 16 * col);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+          }
+          if (is && half == 0) {
+            if (flags & ST_WHOLE) A.lse[out] = lse2 * 0.69314718055994531f;
+            else A.part_lse[part] = lse2;
+          }
+          tc_fence_before();                          // O is free for the next group with this warp's next arrival at p_full
+        }
+      }
+    }
+  }
+  wait_teardown(ctx);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 10) {
+    __syncwarp();
+    tmem_dealloc(tmem, 512);
+  }
 }
 
 // Joins the partial results of groups that several CTAs shared: block c takes the group that began on CTA c, in the CTAs' order.
@@ -1348,7 +1801,8 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
 // largest weights by three counting passes over 11, 11 and 10 bits of the keys, from the top, the counts added up over the cluster;
 // then one pass writes the kept positions in order.
 // Keys go four at a time: they lie side by side in a page, and one place in the page table, one load and one address serve them
-// (key by key the kernel was bound by its instructions, 120 000 warp instructions per block).
+// (key by key the kernel was bound by its instructions, 120 000 warp instructions per block).  2 sequences of 128K tokens, 8 heads: 44 us,
+// 8 blocks per head, bound by the chain of counting passes and cluster barriers; reading the weights alone takes 1.4 us.
 constexpr int SELECT_THREADS = 1024;
 constexpr int SELECT_KEYS = 49152;                    // as many keys of a slice stay in shared memory
 constexpr int SELECT_BINS = 2048;

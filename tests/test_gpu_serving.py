@@ -279,7 +279,7 @@ def test_append_scales_that_are_no_powers_of_two():
 def goes_by_copies(w, new, hq):
     """Whether a call with these new tokens asks for room for bf16 copies of all keys and values, besides the partial results."""
     rows = max(new) * hq // w.hkv
-    tile = next((t for t in (8, 16, 32, 64) if rows <= t), 128)
+    tile = next((t for t in (8, 16, 32) if rows <= t), 128)
     partial, copies = 2 * 148 * tile * (w.d + 1) * 4, len(new) * w.width * w.page * w.hkv * w.d * 4
     return fcp.fcp_cache_attn_workspace_bytes(w.cache, w.batch(new), hq) >= partial + copies
 
@@ -369,7 +369,7 @@ def test_long_ragged_batch_is_split_and_joined():
 
 
 @pytest.mark.parametrize("kind,page,d", [("e4m3", 16, 64), ("int8", 16, 128), ("e4m3", 32, 128), ("int8", 64, 64), ("e4m3", 128, 128), ("int8", 128, 128)])
-@pytest.mark.parametrize("hkv,group,new,before", [(4, 8, [128], [0]), (4, 8, [129, 0, 1], [70, 300, 5]), (8, 3, [300, 40, 257], [129, 0, 700])])
+@pytest.mark.parametrize("hkv,group,new,before", [(8, 8, [300], [0]), (8, 8, [257, 0, 1], [70, 300, 5]), (8, 6, [300, 40, 257], [129, 0, 300])])
 def test_attention_of_long_chunks(kind, page, d, hkv, group, new, before):
     w = World(71, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
     assert goes_by_copies(w, new, hkv * group)
@@ -385,19 +385,21 @@ def test_attention_of_long_chunks(kind, page, d, hkv, group, new, before):
     assert torch.equal(o1, o2) and torch.equal(lse1, lse2)
 
 
-def test_many_rows_without_copies():
-    """More rows than a tile per KV head, few enough in all that no copies are made."""
-    w = World(74, "e4m3", 32, 1, 128, [700]).fill().up()
-    assert not goes_by_copies(w, [200], 2)
-    q, o, lse, rows = attend(w, [200], 2, accumulate=True)
+@pytest.mark.parametrize("kind,page,hkv,d", CASES)
+@pytest.mark.parametrize("group,new,before", [(1, [33, 0, 128], [0, 40, 500]), (4, [9, 1, 31, 0], [1500, 3, 130, 64]), (2, [200], [500]), (8, [16, 16, 1], [127, 5, 2000])])
+def test_many_rows_without_copies(kind, page, hkv, d, group, new, before):
+    """More than 32 rows per KV head, up to and beyond a tile of 128, few enough in all that no copies are made."""
+    w = World(74, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    assert not goes_by_copies(w, new, hkv * group)
+    q, o, lse, rows = attend(w, new, hkv * group, accumulate=True)
     r = R.attention(w.state(), w.table, w.length, w.off, f64(q)[:rows])
     check_attn(w, None, r, o, lse, rows)
 
 
 def test_chunk_of_a_wide_table_is_captured_and_replayed():
     """Lengths of a captured chunk change; the table is far wider than the sequences."""
-    w = World(72, "e4m3", 32, 4, 64, [500, 400], width=64).fill().up()
-    hq, rows = 16, 300
+    w = World(72, "e4m3", 32, 8, 64, [500, 400], width=64).fill().up()
+    hq, rows = 32, 300
     length, off = dev([0, 0]), dev([0, 0, 0])
     q = torch.zeros(rows, hq, 64, dtype=torch.bfloat16, device="cuda")
     o, lse = torch.zeros_like(q), torch.zeros(rows, hq, device="cuda")
@@ -429,7 +431,7 @@ def test_chunk_of_a_wide_table_is_captured_and_replayed():
 def test_chunks_with_sequences_that_need_care(kind):
     """In one call with ordinary sequences: a NaN among the new values, more rows than tokens, a page that does not exist, lengths
     that make no sense."""
-    new, hkv, group = [140, 150, 133, 20, 200], 4, 2
+    new, hkv, group = [140, 150, 133, 20, 200], 4, 8
     w = World(73, kind, 16, hkv, 64, [300, 90, 200, 100, 260]).fill()
     if kind == "e4m3":
         w.codes["v"][w.table[0][290 // 16], 1, 290 % 16, 7] = 0xff
@@ -486,7 +488,7 @@ def test_rows_that_see_nothing():
     assert np.isfinite(added).all() and math.isclose(added.sum(), 4 * 3, rel_tol=1e-5)
 
 
-@pytest.mark.parametrize("new", [1, 6, 40])
+@pytest.mark.parametrize("new", [1, 6, 12, 40])
 def test_nan_values_behind_and_among_the_new_tokens(new):
     """What no row may see must not reach it: stale NaN codes behind the length, and a NaN key or value of a later new token."""
     w = World(26, "e4m3", 16, 1, 128, [117 + new, 64 + new]).fill()
