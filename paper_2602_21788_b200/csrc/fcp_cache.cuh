@@ -1132,11 +1132,12 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
 // ---------------------------------------------------------------------------------------------
 // From 33 rows per KV head on the products go to tcgen05: eight warps turn a tile's codes into halves in shared memory, once for
 // all rows, S = Q K^T and O += P V run on 128 rows whether they are all there or not (1024 clk per tile of 128 keys, D = 128), and
-// eight warps keep the softmax, half a row per thread, with P and O in tensor memory.  A tile takes 4400 to 5000 clk: bound by the chain
-// codes - halves - S - softmax - P - O with its hand-overs between warps and by shared memory (codes in, halves out, halves into the
-// products), not by the products.  16 sequences of 4K to 32K tokens, 40/8 heads, int8: 253 us for 35 rows, 270 us for 125 rows per KV head
-// (404 TFLOP/s); cache_attn_kernel took 323 and 602.  Four converting warps for K and four for V were slower than eight for both (142
-// against 111 us, 4 sequences, 64 new tokens); a second buffer for K's halves in place of a third stage changed nothing.
+// eight warps keep the softmax, half a row per thread, with P and O in tensor memory.  A tile takes about 4500 clk, bound by the
+// softmax warps' chain from S to P (measured with clocks in the kernel: scores out of tensor memory 1100 to 1400, since the products
+// before run meanwhile; maximum and meeting the other half 1500; weights and P 1700), not by the products or the bytes.  16 sequences of 4K to
+// 32K tokens, 40/8 heads, int8: 222 us for 35 rows, 245 us for 125 rows per KV head; cache_attn_kernel took 323 and 602.
+// Tried: V's halves in one buffer 253 (35 rows); masking rows that do not exist 245; four converting warps for K and four for V
+// (4 sequences, 64 new tokens) 142 against 111; the next scores fetched before P is handed over 232.
 //   warps 0..7    codes -> halves: queries at the start of a group, K of tile t, V of tile t - 1
 //   warps 8, 9    the loading warps above
 //   warp 10       issues the products: S of tile t, then O += P V of tile t - 1
@@ -1149,10 +1150,10 @@ constexpr int TILE_RING = 8;                          // what goes with a tile: 
 constexpr int TILE_GROUPS = 4;
 template <int D>
 struct TileSmem {
-  // codes of K and of V in rings of their own; halves of a tile of K, one of V, and the queries
-  static constexpr int TILE = CT_KEYS * D, STAGE = TILE, STAGES = D == 64 ? 6 : 3, QUERY_BYTES = 0;
+  // codes of K and of V in rings of their own; halves of a tile of K, of two of V in turn, and the queries
+  static constexpr int TILE = CT_KEYS * D, STAGE = TILE, STAGES = D == 64 ? 5 : 2, QUERY_BYTES = 0;
   static constexpr int RING = STAGES * STAGE, HALVES = 128 * D * 2;
-  static constexpr int DYN_BYTES = 2 * RING + 3 * HALVES + 1024;
+  static constexpr int DYN_BYTES = 2 * RING + 4 * HALVES + 1024;
 };
 struct TileMeta {
   int32_t flags, key0, row0, n, length, head, row_tile, part;
@@ -1187,7 +1188,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   using S = TileSmem<D>;
   constexpr uint32_t S_COL = 0, P_COL = 256, O_COL = 384;      // P: 64 columns for every other tile
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t bars[4 * S::STAGES + 18];
+  __shared__ __align__(8) uint64_t bars[4 * S::STAGES + 19];
   __shared__ __align__(16) StageMeta stages[S::STAGES];
   __shared__ __align__(16) TileMeta tiles[TILE_RING];
   __shared__ TileGroup groups[TILE_GROUPS];
@@ -1200,25 +1201,25 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t full = smem_u32(bars), empty = full + 2 * S::STAGES * 8, bar0 = empty + 2 * S::STAGES * 8;         // K's, then V's
   // two of each but one, for even and odd tiles: a waiter may be two tiles behind, which one phase bit does not tell
-  const uint32_t v_full = bar0, k_full = bar0 + 8, k_free = bar0 + 24, s_full = bar0 + 40, s_free = bar0 + 56, p_full = bar0 + 72, pv_done = bar0 + 88;
-  ConsumerSync sync = {bar0 + 104, 0};
-  const uint32_t pair = bar0 + 112;                   // the two softmax warps of a quarter, four times
+  const uint32_t v_full = bar0, k_full = bar0 + 16, k_free = bar0 + 32, s_full = bar0 + 48, s_free = bar0 + 64, p_full = bar0 + 80, pv_done = bar0 + 96;
+  ConsumerSync sync = {bar0 + 112, 0};
+  const uint32_t pair = bar0 + 120;                   // the two softmax warps of a quarter, four times
   const uint32_t skip = (1024u - (smem_u32(smem) & 1023u)) & 1023u;
   uint8_t* ring = smem + skip;
   uint8_t* k16 = ring + 2 * S::RING;
   uint8_t* v16 = k16 + S::HALVES;
-  uint8_t* q16 = v16 + S::HALVES;
+  uint8_t* q16 = v16 + 2 * S::HALVES;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < 2 * S::STAGES; ++i) {
       mbar_init(full + i * 8, 1);
       mbar_init(empty + i * 8, TILE_CONVERT);
     }
-    mbar_init(v_full, TILE_CONVERT);
     mbar_init(sync.bar, TILE_CONVERT);
     for (int i = 0; i < 4; ++i) mbar_init(pair + i * 8, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(k_full + i * 8, TILE_CONVERT);
+      mbar_init(v_full + i * 8, TILE_CONVERT);
       mbar_init(k_free + i * 8, 1);
       mbar_init(p_full + i * 8, 8);
       mbar_init(pv_done + i * 8, 2);
@@ -1293,7 +1294,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
             const float up = __uint_as_float((uint32_t)(262 - e) << 23);
             if (lane == 0) {
               grp.factor[r] = A.scale_log2 * __uint_as_float((uint32_t)(e - 8) << 23);
-              grp.limit[r] = row < n_rows ? meta.length - meta.n + j + 1 : 0;
+              grp.limit[r] = min(meta.length - meta.n + j + 1, next_most);       // rows that do not exist mask nothing
             }
             const uint32_t h0 = pack_half(bf_lo(x.x) * up, bf_hi(x.x) * up), h1 = pack_half(bf_lo(x.y) * up, bf_hi(x.y) * up);
             if (D == 128)
@@ -1318,7 +1319,8 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
       if (t > 0) {
         // V of the tile before
         if (!mbar_wait_warp(full + (S::STAGES + v_stage) * 8, v_phase, ctx, 945)) break;
-        if (t > 1 && !mbar_wait_warp(pv_done + (t & 1) * 8, ((t - 2) >> 1) & 1, ctx, 943)) break;
+        if (t > 2 && !mbar_wait_warp(pv_done + ((t - 3) & 1) * 8, ((t - 3) >> 1) & 1, ctx, 943)) break;
+        uint8_t* half = v16 + ((t - 1) & 1) * S::HALVES;
         const uint8_t* raw = ring + S::RING + v_stage * S::STAGE;
         uint32_t all[PER][4];
 #pragma unroll
@@ -1328,7 +1330,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
           const int r = warp * KEYS + (i * 32 + lane) / C, c = lane % C, pos = v_key0 + r;
           uint32_t (&w)[4] = all[i];
           if (v_key0 + CT_KEYS <= v_least && v_scale != 0.f) {       // every row sees every key of the tile
-            put_halves<D, KIND>(v16, r, c, w);
+            put_halves<D, KIND>(half, r, c, w);
             continue;
           }
           // what no row sees is whatever the page held, and must not meet a zero weight; nor must a NaN that some rows see
@@ -1346,12 +1348,12 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
               groups[v_seg % TILE_GROUPS].nan_any = 1;
             }
           }
-          put_halves<D, KIND>(v16, r, c, w);
+          put_halves<D, KIND>(half, r, c, w);
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(v_full);
+          mbar_arrive(v_full + ((t - 1) & 1) * 8);
           mbar_arrive(empty + (S::STAGES + v_stage) * 8);
         }
         if (++v_stage == S::STAGES) {
@@ -1390,10 +1392,10 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
         if (lane == 0) mbar_arrive(s_full + (t & 1) * 8);      // passes on what the converting warps wrote about the tile
       }
       if (t > 0) {
-        if (!mbar_wait_warp(v_full, (t - 1) & 1, ctx, 954)) break;
+        if (!mbar_wait_warp(v_full + ((t - 1) & 1) * 8, ((t - 1) >> 1) & 1, ctx, 954)) break;
         if (!mbar_wait_warp(p_full + ((t - 1) & 1) * 8, ((t - 1) >> 1) & 1, ctx, 955)) break;
         tc_fence_after();
-        umma_loop_ts<0, 8>(tmem + O_COL, tmem + P_COL + ((t - 1) & 1) * 64, false, smem_u32(v16), IDESC_PV, before & ST_FIRST ? 0u : 1u);
+        umma_loop_ts<0, 8>(tmem + O_COL, tmem + P_COL + ((t - 1) & 1) * 64, false, smem_u32(v16) + ((t - 1) & 1) * S::HALVES, IDESC_PV, before & ST_FIRST ? 0u : 1u);
         tc_commit(pv_done + ((t - 1) & 1) * 8);
         if (lane == 0) mbar_arrive(pv_done + ((t - 1) & 1) * 8);
       }
