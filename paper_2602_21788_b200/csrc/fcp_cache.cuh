@@ -1132,12 +1132,12 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
 // ---------------------------------------------------------------------------------------------
 // From 33 rows per KV head on the products go to tcgen05: eight warps turn a tile's codes into halves in shared memory, once for
 // all rows, S = Q K^T and O += P V run on 128 rows whether they are all there or not (1024 clk per tile of 128 keys, D = 128), and
-// eight warps keep the softmax, half a row per thread, with P and O in tensor memory.  A tile takes about 4500 clk, bound by the
-// softmax warps' chain from S to P (measured with clocks in the kernel: scores out of tensor memory 1100 to 1400, since the products
-// before run meanwhile; maximum and meeting the other half 1500; weights and P 1700), not by the products or the bytes.  16 sequences of 4K to
-// 32K tokens, 40/8 heads, int8: 222 us for 35 rows, 245 us for 125 rows per KV head; cache_attn_kernel took 323 and 602.
-// Tried: V's halves in one buffer 253 (35 rows); masking rows that do not exist 245; four converting warps for K and four for V
-// (4 sequences, 64 new tokens) 142 against 111; the next scores fetched before P is handed over 232.
+// eight warps keep the softmax, half a row per thread, with P and O in tensor memory.  A tile takes about 4400 clk, neither the products'
+// nor the bytes' time: the converting warps (3000), the softmax warps' way from S to P and the products wait for one another.  16
+// sequences of 4K to 32K tokens, 40/8 heads, int8: 222 us for 35 rows, 242 us for 125 rows per KV head; cache_attn_kernel took 323 and 602.
+// Tried, us for 35 rows: V's halves in one buffer 253; masking rows that do not exist 245; the next scores fetched before P is handed
+// over 232; even and odd tiles to four softmax warps each, with an output of their own, 264.  Four converting warps for K and four
+// for V took 142 against 111 (4 sequences, 64 new tokens).
 //   warps 0..7    codes -> halves: queries at the start of a group, K of tile t, V of tile t - 1
 //   warps 8, 9    the loading warps above
 //   warp 10       issues the products: S of tile t, then O += P V of tile t - 1
