@@ -445,7 +445,7 @@ typedef struct fcp_cache_batch {
   int32_t B;                         /* sequences                                              */
   int32_t rows;                      /* rows of the call's tensors                             */
   int32_t max_new;                   /* no sequence has more new tokens than this              */
-  int32_t table_width;               /* columns of page_table                                  */
+  int32_t table_width;               /* columns of page_table; times page_tokens <= 2^31 - 256 */
   const int32_t* page_table;         /* device [B][table_width]                                */
   const int32_t* length;             /* device [B]                                             */
   const int32_t* row_offset;         /* device [B+1]                                           */
@@ -477,9 +477,9 @@ int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const
  * query heads of its KV head (what fcp_cache_evict goes by).
  * workspace: device, 256-byte aligned, of at least fcp_cache_attn_workspace_bytes; its contents need not be initialised; two calls
  * that may overlap on the GPU, also two captured ones, need one each.
- * Scores, statistics and sums are fp32; the weights of the values are rounded to halves, and in calls with many new tokens, which go
- * through bf16 copies of the codes in the workspace (up to 8 GB, where that is faster), to bf16, as is code * scale where a
- * scale is no power of two.  The same call gives the same bits again, unless sequences of one call share a page and accumulate.
+ * Scores, statistics and sums are fp32; the weights of the values are rounded to halves (a weight times its value scale to 0 below
+ * 2^-33 of the row's largest), and in calls with many new tokens, which go through bf16 copies of the codes in the workspace (up to
+ * 8 GB, where that is faster), to bf16, as is code * scale where a scale is no power of two.  The same call gives the same bits again, unless sequences of one call share a page and accumulate.
  */
 int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t hq, int64_t* bytes);
 int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const void* q, int64_t q_stride, int32_t hq,

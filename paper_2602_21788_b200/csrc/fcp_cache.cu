@@ -74,7 +74,8 @@ int check_batch(const char* call, const fcp_cache* cache, const fcp_cache_batch*
     fcp_set_error("%s: NULL cache or batch", call);
     return FCP_ERR_INVALID_ARG;
   }
-  if (b->B < 0 || b->table_width < 1 || (int64_t)b->table_width * cache->config.page_tokens >= int64_t(1) << 31 ||
+  // positions, and those of the ends of the tiles that hold them, stay below 2^31
+  if (b->B < 0 || b->table_width < 1 || (int64_t)b->table_width * cache->config.page_tokens > (int64_t(1) << 31) - 2 * CT_KEYS ||
       (b->B > 0 && (!b->page_table || !b->length))) {
     fcp_set_error("%s: B %d, table_width %d, or a NULL page_table or length", call, b->B, b->table_width);
     return FCP_ERR_INVALID_ARG;

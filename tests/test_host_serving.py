@@ -143,7 +143,7 @@ def test_cache_calls_that_are_refused():
         return L.fcp_cache_evict(hh, b, sink, heavy, recent, dst, width, new, kept, None)
     for call in (append, attn, evict):
         assert call(hh=None) == -1 and call(b=None) == -1
-        for more in (dict(B=-1), dict(table_width=0), dict(table_width=1 << 27), dict(page_table=None), dict(length=None)):
+        for more in (dict(B=-1), dict(table_width=0), dict(table_width=1 << 27), dict(table_width=(1 << 27) - 15), dict(page_table=None), dict(length=None)):
             assert call(b=batch(**more)) == -1, more
         assert call(b=batch(B=0)) == 0
     for call in (append, attn):
