@@ -23,7 +23,7 @@ namespace {
 
 // Row tiles in blocks of 8 rows: the smallest that holds a KV head's rows.  1, 2 and 4 blocks go by cache_attn_kernel, whose time grows
 // with the rows, 16 by cache_tile_kernel, whose time does not.  16 sequences of 4K to 32K tokens, 40/8 heads, int8, us, the one against the
-// other: 25 rows per KV head 189, 218; 35 rows (8 blocks) 323, 222; 100 rows (16 blocks) 599, 236.
+// other: 25 rows per KV head 189, 218; 35 rows (8 blocks) 323, 224; 100 rows (16 blocks) 599, 239.
 constexpr int kWeights = 0;
 int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 ? 4 : TILE_ROWS / 8; }
 

@@ -1132,18 +1132,20 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
 // ---------------------------------------------------------------------------------------------
 // From 33 rows per KV head on the products go to tcgen05: eight warps turn a tile's codes into halves in shared memory, once for
 // all rows, S = Q K^T and O += P V run on 128 rows whether they are all there or not (1024 clk per tile of 128 keys, D = 128), and
-// eight warps keep the softmax, half a row per thread, with P and O in tensor memory.  A tile takes about 4400 clk, neither the products'
-// nor the bytes' time: the converting warps (3000), the softmax warps' way from S to P and the products wait for one another.  16
-// sequences of 4K to 32K tokens, 40/8 heads, int8: 222 us for 35 rows, 242 us for 125 rows per KV head; cache_attn_kernel took 323 and 602.
-// Tried, us for 35 rows: V's halves in one buffer 253; masking rows that do not exist 245; the next scores fetched before P is handed
-// over 232; even and odd tiles to four softmax warps each, with an output of their own, 264.  Four converting warps for K and four
-// for V took 142 against 111 (4 sequences, 64 new tokens).
+// sixteen warps keep the softmax, a quarter of a row per thread, with P and O in tensor memory.  A tile takes about 4400 clk, neither
+// the products' nor the bytes' time: codes to halves (2000 to 3000 clk), the softmax warps' way from S to P (of it 1000 for the
+// exponentials) and the products wait for one another.  16 sequences of 4K to 32K tokens, 40/8 heads, us: 224 for 35 rows, 239 for 100 rows
+// per KV head with int8, 228 with e4m3; cache_attn_kernel took 323 and 599 with int8.
+// Tried, with eight softmax warps: as it stands, 222, 236 and 247 us; V's halves in one buffer 253 for 35 rows; masking rows that do not
+// exist 245; the next scores fetched before P is handed over 232; even and odd tiles to four softmax warps each, with an output of
+// their own, 264; polling in front of waits 228; halves made before their place is free 221, e4m3 249.  Four converting warps for K
+// and four for V took 142 against 111 (4 sequences, 64 new tokens).
 //   warps 0..7    codes -> halves: queries at the start of a group, K of tile t, V of tile t - 1
 //   warps 8, 9    the loading warps above
 //   warp 10       issues the products: S of tile t, then O += P V of tile t - 1
-//   warps 12..19  softmax and output: two per quarter of the tensor memory's lanes, each with half of a tile's columns
+//   warps 12..27  softmax and output: four per quarter of the tensor memory's lanes, each with 32 of a tile's columns
 // Tensor memory: S of two tiles in turn | P of two tiles | O.
-constexpr int TILE_THREADS = 640;
+constexpr int TILE_THREADS = 896;
 constexpr int TILE_ROWS = 128;
 constexpr int TILE_CONVERT = 8;                       // converting warps
 constexpr int TILE_RING = 8;                          // what goes with a tile: nobody is more than four behind; with a group: three
@@ -1196,14 +1198,14 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
   __shared__ uint16_t nans[NANS ? TILE_GROUPS : 1][NANS ? 128 : 1][D / 16];       // columns that are NaN in the keys from `least` on
   __shared__ int64_t scratch[16];
   __shared__ int abort_flag;
-  __shared__ float tops[2][2][TILE_ROWS], sums[2][TILE_ROWS];
+  __shared__ float tops[2][4][TILE_ROWS], sums[4][TILE_ROWS];
   __shared__ uint32_t tmem_slot;
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t full = smem_u32(bars), empty = full + 2 * S::STAGES * 8, bar0 = empty + 2 * S::STAGES * 8;         // K's, then V's
   // two of each but one, for even and odd tiles: a waiter may be two tiles behind, which one phase bit does not tell
   const uint32_t v_full = bar0, k_full = bar0 + 16, k_free = bar0 + 32, s_full = bar0 + 48, s_free = bar0 + 64, p_full = bar0 + 80, pv_done = bar0 + 96;
   ConsumerSync sync = {bar0 + 112, 0};
-  const uint32_t pair = bar0 + 120;                   // the two softmax warps of a quarter, four times
+  const uint32_t quartet = bar0 + 120;                // the four softmax warps of a quarter, four times
   const uint32_t skip = (1024u - (smem_u32(smem) & 1023u)) & 1023u;
   uint8_t* ring = smem + skip;
   uint8_t* k16 = ring + 2 * S::RING;
@@ -1216,15 +1218,15 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
       mbar_init(empty + i * 8, TILE_CONVERT);
     }
     mbar_init(sync.bar, TILE_CONVERT);
-    for (int i = 0; i < 4; ++i) mbar_init(pair + i * 8, 2);
+    for (int i = 0; i < 4; ++i) mbar_init(quartet + i * 8, 4);
     for (int i = 0; i < 2; ++i) {
       mbar_init(k_full + i * 8, TILE_CONVERT);
       mbar_init(v_full + i * 8, TILE_CONVERT);
       mbar_init(k_free + i * 8, 1);
-      mbar_init(p_full + i * 8, 8);
+      mbar_init(p_full + i * 8, 16);
       mbar_init(pv_done + i * 8, 2);
       mbar_init(s_full + i * 8, 2);
-      mbar_init(s_free + i * 8, 8);
+      mbar_init(s_free + i * 8, 16);
     }
     fence_mbar_init();
     prefetch_tmap(&tk);
@@ -1408,9 +1410,9 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
     }
   } else if (warp >= 12) {
     // ------------------------------------------------------------------ softmax
-    const int quarter = warp & 3, half = (warp - 12) >> 2, row = quarter * 32 + lane;
-    const uint32_t t_o = tmem_addr(tmem, quarter * 32, O_COL + half * (D / 2));
-    ConsumerSync both = {pair + quarter * 8, 0};
+    const int quarter = warp & 3, part = (warp - 12) >> 2, row = quarter * 32 + lane;
+    const uint32_t t_o = tmem_addr(tmem, quarter * 32, O_COL + part * (D / 4));
+    ConsumerSync all = {quartet + quarter * 8, 0};
     float factor = 0.f, ref = -3e38f, l = 0.f;
     int limit = 0, seg = -1;
     bool there = false, begun = false;                // these warps have rows; O holds something of this group
@@ -1429,19 +1431,18 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
         l = 0.f;
         begun = false;
       }
-      uint32_t x[64];                                 // this warp's half of the row's scores
+      uint32_t x[32];                                 // this warp's part of the row's scores
       float top = -INFINITY;
-      const int seen = limit - meta.key0 - 64 * half; // columns of the half that the row sees
-      const bool edge = __any_sync(0xffffffffu, seen < 64);
+      const int seen = limit - meta.key0 - 32 * part; // columns of the part that the row sees
+      const bool edge = __any_sync(0xffffffffu, seen < 32);
       if (there) {
-        const uint32_t t_s = tmem_addr(tmem, quarter * 32, S_COL + (t & 1) * 128 + 64 * half);
-        tmem_ld32(t_s, *reinterpret_cast<uint32_t(*)[32]>(x));
-        tmem_ld32(t_s + 32, *reinterpret_cast<uint32_t(*)[32]>(x + 32));
+        const uint32_t t_s = tmem_addr(tmem, quarter * 32, S_COL + (t & 1) * 128 + 32 * part);
+        tmem_ld32(t_s, x);
         tc_wait_ld(x);
         // a = score in log2 units plus log2 of the value scale, as in AttnConsumer
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const float4 about = meta.sub[4 * half + h];
+        for (int h = 0; h < 2; ++h) {
+          const float4 about = meta.sub[2 * part + h];
           if (edge || about.x == 0.f) {
             const int n = about.x == 0.f ? 0 : seen - 16 * h;
 #pragma unroll
@@ -1456,7 +1457,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
           }
           if (about.x != 0.f) top = fmaxf(top, fmaf(fmaxf(m0, m1), fmaxf(factor * about.x, 1.2e-38f), about.y));
         }
-        tops[t & 1][half][row] = top;
+        tops[t & 1][part][row] = top;
       }
       tc_fence_before();
       __syncwarp();
@@ -1464,10 +1465,10 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
       // this tile's place for P is free.  Warps without rows wait too, so that none arrives twice in one phase of p_full.
       if (t > 1 && !mbar_wait_warp(pv_done + (t & 1) * 8, ((t - 2) >> 1) & 1, ctx, 962)) break;
       if (there) {
-        if (!both(ctx, lane, 965)) break;
-        top = fmaxf(top, tops[t & 1][half ^ 1][row]);
+        if (!all(ctx, lane, 965)) break;
+        top = fmaxf(fmaxf(tops[t & 1][0][row], tops[t & 1][1][row]), fmaxf(tops[t & 1][2][row], tops[t & 1][3][row]));
         tc_fence_after();
-        if (__any_sync(0xffffffffu, top > ref + 15.f)) {       // the same in both warps
+        if (__any_sync(0xffffffffu, top > ref + 15.f)) {       // the same in all four warps
           const float m = top > ref + 15.f ? top - 8.f : ref, shrink = exp2_approx(ref - m);
           l *= shrink;
           ref = m;
@@ -1475,7 +1476,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
             if (!mbar_wait_warp(pv_done + ((t - 1) & 1) * 8, ((t - 1) >> 1) & 1, ctx, 963)) break;
             tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = 0; c < D / 64; ++c) {
               uint32_t o[16];
               tmem_ld16(t_o + 16 * c, o);
               tc_wait_ld(o);
@@ -1485,27 +1486,24 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
             }
           }
         }
+        uint32_t p[16];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t p[16];
+        for (int h = 0; h < 2; ++h) {
+          const float4 about = meta.sub[2 * part + h];
+          const bool is = about.x != 0.f;             // else the scores are -infinity whatever they are multiplied by
+          const float f = is ? fmaxf(factor * about.x, 1.2e-38f) : 1.f, shift = about.y - ref;        // not 0: times -infinity
+          float z0 = 0.f, z1 = 0.f;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float4 about = meta.sub[4 * half + 2 * c + h];
-            const bool is = about.x != 0.f;           // else the scores are -infinity whatever they are multiplied by
-            const float f = is ? fmaxf(factor * about.x, 1.2e-38f) : 1.f, shift = about.y - ref;      // not 0: times -infinity
-            float z0 = 0.f, z1 = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int e = 32 * c + 16 * h + 2 * i;
-              const float a = exp2_approx(fmaf(__uint_as_float(x[e]), f, shift)), b = exp2_approx(fmaf(__uint_as_float(x[e + 1]), f, shift));
-              z0 += a;
-              z1 += b;
-              p[8 * h + i] = pack_half(a, b);
-            }
-            l = fmaf(z0 + z1, about.z, l);
+          for (int i = 0; i < 8; ++i) {
+            const int e = 16 * h + 2 * i;
+            const float a = exp2_approx(fmaf(__uint_as_float(x[e]), f, shift)), b = exp2_approx(fmaf(__uint_as_float(x[e + 1]), f, shift));
+            z0 += a;
+            z1 += b;
+            p[8 * h + i] = pack_half(a, b);
           }
-          tmem_st16(tmem_addr(tmem, quarter * 32, P_COL + (t & 1) * 64 + half * 32 + 16 * c), p);
+          l = fmaf(z0 + z1, about.z, l);
         }
+        tmem_st16(tmem_addr(tmem, quarter * 32, P_COL + (t & 1) * 64 + 16 * part), p);
         tc_wait_st();
         begun = true;
       }
@@ -1514,22 +1512,22 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
       if (lane == 0) mbar_arrive(p_full + (t & 1) * 8);
       if (flags & ST_LAST) {
         if (there) {
-          sums[half][row] = l;
-          if (!both(ctx, lane, 966)) break;
-          const float z = sums[0][row] + sums[1][row];
+          sums[part][row] = l;
+          if (!all(ctx, lane, 966)) break;
+          const float z = (sums[0][row] + sums[1][row]) + (sums[2][row] + sums[3][row]);
           if (!mbar_wait_warp(pv_done + (t & 1) * 8, (t >> 1) & 1, ctx, 964)) break;
           tc_fence_after();
           const int gr = meta.row_tile * TILE_ROWS + row, j = gr / A.group;
           const bool is = gr < meta.n * A.group;
           const float inverse = z == 0.f ? 0.f : 1.f / z, lse2 = z == 0.f ? -INFINITY : ref + __log2f(z);
-          const int64_t out = (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + gr - j * A.group, part = (int64_t)meta.part * TILE_ROWS + row;
+          const int64_t out = (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + gr - j * A.group, place = (int64_t)meta.part * TILE_ROWS + row;
           const TileGroup& grp = groups[seg % TILE_GROUPS];
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {          // this warp's half of the columns
+          for (int c = 0; c < D / 64; ++c) {          // this warp's part of the columns
             uint32_t o[16];
             tmem_ld16(t_o + 16 * c, o);
             tc_wait_ld(o);
-            const int col = half * (D / 32) + c;
+            const int col = part * (D / 64) + c;
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(z == 0.f ? 0.f : __uint_as_float(o[i]) * inverse);
             if (NANS && grp.nan_any) {
@@ -1548,14 +1546,14 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
               dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
               dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
             } else {
-              uint4* dst = reinterpret_cast<uint4*>(A.part_o + part * D + 16 * col);
+              uint4* dst = reinterpret_cast<uint4*>(A.part_o + place * D + 16 * col);
 #pragma unroll
               for (int i = 0; i < 4; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             }
           }
-          if (is && half == 0) {
+          if (is && part == 0) {
             if (flags & ST_WHOLE) A.lse[out] = lse2 * 0.69314718055994531f;
-            else A.part_lse[part] = lse2;
+            else A.part_lse[place] = lse2;
           }
           tc_fence_before();                          // O is free for the next group with this warp's next arrival at p_full
         }
