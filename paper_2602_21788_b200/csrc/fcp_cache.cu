@@ -171,8 +171,9 @@ int64_t chunk_stride(const fcp_cache_config& c, const fcp_cache_batch& b) {
 // Whether a call goes through bf16 copies and the packed attention: where that takes less time by a third by what both were measured to
 // take, in clk of the device per tile of 128 keys.  cache_tile_kernel: 4800 per KV head and 128 rows, spread over all SMs.  The other way:
 // 5900 per KV head for the copies; fcp_fwd_kernel takes 1700 per query head and tile of 128 new tokens, 1270 where two run beside
-// each other, and no item is cut along the keys.  4 sequences of 6K to 12K tokens, 32/8 heads, us, copies against not: 512 new
-// tokens 291, 535; 256 232, 290; 128 185, 172; 64 194, 110.  The copies may take up to 8 GB.
+// each other, and no item is cut along the keys.  4 sequences of 6K to 12K tokens, 32/8 heads, int8, us, copies against not: 512 new
+// tokens 294, 541; 256 235, 291; 192 244, 229 (goes by copies); 128 188, 171; 64 196, 110; one sequence, 256 165, 128.  The copies may
+// take up to 8 GB.
 constexpr int64_t kChunkBytes = int64_t(8) << 30;
 bool in_chunks(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq) {
   const int64_t tokens = b.B * chunk_stride(c, b), units = (int64_t)b.B * ((b.max_new + FCP_FWD_UNIT_ROWS - 1) / FCP_FWD_UNIT_ROWS);
