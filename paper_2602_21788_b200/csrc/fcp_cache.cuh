@@ -293,6 +293,18 @@ constexpr int CT_WARPS = 8;                           // consumer warps; two mor
 constexpr int CT_THREADS = (CT_WARPS + 2) * 32;
 constexpr int WEIGHT_CTAS = 2;                        // per SM, of the kernel that adds up weights
 
+// What goes with 16 keys: key scale (0: absent), log2 and inverse of the value scale, and for the weights' kernel the row of the
+// first code (bits), for the others a power of two that the weights are multiplied by before they meet the values.
+// The sum of the probabilities is kept as weights over value scales, and a weight stands at up to 2^15.  With the smallest scale, 2^-100,
+// which a page of zeros has, 2^13 keys at 2^15 already sum to infinity; so a scale below 2^-80 counts 2^n times as much, enough
+// for 2^-80, and its weights 2^-n times: 2^31 keys then sum to 2^126 at most.  Scales of up to 2^122 keep their sum above 2^-114.
+constexpr int CT_LEAST_EXPONENT = 127 - 80;           // biased, of 2^-80
+__device__ __forceinline__ float4 about_keys(float ks, float vs, int32_t row, bool weights) {
+  const int up = max(0, CT_LEAST_EXPONENT - (int)(__float_as_uint(vs) >> 23));
+  const float s = __uint_as_float(__float_as_uint(vs) + ((uint32_t)up << 23));
+  return make_float4(ks, __log2f(s), 1.f / s, weights ? __int_as_float(row) : __uint_as_float((uint32_t)(127 - up) << 23));
+}
+
 struct AttnArgs {
   CacheView c;
   BatchView s;
@@ -311,8 +323,7 @@ struct AttnArgs {
 struct StageMeta {                                    // what a stage holds, for the consumers
   int32_t row0, n, length, head;                      // of the sequence and group
   int32_t row_tile, key0, flags, part;
-  // per 16 keys: key scale (0: absent), log2 and inverse of the value scale, row of the first code (bits)
-  float4 sub[CT_KEYS / 16];
+  float4 sub[CT_KEYS / 16];                           // about_keys of each 16
 };
 enum { ST_FIRST = 1, ST_LAST = 2, ST_WHOLE = 4, ST_END = 8 };
 enum { SP_COUNT = 0, SP_ROW0, SP_N, SP_HEAD, SP_ROW_TILE, SP_W = 8 };
@@ -671,7 +682,7 @@ struct AttnProducer {
         now.row = -1;
       }
       const bool usable = now.row >= 0;
-      const float4 about = usable ? make_float4(now.ks, __log2f(now.vs), 1.f / now.vs, __int_as_float(now.row)) : make_float4(0.f, 0.f, 1.f, 0.f);
+      const float4 about = usable ? about_keys(now.ks, now.vs, now.row, WEIGHTS) : make_float4(0.f, 0.f, 1.f, 1.f);
       for (int i = 0; i < now.tiles; ++i) {
         if (!mbar_wait_warp(empty + stage * 8, phase ^ 1, ctx, 911)) {
           ok = false;
@@ -759,6 +770,7 @@ struct AttnConsumer {
     // a = score in log2 units plus log2 of the value scale, so that 2^(a - ref) are the weights of the value codes, and the sum
     // of the probabilities is that of the weights over the value scale.  ref follows the largest a from 8 below it and is left
     // alone until a weight would pass 2^15: a half holds weights down to 2^-24, 2^-32 of the largest and less.
+    // (Value scales below 2^-80: about_keys.)
     const bool edge = key + 32 > least || about[0].x == 0.f || about[1].x == 0.f;
     float top[NR][2];
     bool high = false;
@@ -809,6 +821,10 @@ struct AttnConsumer {
         for (int c = 0; c < 4; ++c) s[h][i][c] = exp2_approx(s[h][i][c] - ref[i][c & 1]);
         l[i][0] = fmaf(s[h][i][0] + s[h][i][2], about[h].z, l[i][0]);
         l[i][1] = fmaf(s[h][i][1] + s[h][i][3], about[h].z, l[i][1]);
+        if (about[h].w != 1.f) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[h][i][c] *= about[h].w;
+        }
         p[h][i][0] = transpose8(pack_half(s[h][i][0], s[h][i][1]));
         p[h][i][1] = transpose8(pack_half(s[h][i][2], s[h][i][3]));
       }
@@ -1502,6 +1518,11 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
             p[8 * h + i] = pack_half(a, b);
           }
           l = fmaf(z0 + z1, about.z, l);
+          if (about.w != 1.f) {                       // a power of two from 2^-20 on
+            const __half2 down = __float2half2_rn(about.w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[8 * h + i] = h2_bits(__hmul2(*reinterpret_cast<const __half2*>(&p[8 * h + i]), down));
+          }
         }
         tmem_st16(tmem_addr(tmem, quarter * 32, P_COL + (t & 1) * 64 + 16 * part), p);
         tc_wait_st();

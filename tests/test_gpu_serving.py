@@ -871,3 +871,88 @@ def test_prompt_then_tokens_then_eviction(kind, d):
     same(w.now(), state)
     tokens(dev(dst), new_length.tolist(), 3)
     assert w.cache.device_status().tolist() == [0, 0, 0, 0]
+
+
+# ---------------------------------------------------------------------------------------------------------
+# Values and scales at the ends of their range
+# ---------------------------------------------------------------------------------------------------------
+def unit_code(kind):
+    """The code of 1."""
+    return 0x38 if kind == "e4m3" else 1
+
+
+def shared_batch(w, B):
+    """B sequences of one new token each, all on the pages of the first one."""
+    table = np.repeat(w.table[:1], B, axis=0)
+    return fcp.CacheBatch(dev(table), dev([int(w.length[0])] * B), dev(np.arange(B + 1)), rows=B, max_new=1)
+
+
+def attend_batch(w, batch, q, hq, scale=0.0, accumulate=False):
+    o, lse = torch.full((batch.rows, hq, w.d), 3.0, dtype=torch.bfloat16, device="cuda"), torch.full((batch.rows, hq), 5.0, device="cuda")
+    n = fcp.fcp_cache_attn_workspace_bytes(w.cache, batch, hq)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    fcp.fcp_cache_attn(w.cache, batch, q.cuda(), o, lse, ws, n, scale=scale, accumulate=accumulate, stream=stream())
+    torch.cuda.synchronize()
+    return o, lse
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("hq", [1, 10, 25, 40])
+@pytest.mark.parametrize("B", [1, 74, 148])
+def test_zero_values_and_scores_that_rise(kind, hq, B):
+    """A KV head whose values are all zero has pages of the smallest scale, 2^-100.  The first keys of every block's share have score 0,
+    the others 4.6875: the sum of the weights over the value scales has to stay finite.  Alone, two blocks a sequence, one block a sequence."""
+    T = 320 * 128
+    w = World(81, kind, 128, 1, 64, [T], spare=0)
+    low = np.zeros(T, bool)
+    low[:256] = low[159 * 128:161 * 128] = True
+    k = np.zeros((T, 64), np.uint8)
+    k[~low, 0] = unit_code(kind)
+    for i, p in enumerate(w.table[0]):
+        w.codes["k"][p, 0], w.codes["v"][p, 0] = k[i * 128:(i + 1) * 128], 0
+    w.scale["k"][:], w.scale["v"][:], w.weight[:] = 1.0, 2.0 ** -100, 0.0
+    w.up()
+    q = torch.zeros(B, hq, 64, dtype=torch.bfloat16)
+    q[..., 0] = 37.5                                              # times 1/8
+    o, lse = attend_batch(w, shared_batch(w, B), q, hq, accumulate=True)
+    s = np.where(low, 0.0, 4.6875)
+    want = 4.6875 + math.log(np.exp(s - 4.6875).sum())
+    # a thread adds at most T / 32 weights, one rounding each; the join of threads, warps and blocks a few hundred roundings more;
+    # scores are exact but for their place in log2 units (2^-23 of at most 16)
+    tol = (T / 32 + 300) * F32 + 16 * 2.0 ** -22
+    assert np.abs(f64(lse) - want).max() <= tol
+    assert bool((o == 0).all())
+    weight = f64(w.w)[w.table[0], 0].reshape(-1)
+    assert np.all(np.abs(weight / (B * hq * np.exp(s - want)) - 1) <= 2 * tol + (B + 64) * F32)
+
+
+@pytest.mark.parametrize("kind,page,d", [("e4m3", 16, 64), ("int8", 16, 128), ("int8", 128, 64), ("e4m3", 128, 128)])
+@pytest.mark.parametrize("new,hq", [(1, 3), (3, 4), (5, 5), (1, 40)])
+@pytest.mark.parametrize("top", [-100, -77, -3])
+def test_value_scales_down_to_the_smallest(kind, page, d, new, hq, top):
+    """Pages whose value scales, powers of two and others, lie between 2^-100 and 2^top."""
+    w = World(82, kind, page, 1, d, [2000, 5000]).fill()
+    exponent = np.minimum(-100 + w.rng.integers(0, 28, w.n_pages), top)
+    exponent[::9] = top
+    w.scale["v"][:, 0] = 2.0 ** exponent * np.where((exponent > -100) & (w.rng.random(w.n_pages) < 0.5), w.rng.uniform(0.75, 1.0, w.n_pages), 1.0)
+    w.up()
+    q, o, lse, rows = attend(w, [new, new], hq, spare=0)
+    state = w.state()
+    r = R.attention(state, w.table, w.length, w.off, f64(q))
+    # as in test_tiles_of_rows_that_see_nothing_or_differ_in_size, with scales below 2^-80 counted as up to 2^-79: every code is off by
+    # at most 2^-33 of the row's largest product of a weight and such a scale
+    lost = np.zeros((rows, hq, d))
+    for b in range(2):
+        t = w.length[b]
+        pages = np.asarray(w.table[b][:-(-t // page)])
+        k, code = R.gather(state, "k", pages, t, 0), state["v"][pages, 0].reshape(-1, d)[:t]
+        scale = np.maximum(np.repeat(state["v_scale"][pages, 0], page)[:t], 2.0 ** -79)
+        for j in range(new):
+            row, seen = w.off[b] + j, t - new + j + 1
+            for h in range(hq):
+                s = k[:seen] @ f64(q)[row, h] / math.sqrt(d)
+                lost[row, h] = 2.0 ** -33 * (np.exp(s - r["lse"][row, h]) * scale[:seen]).max() * np.abs(code[:seen]).sum(axis=0)
+    score = d * 2 * F32 * r["size"] + 2.0 ** -20
+    assert np.all(np.abs(f64(lse) - r["lse"]) <= score + 4 * F32 * np.abs(r["lse"]))
+    bound = BF16 * np.abs(r["o"]) + (HALF + 2 * score[..., None]) * r["spread"] * (1 + BF16) + lost
+    assert np.all(np.abs(f64(o) - r["o"]) <= bound), np.max(np.abs(f64(o) - r["o"]) / bound)
