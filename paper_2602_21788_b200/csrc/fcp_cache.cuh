@@ -305,6 +305,11 @@ __device__ __forceinline__ float4 about_keys(float ks, float vs, int32_t row, bo
   return make_float4(ks, __log2f(s), 1.f / s, weights ? __int_as_float(row) : __uint_as_float((uint32_t)(127 - up) << 23));
 }
 
+// A partial output may pass fp32's range where the whole one does not: an infinite value is stored as 448 * 2^120 or 127 * 2^122, and
+// its weight may be 1 among one CTA's keys and 0 among all.  Partial outputs are held 2^-12 times: their sum over 148 CTAs then
+// stays below 2^127, and the smallest bf16 keeps 11 bits.
+constexpr float CT_PART_UNIT = 0x1p-12f;
+
 struct AttnArgs {
   CacheView c;
   BatchView s;
@@ -944,7 +949,8 @@ struct AttnConsumer {
       }
       const float inverse = z == 0.f ? 0.f : 1.f / z;
       const float lse2 = z == 0.f ? -INFINITY : top + __log2f(z);
-      x.x *= inverse; x.y *= inverse; x.z *= inverse; x.w *= inverse;
+      const float unit = meta.flags & ST_WHOLE ? 1.f : CT_PART_UNIT;
+      x.x = x.x * unit * inverse; x.y = x.y * unit * inverse; x.z = x.z * unit * inverse; x.w = x.w * unit * inverse;
       if (meta.flags & ST_WHOLE) {
         const int gr = meta.row_tile * RT + r, j = gr / A.group;
         const int64_t out = (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + gr - j * A.group;
@@ -1541,6 +1547,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
           const int gr = meta.row_tile * TILE_ROWS + row, j = gr / A.group;
           const bool is = gr < meta.n * A.group;
           const float inverse = z == 0.f ? 0.f : 1.f / z, lse2 = z == 0.f ? -INFINITY : ref + __log2f(z);
+          const float unit = flags & ST_WHOLE ? 1.f : CT_PART_UNIT;
           const int64_t out = (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + gr - j * A.group, place = (int64_t)meta.part * TILE_ROWS + row;
           const TileGroup& grp = groups[seg % TILE_GROUPS];
 #pragma unroll 1
@@ -1550,7 +1557,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
             tc_wait_ld(o);
             const int col = part * (D / 64) + c;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(z == 0.f ? 0.f : __uint_as_float(o[i]) * inverse);
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(z == 0.f ? 0.f : __uint_as_float(o[i]) * unit * inverse);
             if (NANS && grp.nan_any) {
               uint32_t bits = 0;
               for (int k = 0; k < min(limit - grp.least, 128); ++k) bits |= nans[seg % TILE_GROUPS][k][col];
@@ -1635,7 +1642,8 @@ __global__ void __launch_bounds__(MERGE_THREADS) cache_merge_kernel(const __grid
     const float inverse = z == 0.f ? 0.f : 1.f / z;
     const int gr = first + r, j = gr / A.group;
     const int64_t out = (int64_t)(row0 + j) * A.hq + head * A.group + gr - j * A.group;
-    *reinterpret_cast<uint2*>(A.o + out * D + f * 4) = make_uint2(pack_bf16(x.x * inverse, x.y * inverse), pack_bf16(x.z * inverse, x.w * inverse));
+    x.x = x.x * inverse / CT_PART_UNIT; x.y = x.y * inverse / CT_PART_UNIT; x.z = x.z * inverse / CT_PART_UNIT; x.w = x.w * inverse / CT_PART_UNIT;
+    *reinterpret_cast<uint2*>(A.o + out * D + f * 4) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
     if (f == 0) A.lse[out] = z == 0.f ? -INFINITY : (ref + __log2f(z)) * 0.69314718055994531f;
   }
 }

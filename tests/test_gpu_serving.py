@@ -956,3 +956,34 @@ def test_value_scales_down_to_the_smallest(kind, page, d, new, hq, top):
     assert np.all(np.abs(f64(lse) - r["lse"]) <= score + 4 * F32 * np.abs(r["lse"]))
     bound = BF16 * np.abs(r["o"]) + (HALF + 2 * score[..., None]) * r["spread"] * (1 + BF16) + lost
     assert np.all(np.abs(f64(o) - r["o"]) <= bound), np.max(np.abs(f64(o) - r["o"]) / bound)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("hq", [1, 10, 25, 40])
+def test_a_huge_value_that_weighs_little(kind, hq):
+    """One block's share of a sequence holds keys of small score, the largest of them with a value as an infinity is stored: that block's
+    result is beyond fp32, the whole one is not."""
+    T, at = 320 * 128, 200 * 128 + 40
+    w = World(83, kind, 128, 1, 64, [T], spare=0)
+    unit, s = unit_code(kind), np.zeros(T)
+    s[at - 1000:at + 1000], s[at] = -40.0, -30.0
+    k, v = np.zeros((T, 64), np.uint8), np.zeros((T, 64), np.uint8)
+    k[s == -40, 0] = k[at, 1] = unit
+    v[:] = unit
+    v[at] = 0x7e if kind == "e4m3" else 127
+    top = R.TOP[kind] * 2.0 ** (120 if kind == "e4m3" else 122)
+    for i, p in enumerate(w.table[0]):
+        w.codes["k"][p, 0], w.codes["v"][p, 0] = k[i * 128:(i + 1) * 128], v[i * 128:(i + 1) * 128]
+    w.scale["k"][:], w.scale["v"][:] = 1.0, 1.0
+    page = w.table[0][at // 128]
+    w.scale["v"][page] = top / R.TOP[kind]
+    keep = w.codes["v"][page, 0, at % 128].copy()
+    w.codes["v"][page, 0], w.codes["v"][page, 0, at % 128] = 0, keep
+    w.up()
+    q = torch.zeros(1, hq, 64, dtype=torch.bfloat16)
+    q[..., 0], q[..., 1] = -320.0, -240.0                         # times 1/8
+    o, lse = attend_batch(w, shared_batch(w, 1), q, hq)
+    z = np.exp(s).sum()
+    value = np.exp(-30.0) * top / z                               # what the other values add is below 2^-60 of it
+    assert np.abs(f64(lse) - math.log(z)).max() <= (T / 32 + 300) * F32 + 2.0 ** -20
+    assert np.all(np.abs(f64(o) - value) <= (BF16 + HALF + 2.0 ** -12) * value)
