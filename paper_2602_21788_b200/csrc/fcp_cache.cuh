@@ -293,16 +293,34 @@ constexpr int CT_WARPS = 8;                           // consumer warps; two mor
 constexpr int CT_THREADS = (CT_WARPS + 2) * 32;
 constexpr int WEIGHT_CTAS = 2;                        // per SM, of the kernel that adds up weights
 
-// What goes with 16 keys: key scale (0: absent), log2 and inverse of the value scale, and for the weights' kernel the row of the
-// first code (bits), for the others a power of two that the weights are multiplied by before they meet the values.
-// The sum of the probabilities is kept as weights over value scales, and a weight stands at up to 2^15.  With the smallest scale, 2^-100,
-// which a page of zeros has, 2^13 keys at 2^15 already sum to infinity; so a scale below 2^-80 counts 2^n times as much, enough
-// for 2^-80, and its weights 2^-n times: 2^31 keys then sum to 2^126 at most.  Scales of up to 2^122 keep their sum above 2^-114.
-constexpr int CT_LEAST_EXPONENT = 127 - 80;           // biased, of 2^-80
-__device__ __forceinline__ float4 about_keys(float ks, float vs, int32_t row, bool weights) {
-  const int up = max(0, CT_LEAST_EXPONENT - (int)(__float_as_uint(vs) >> 23));
-  const float s = __uint_as_float(__float_as_uint(vs) + ((uint32_t)up << 23));
-  return make_float4(ks, __log2f(s), 1.f / s, weights ? __int_as_float(row) : __uint_as_float((uint32_t)(127 - up) << 23));
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A weight is 2^(a - ref), a the score plus y, the log2 of its value scale; the probabilities are the weights over the value scales.  With y
+// from -100 (pages of zeros) to 122 (infinite values) neither the plain sum of the probabilities nor the weights of keys whose scale
+// is small beside others' stay in fp32's range.  So:
+//   - the sum is kept times 2^CT_SHIFT: between 2^(8 - 40 - 60), a row's largest weight alone with y = 60, and 2^(46 - 40 + 100), 2^31
+//     weights of 2^15 with y = -100; in rows whose largest weight has a greater y, times 2^CT_SHIFT_HUGE (cache_tile_kernel, whose
+//     warps hold parts of a row's sum under one reference: where the part asks for it);
+//   - from the first tiles of a group on that hold keys whose y is 60 from another's, tiles are marked ST_APART, and from its first key with
+//     y >= 60 on ST_HUGE besides: their probabilities get exponentials of their own, because the weights may vanish where the
+//     probabilities do not.
+constexpr int CT_APART = 60, CT_HUGE = 60;
+constexpr float CT_SHIFT = -40.f, CT_SHIFT_HUGE = 20.f, CT_UNIT = 0x1p-40f, CT_UNIT_HUGE = 0x1p20f;
+// l times 2^e, for -250 < e < 250 where the result is in range; 0 stays 0
+__device__ __forceinline__ float times_exp2(float l, float e) {
+  const float half = exp2_approx(0.5f * e);
+  return l * half * half;
+}
+// A sum times 2^CT_SHIFT_HUGE is passed on with a minus sign.
+__device__ __forceinline__ float sum_shift(float l) { return l < 0.f ? CT_SHIFT_HUGE : CT_SHIFT; }
+// The logarithm's error grows with its size, so the exponent goes by itself.
+__device__ __forceinline__ float log2_split(float z) {
+  const uint32_t u = __float_as_uint(z);
+  return z < INFINITY ? (float)((int)(u >> 23) - 127) + __log2f(__uint_as_float((u & 0x7fffffu) | 0x3f800000u)) : z;
 }
 
 // A partial output may pass fp32's range where the whole one does not: an infinite value is stored as 448 * 2^120 or 127 * 2^122, and
@@ -328,9 +346,10 @@ struct AttnArgs {
 struct StageMeta {                                    // what a stage holds, for the consumers
   int32_t row0, n, length, head;                      // of the sequence and group
   int32_t row_tile, key0, flags, part;
-  float4 sub[CT_KEYS / 16];                           // about_keys of each 16
+  // per 16 keys: key scale (0: absent), log2 and 2^CT_SHIFT times the inverse (ST_APART: 0) of the value scale, row of the first code (bits)
+  float4 sub[CT_KEYS / 16];
 };
-enum { ST_FIRST = 1, ST_LAST = 2, ST_WHOLE = 4, ST_END = 8 };
+enum { ST_FIRST = 1, ST_LAST = 2, ST_WHOLE = 4, ST_END = 8, ST_APART = 16, ST_HUGE = 32 };
 enum { SP_COUNT = 0, SP_ROW0, SP_N, SP_HEAD, SP_ROW_TILE, SP_W = 8 };
 
 // NR blocks of 8 rows per warp, WR warps side by side: 8 * NR * WR rows of a group (WR = 0: the weights, NR blocks at a time).
@@ -368,11 +387,6 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-__device__ __forceinline__ float exp2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
@@ -678,6 +692,7 @@ struct AttnProducer {
     bool have = next(now, lane), have_soon = have && next(soon, lane), have_later = false;
     if (have) fetch_scales(now);
     bool ok = true, whole = false, from_start = false;
+    int top = 0, least = 255, apart = 0;              // largest and smallest biased exponent of a value scale of the group so far; marks
     while (have) {
       if (have_soon) fetch_scales(soon);
       have_later = have_soon && next(later, lane);
@@ -687,7 +702,14 @@ struct AttnProducer {
         now.row = -1;
       }
       const bool usable = now.row >= 0;
-      const float4 about = usable ? about_keys(now.ks, now.vs, now.row, WEIGHTS) : make_float4(0.f, 0.f, 1.f, 1.f);
+      if (!WEIGHTS && !is_v) {
+        const int e = (int)(__float_as_uint(now.vs) >> 23);
+        const int high = __reduce_max_sync(0xffffffffu, usable ? e : 0), low = __reduce_min_sync(0xffffffffu, usable ? e : 255);
+        top = now.first ? high : max(top, high);
+        least = now.first ? low : min(least, low);
+        apart = (least + CT_APART < top ? ST_APART : 0) | (top >= 127 + CT_HUGE ? ST_APART | ST_HUGE : 0);
+      }
+      const float4 about = usable ? make_float4(now.ks, __log2f(now.vs), apart ? 0.f : CT_UNIT / now.vs, __int_as_float(now.row)) : make_float4(0.f, 0.f, 0.f, 0.f);
       for (int i = 0; i < now.tiles; ++i) {
         if (!mbar_wait_warp(empty + stage * 8, phase ^ 1, ctx, 911)) {
           ok = false;
@@ -706,7 +728,7 @@ struct AttnProducer {
           m.row0 = now.s.row0; m.n = now.s.n; m.length = now.s.length; m.head = now.head;
           m.row_tile = now.row_tile;
           m.key0 = (now.tile + i) * CT_KEYS;
-          m.flags = (first ? ST_FIRST : 0) | (last ? ST_LAST : 0) | (whole ? ST_WHOLE : 0);
+          m.flags = (first ? ST_FIRST : 0) | (last ? ST_LAST : 0) | (whole ? ST_WHOLE : 0) | apart;
           m.part = 2 * (int)blockIdx.x + (from_start ? 1 : 0);
         }
         __syncwarp();
@@ -765,17 +787,19 @@ struct AttnConsumer {
   float factor[NR][2];                                // of rows 2t and 2t + 1 of each block
   int32_t limit[NR][2], least, most;                  // least, most: limits of the first and the last row that exist
   float o[NR][MT][4];                                 // O^T: block j of 16 columns: columns g MT*2 + 2j (| + 1) x rows 2t (| + 1)
-  float ref[NR][2], l[NR][2];                         // weights are 2^(a - ref); their sum over the value scale
+  float ref[NR][2], l[NR][2];                         // weights are 2^(a - ref); sum of the probabilities, times 2^CT_SHIFT
+  uint32_t huge;                                      // bit 2i + r: that row's sum is times 2^CT_SHIFT_HUGE
+  __device__ __forceinline__ float shift(int i, int r) const { return huge >> (2 * i + r) & 1u ? CT_SHIFT_HUGE : CT_SHIFT; }
 
-  // 32 keys from `key` (position) on, at `at` in the stage
-  __device__ __forceinline__ void step(const uint8_t* ktile, const uint8_t* vtile, int at, int key, const float4 (&about)[2], int lane) {
+  // 32 keys from `key` (position) on, at `at` in the stage.  APART: of a tile with that mark; `with_huge`: with the other one.
+  template <bool APART>
+  __device__ __forceinline__ void step(const uint8_t* ktile, const uint8_t* vtile, int at, int key, const float4 (&about)[2], bool with_huge, int lane) {
     const int g = lane >> 2, t = lane & 3;
     float s[2][NR][4];
     scores<D, KIND, 2, NR>(frag, ktile, at, lane, s);
     // a = score in log2 units plus log2 of the value scale, so that 2^(a - ref) are the weights of the value codes, and the sum
     // of the probabilities is that of the weights over the value scale.  ref follows the largest a from 8 below it and is left
     // alone until a weight would pass 2^15: a half holds weights down to 2^-24, 2^-32 of the largest and less.
-    // (Value scales below 2^-80: about_keys.)
     const bool edge = key + 32 > least || about[0].x == 0.f || about[1].x == 0.f;
     float top[NR][2];
     bool high = false;
@@ -806,16 +830,39 @@ struct AttnConsumer {
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+          float rise = 0.f;
+          if (APART && with_huge) {
+            float at = -INFINITY;                     // the largest with such a value scale
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (about[h].y >= (float)CT_HUGE) at = fmaxf(at, fmaxf(s[h][i][r], s[h][i][r + 2]));
+            at = fmaxf(at, __shfl_xor_sync(0xffffffffu, at, 4));
+            at = fmaxf(at, __shfl_xor_sync(0xffffffffu, at, 8));
+            at = fmaxf(at, __shfl_xor_sync(0xffffffffu, at, 16));
+            if (at >= m && m - 8.f > ref[i][r] && shift(i, r) == CT_SHIFT) {
+              rise = CT_SHIFT_HUGE - CT_SHIFT;
+              huge |= 1u << (2 * i + r);
+            }
+          }
           m = fmaxf(ref[i][r], m - 8.f);
-          const float shrink = exp2_approx(ref[i][r] - m);
+          // in two halves: the sum may outlast what o loses
+          const float half = exp2_approx(0.5f * (ref[i][r] - m)), shrink = half * half;
+          l[i][r] = APART ? times_exp2(l[i][r], ref[i][r] - m + rise) : l[i][r] * half * half;
           ref[i][r] = m;
-          l[i][r] *= shrink;
 #pragma unroll
           for (int j = 0; j < MT; ++j) {
             o[i][j][r] *= shrink;
             o[i][j][r + 2] *= shrink;
           }
         }
+    }
+    if (APART) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) l[i][c & 1] += about[h].x == 0.f ? 0.f : exp2_approx(s[h][i][c] - ref[i][c & 1] + (shift(i, c & 1) - about[h].y));
     }
     uint32_t p[2][NR][2];                             // P^T as the second operand: keys 2t, 2t + 1 (| + 8) x row g
 #pragma unroll
@@ -824,11 +871,9 @@ struct AttnConsumer {
       for (int i = 0; i < NR; ++i) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) s[h][i][c] = exp2_approx(s[h][i][c] - ref[i][c & 1]);
-        l[i][0] = fmaf(s[h][i][0] + s[h][i][2], about[h].z, l[i][0]);
-        l[i][1] = fmaf(s[h][i][1] + s[h][i][3], about[h].z, l[i][1]);
-        if (about[h].w != 1.f) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) s[h][i][c] *= about[h].w;
+        if (!APART) {
+          l[i][0] = fmaf(s[h][i][0] + s[h][i][2], about[h].z, l[i][0]);
+          l[i][1] = fmaf(s[h][i][1] + s[h][i][3], about[h].z, l[i][1]);
         }
         p[h][i][0] = transpose8(pack_half(s[h][i][0], s[h][i][1]));
         p[h][i][1] = transpose8(pack_half(s[h][i][2], s[h][i][3]));
@@ -926,7 +971,7 @@ struct AttnConsumer {
         l[i][r] += __shfl_xor_sync(0xffffffffu, l[i][r], 16);
         const int row = 8 * i + 2 * t + r;
         if (warp % WR * 8 * NR + row >= n_rows) continue;
-        if (g == 0) stats[warp * 8 * NR + row] = make_float2(ref[i][r], l[i][r]);
+        if (g == 0) stats[warp * 8 * NR + row] = make_float2(ref[i][r], shift(i, r) == CT_SHIFT ? l[i][r] : -l[i][r]);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
           mine[join_slot(row, g * (D / 32) + c)] = make_float4(o[i][2 * c][r], o[i][2 * c][r + 2], o[i][2 * c + 1][r], o[i][2 * c + 1][r + 2]);
@@ -934,7 +979,7 @@ struct AttnConsumer {
     if (!sync(ctx, lane, 924)) return false;
     for (int e = tid; e < n_rows * (D / 4); e += CT_WARPS * 32) {
       const int r = e / (D / 4), f = e % (D / 4), wr = r / (8 * NR), row = r % (8 * NR);
-      float top = -3e38f;
+      float top = -3e38f, shift = CT_SHIFT;
 #pragma unroll
       for (int k = 0; k < KG; ++k) top = fmaxf(top, stats[(k * WR + wr) * 8 * NR + row].x);
       float z = 0.f;
@@ -947,10 +992,20 @@ struct AttnConsumer {
         z = fmaf(ml.y, w, z);
         x.x = fmaf(y.x, w, x.x); x.y = fmaf(y.y, w, x.y); x.z = fmaf(y.z, w, x.z); x.w = fmaf(y.w, w, x.w);
       }
+      if (meta.flags & ST_APART) {                    // sums in different units, or beside which w vanishes
+        z = 0.f;
+#pragma unroll 1
+        for (int k = 0; k < KG; ++k) shift = fmaxf(shift, sum_shift(stats[(k * WR + wr) * 8 * NR + row].y));
+#pragma unroll 1
+        for (int k = 0; k < KG; ++k) {
+          const float2 ml = stats[(k * WR + wr) * 8 * NR + row];
+          z += times_exp2(fabsf(ml.y), ml.x - top + (shift - sum_shift(ml.y)));
+        }
+      }
       const float inverse = z == 0.f ? 0.f : 1.f / z;
-      const float lse2 = z == 0.f ? -INFINITY : top + __log2f(z);
-      const float unit = meta.flags & ST_WHOLE ? 1.f : CT_PART_UNIT;
-      x.x = x.x * unit * inverse; x.y = x.y * unit * inverse; x.z = x.z * unit * inverse; x.w = x.w * unit * inverse;
+      const float lse2 = z == 0.f ? -INFINITY : top - shift + log2_split(z);
+      const float unit = (shift == CT_SHIFT ? CT_UNIT : CT_UNIT_HUGE) * (meta.flags & ST_WHOLE ? 1.f : CT_PART_UNIT);
+      x.x = x.x * inverse * unit; x.y = x.y * inverse * unit; x.z = x.z * inverse * unit; x.w = x.w * inverse * unit;
       if (meta.flags & ST_WHOLE) {
         const int gr = meta.row_tile * RT + r, j = gr / A.group;
         const int64_t out = (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + gr - j * A.group;
@@ -981,6 +1036,7 @@ struct AttnConsumer {
         const int first_row = meta.row_tile * RT + wr * 8 * NR, n_rows = meta.n * A.group;
         const int last_row = min(first_row + 8 * NR, n_rows) - 1;
         least = meta.length - meta.n + first_row / A.group + 1;
+        huge = 0;
         most = first_row < n_rows ? meta.length - meta.n + last_row / A.group + 1 : 0;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
@@ -1000,7 +1056,10 @@ struct AttnConsumer {
         const uint8_t* ktile = ring + stage * S::STAGE;
         const int key = meta.key0 + i * CT_STEP;
         const float4 about[2] = {meta.sub[2 * i], meta.sub[2 * i + 1]};
-        if (key < most && (about[0].x != 0.f || about[1].x != 0.f)) step(ktile, ktile + S::TILE, i * CT_STEP, key, about, lane);
+        if (key < most && (about[0].x != 0.f || about[1].x != 0.f)) {
+          if (!(flags & ST_APART)) step<false>(ktile, ktile + S::TILE, i * CT_STEP, key, about, false, lane);
+          else step<true>(ktile, ktile + S::TILE, i * CT_STEP, key, about, flags & ST_HUGE, lane);
+        }
       }
       if ((flags & ST_LAST) && !finish(A, meta, join, stats, sync, ctx, warp, lane)) break;
       __syncwarp();
@@ -1436,6 +1495,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
     const uint32_t t_o = tmem_addr(tmem, quarter * 32, O_COL + part * (D / 4));
     ConsumerSync all = {quartet + quarter * 8, 0};
     float factor = 0.f, ref = -3e38f, l = 0.f;
+    bool huge = false;                                // the row's sum is times 2^CT_SHIFT_HUGE
     int limit = 0, seg = -1;
     bool there = false, begun = false;                // these warps have rows; O holds something of this group
     for (int t = 0;; ++t) {
@@ -1451,6 +1511,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
         there = meta.row_tile * TILE_ROWS + quarter * 32 < meta.n * A.group;
         ref = -3e38f;
         l = 0.f;
+        huge = false;
         begun = false;
       }
       uint32_t x[32];                                 // this warp's part of the row's scores
@@ -1492,7 +1553,10 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
         tc_fence_after();
         if (__any_sync(0xffffffffu, top > ref + 15.f)) {       // the same in all four warps
           const float m = top > ref + 15.f ? top - 8.f : ref, shrink = exp2_approx(ref - m);
-          l *= shrink;
+          // the sum keeps what it can of its range
+          const bool rises = (flags & ST_HUGE) && !huge && (float)((int)(__float_as_uint(l) >> 23) - 127) + (ref - m) < -60.f;
+          l = times_exp2(l, ref - m + (rises ? CT_SHIFT_HUGE - CT_SHIFT : 0.f));
+          huge |= rises;
           ref = m;
           if (begun) {                                // O is at rest once the tile before is in it
             if (!mbar_wait_warp(pv_done + ((t - 1) & 1) * 8, ((t - 1) >> 1) & 1, ctx, 963)) break;
@@ -1507,6 +1571,25 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
               tmem_st16(t_o + 16 * c, o);
             }
           }
+        }
+        if (flags & ST_APART) {
+          auto e = [&](int h, int i) {                // score over the reference, without the value scale
+            const float4 about = meta.sub[2 * part + h];
+            return fmaf(__uint_as_float(x[16 * h + i]), fmaxf(factor * about.x, 1.2e-38f), about.y - ref) - about.y;
+          };
+          if (flags & ST_HUGE) {
+            float most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (meta.sub[2 * part + (i >> 4)].x != 0.f) most = fmaxf(most, e(i >> 4, i & 15));
+            const bool up = !huge && most < -50.f && l < 0x1p-60f, down = huge && most > 40.f;
+            if (up) l /= CT_UNIT / CT_UNIT_HUGE;
+            if (down) l *= CT_UNIT / CT_UNIT_HUGE;
+            huge = up || (huge && !down);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (meta.sub[2 * part + (i >> 4)].x != 0.f) l += exp2_approx(e(i >> 4, i & 15) + (huge ? CT_SHIFT_HUGE : CT_SHIFT));
         }
         uint32_t p[16];
 #pragma unroll
@@ -1524,11 +1607,6 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
             p[8 * h + i] = pack_half(a, b);
           }
           l = fmaf(z0 + z1, about.z, l);
-          if (about.w != 1.f) {                       // a power of two from 2^-20 on
-            const __half2 down = __float2half2_rn(about.w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[8 * h + i] = h2_bits(__hmul2(*reinterpret_cast<const __half2*>(&p[8 * h + i]), down));
-          }
         }
         tmem_st16(tmem_addr(tmem, quarter * 32, P_COL + (t & 1) * 64 + 16 * part), p);
         tc_wait_st();
@@ -1539,15 +1617,24 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
       if (lane == 0) mbar_arrive(p_full + (t & 1) * 8);
       if (flags & ST_LAST) {
         if (there) {
-          sums[part][row] = l;
+          sums[part][row] = huge ? -l : l;
           if (!all(ctx, lane, 966)) break;
-          const float z = (sums[0][row] + sums[1][row]) + (sums[2][row] + sums[3][row]);
+          float z = (sums[0][row] + sums[1][row]) + (sums[2][row] + sums[3][row]);
+          if (flags & ST_HUGE) {
+            float shift = CT_SHIFT;
+            z = 0.f;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) shift = fmaxf(shift, sum_shift(sums[i][row]));
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) z += times_exp2(fabsf(sums[i][row]), shift - sum_shift(sums[i][row]));
+            huge = shift == CT_SHIFT_HUGE;
+          }
           if (!mbar_wait_warp(pv_done + (t & 1) * 8, (t >> 1) & 1, ctx, 964)) break;
           tc_fence_after();
           const int gr = meta.row_tile * TILE_ROWS + row, j = gr / A.group;
           const bool is = gr < meta.n * A.group;
-          const float inverse = z == 0.f ? 0.f : 1.f / z, lse2 = z == 0.f ? -INFINITY : ref + __log2f(z);
-          const float unit = flags & ST_WHOLE ? 1.f : CT_PART_UNIT;
+          const float inverse = z == 0.f ? 0.f : 1.f / z, lse2 = z == 0.f ? -INFINITY : ref - (huge ? CT_SHIFT_HUGE : CT_SHIFT) + log2_split(z);
+          const float unit = (huge ? CT_UNIT_HUGE : CT_UNIT) * (flags & ST_WHOLE ? 1.f : CT_PART_UNIT);
           const int64_t out = (int64_t)(meta.row0 + j) * A.hq + meta.head * A.group + gr - j * A.group, place = (int64_t)meta.part * TILE_ROWS + row;
           const TileGroup& grp = groups[seg % TILE_GROUPS];
 #pragma unroll 1
@@ -1557,7 +1644,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
             tc_wait_ld(o);
             const int col = part * (D / 64) + c;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(z == 0.f ? 0.f : __uint_as_float(o[i]) * unit * inverse);
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(z == 0.f ? 0.f : __uint_as_float(o[i]) * inverse * unit);
             if (NANS && grp.nan_any) {
               uint32_t bits = 0;
               for (int k = 0; k < min(limit - grp.least, 128); ++k) bits |= nans[seg % TILE_GROUPS][k][col];

@@ -987,3 +987,34 @@ def test_a_huge_value_that_weighs_little(kind, hq):
     value = np.exp(-30.0) * top / z                               # what the other values add is below 2^-60 of it
     assert np.abs(f64(lse) - math.log(z)).max() <= (T / 32 + 300) * F32 + 2.0 ** -20
     assert np.all(np.abs(f64(o) - value) <= (BF16 + HALF + 2.0 ** -12) * value)
+
+
+@pytest.mark.parametrize("kind,page,d", [("e4m3", 16, 64), ("int8", 16, 128), ("int8", 128, 64), ("e4m3", 128, 128)])
+@pytest.mark.parametrize("new,hq", [(1, 3), (3, 4), (5, 5), (1, 40)])
+@pytest.mark.parametrize("exponents", [[-9], [-100, -9], [-9, 120], [-100, -60, -35, -9, 20, 60, 120]])
+def test_value_scales_far_apart(kind, page, d, new, hq, exponents):
+    """Probabilities count in full however small their value scale is beside the others': pages of zeros, ordinary ones, and those of
+    values that were infinite."""
+    w = World(85, kind, page, 1, d, [3, 700, 9000]).fill()
+    w.scale["v"][:, 0] = 2.0 ** np.asarray(exponents)[w.rng.integers(0, len(exponents), w.n_pages)]
+    w.up()
+    q, o, lse, rows = attend(w, [min(new, 3), new, new], hq, spare=0)
+    state = w.state()
+    r = R.attention(state, w.table, w.length, w.off, f64(q))
+    lost = np.zeros((rows, hq, d))                                # as in test_tiles_of_rows_that_see_nothing_or_differ_in_size
+    for b, n in enumerate(np.diff(w.off)):
+        t = w.length[b]
+        pages = np.asarray(w.table[b][:-(-t // page)])
+        k, code = R.gather(state, "k", pages, t, 0), state["v"][pages, 0].reshape(-1, d)[:t]
+        scale = np.repeat(state["v_scale"][pages, 0], page)[:t]
+        for j in range(n):
+            row, seen = w.off[b] + j, t - n + j + 1
+            for h in range(hq):
+                s = k[:seen] @ f64(q)[row, h] / math.sqrt(d)
+                lost[row, h] = 2.0 ** -33 * (np.exp(s - r["lse"][row, h]) * scale[:seen]).max() * np.abs(code[:seen]).sum(axis=0)
+    # a score stands in log2 units beside the log2 of its value scale: an fp32 below 2^8, half a step 2^-17, and so does the reference
+    score = d * 2 * F32 * r["size"] + (2.0 ** -20 if exponents == [-9] else 2.0 ** -16)
+    assert np.all(np.abs(f64(lse) - r["lse"]) <= score + 4 * F32 * np.abs(r["lse"]))
+    bound = BF16 * np.abs(r["o"]) + (HALF + 2 * score[..., None]) * r["spread"] * (1 + BF16) + lost
+    fits = np.abs(r["o"]) + bound < 3.38e38                       # beyond what a bf16 holds an infinity stands for the number
+    assert np.all((np.abs(f64(o) - r["o"]) <= bound)[fits]) and not np.isnan(f64(o)).any()
