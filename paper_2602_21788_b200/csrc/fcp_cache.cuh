@@ -1575,7 +1575,7 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
         if (flags & ST_APART) {
           auto e = [&](int h, int i) {                // score over the reference, without the value scale
             const float4 about = meta.sub[2 * part + h];
-            return fmaf(__uint_as_float(x[16 * h + i]), fmaxf(factor * about.x, 1.2e-38f), about.y - ref) - about.y;
+            return fmaf(__uint_as_float(x[16 * h + i]), fmaxf(factor * about.x, 1.2e-38f), about.y) - ref - about.y;
           };
           if (flags & ST_HUGE) {
             float most = -INFINITY;
@@ -1595,13 +1595,15 @@ cache_tile_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float4 about = meta.sub[2 * part + h];
-          const bool is = about.x != 0.f;             // else the scores are -infinity whatever they are multiplied by
-          const float f = is ? fmaxf(factor * about.x, 1.2e-38f) : 1.f, shift = about.y - ref;        // not 0: times -infinity
+          const float f = about.x != 0.f ? fmaxf(factor * about.x, 1.2e-38f) : 1.f;       // not 0: times -infinity; absent keys have -infinity
           float z0 = 0.f, z1 = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int e = 16 * h + 2 * i;
-            const float a = exp2_approx(fmaf(__uint_as_float(x[e]), f, shift)), b = exp2_approx(fmaf(__uint_as_float(x[e + 1]), f, shift));
+            // rounded as the reference was before it is taken off: in one step a score of 2^26 or more would differ from its own
+            // reference by the rounding, and its weight would overflow
+            const float2 s2 = add2(fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), make_float2(f, f), make_float2(about.y, about.y)), make_float2(-ref, -ref));
+            const float a = exp2_approx(s2.x), b = exp2_approx(s2.y);
             z0 += a;
             z1 += b;
             p[8 * h + i] = pack_half(a, b);

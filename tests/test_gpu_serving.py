@@ -1018,3 +1018,33 @@ def test_value_scales_far_apart(kind, page, d, new, hq, exponents):
     bound = BF16 * np.abs(r["o"]) + (HALF + 2 * score[..., None]) * r["spread"] * (1 + BF16) + lost
     fits = np.abs(r["o"]) + bound < 3.38e38                       # beyond what a bf16 holds an infinity stands for the number
     assert np.all((np.abs(f64(o) - r["o"]) <= bound)[fits]) and not np.isnan(f64(o)).any()
+
+
+@pytest.mark.parametrize("kind,page,d", [("e4m3", 16, 64), ("int8", 128, 128)])
+@pytest.mark.parametrize("new,hq", [(1, 3), (3, 4), (5, 5), (1, 40)])
+@pytest.mark.parametrize("exponent", [24, 60, 110])
+def test_scores_far_beyond_the_exponentials(kind, page, d, new, hq, exponent):
+    """Scores of 2^24 to 2^116: the key with the largest takes all, and nothing overflows."""
+    w = World(86, kind, page, 1, d, [3, 700, 9000]).fill()
+    w.scale["k"] *= np.float32(2.0 ** exponent)
+    w.up()
+    q, o, lse, rows = attend(w, [min(new, 3), new, new], hq, spare=0)
+    state = w.state()
+    r = R.attention(state, w.table, w.length, w.off, f64(q))
+    score = d * 2 * F32 * r["size"]
+    assert np.all(np.abs(f64(lse) - r["lse"]) <= score + 4 * F32 * np.abs(r["lse"]) + 1)
+    # one key: its weight and the sum are the same number but for two roundings of an exponential
+    clear, got = 0, f64(o)
+    for b, n in enumerate(np.diff(w.off)):
+        t = w.length[b]
+        pages = np.asarray(w.table[b][:-(-t // page)])
+        k, v = R.gather(state, "k", pages, t, 0), R.gather(state, "v", pages, t, 0)
+        for j in range(n):
+            row, seen = w.off[b] + j, t - n + j + 1
+            for h in range(hq):
+                s = k[:seen] @ f64(q)[row, h] / math.sqrt(d)
+                at, gap = s.argmax(), np.diff(np.sort(s)[-2:]) if seen > 1 else np.inf
+                if gap > 2 * score[row, h] + 100:
+                    clear += 1
+                    assert np.all(np.abs(got[row, h] - v[at]) <= (BF16 + HALF + 2.0 ** -18) * np.abs(v[at]) + 1e-30)
+    assert clear > 0.9 * rows * hq and not np.isnan(got).any()
