@@ -478,8 +478,11 @@ int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const
  * workspace: device, 256-byte aligned, of at least fcp_cache_attn_workspace_bytes; its contents need not be initialised; two calls
  * that may overlap on the GPU, also two captured ones, need one each.
  * Scores, statistics and sums are fp32; the weights of the values are rounded to halves (a weight times its value scale to 0 below
- * 2^-33 of the row's largest), and in calls with many new tokens, which go through bf16 copies of the codes in the workspace (up to
- * 8 GB, where that is faster), to bf16, as is code * scale where a scale is no power of two.  The same call gives the same bits again, unless sequences of one call share a page and accumulate.
+ * 2^-33 of the row's largest: a page with an infinite value leaves next to nothing of the others' for the rows that see any of its
+ * tokens), and in calls with many new tokens, which go through bf16 copies of the codes in the workspace (up to 8 GB, where that is
+ * faster), to bf16, as is code * scale where a scale is no power of two; beyond the largest bf16 it counts as that.  A row with a score of
+ * 2^128 log 2 or more (in calls by copies 2^30) has no defined result.  The same call gives the same bits again, unless sequences of one
+ * call share a page and accumulate.
  */
 int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t hq, int64_t* bytes);
 int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const void* q, int64_t q_stride, int32_t hq,

@@ -1744,8 +1744,9 @@ __global__ void __launch_bounds__(MERGE_THREADS) cache_merge_kernel(const __grid
 // are written out as bf16 once (exactly, where the scale is a power of two), [sequence][capacity][hkv][D], and the packed
 // attention of this library (fcp_fwd_kernel) runs over them, with work units and row limits made on the device.
 //
-// Sequences that this cannot serve exactly are marked and left to cache_attn_kernel: tokens on pages that do not exist, more new rows
-// than tokens, a NaN value among the new tokens (it would meet zero weights of rows that do not see it).
+// Sequences that this cannot serve exactly are marked and left to cache_attn_kernel or cache_tile_kernel: tokens on pages that do not
+// exist, more new rows than tokens, a NaN value among the new tokens (it would meet zero weights of rows that do not see it), key
+// scales above CHUNK_MOST_K.
 struct ChunkArgs {
   CacheView c;
   BatchView s;
@@ -1757,6 +1758,14 @@ struct ChunkArgs {
 };
 
 constexpr int UNPACK_THREADS = 256;
+// fcp_fwd_kernel's weights overflow at scores of 2^31.  Keys of up to 2^17 stay clear of that.
+constexpr float CHUNK_MOST_K = 0x1p8f;
+// code * scale as it goes into a bf16.  From scales of 2^119 on it may be beyond one (an infinite value is stored with 2^120 or 2^122),
+// and an infinity would meet the zero weights of rows that do not see it: the largest bf16 instead.
+__device__ __forceinline__ float held_by_bf16(float x) {
+  const float most = __uint_as_float(0x7f7f0000u);
+  return fabsf(x) > most ? copysignf(most, x) : x;     // a NaN stays one
+}
 // 16 codes -> 16 bf16
 template <int KIND>
 __device__ __forceinline__ void unpack16(const uint4& x, float scale, uint4 (&out)[2]) {
@@ -1768,6 +1777,10 @@ __device__ __forceinline__ void unpack16(const uint4& x, float scale, uint4 (&ou
     const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
     y[2 * i] = pack_bf16(a.x * scale, a.y * scale);
     y[2 * i + 1] = pack_bf16(b.x * scale, b.y * scale);
+    if (scale > 0x1p118f) {
+      y[2 * i] = pack_bf16(held_by_bf16(a.x * scale), held_by_bf16(a.y * scale));
+      y[2 * i + 1] = pack_bf16(held_by_bf16(b.x * scale), held_by_bf16(b.y * scale));
+    }
   }
   out[0] = make_uint4(y[0], y[1], y[2], y[3]);
   out[1] = make_uint4(y[4], y[5], y[6], y[7]);
@@ -1802,6 +1815,7 @@ __global__ void __launch_bounds__(UNPACK_THREADS) cache_unpack_kernel(const __gr
         row = -2;
         careful = true;
       }
+      careful |= ks > CHUNK_MOST_K;
     }
     rows[tid] = row;
     scales[0][tid] = ks;

@@ -1048,3 +1048,40 @@ def test_scores_far_beyond_the_exponentials(kind, page, d, new, hq, exponent):
                     clear += 1
                     assert np.all(np.abs(got[row, h] - v[at]) <= (BF16 + HALF + 2.0 ** -18) * np.abs(v[at]) + 1e-30)
     assert clear > 0.9 * rows * hq and not np.isnan(got).any()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunks_with_values_beyond_bf16(kind, d):
+    """Keys and values that were infinite or next to the largest bf16 stand in the cache as numbers beyond bf16; in calls that go by
+    copies they reach the rows that see them, and no others."""
+    new, before, hkv, group = [200, 150, 300, 133], [100, 0, 37, 300], 4, 8
+    w = World(84, kind, 16, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    hq, rows = hkv * group, sum(new)
+    assert goes_by_copies(w, new, hq)
+    batch = w.batch(new)
+    k, v, q = bf16(w.rng, rows, hkv, d), bf16(w.rng, rows, hkv, d), bf16(w.rng, rows, hq, d)
+    at = {0: 150, 1: 120, 2: 290}                                 # of each sequence's new tokens
+    v[w.off[0] + at[0], 1, 5], v[w.off[0] + at[0], 2, 6] = math.inf, -math.inf
+    v[w.off[1] + at[1], :, 3] = 3.3e38
+    k[w.off[2] + at[2], 0, 2] = math.inf
+    k[w.off[2] + at[2], 3, 0] = 1e30
+    fcp.fcp_cache_append(w.cache, batch, k.cuda(), v.cuda(), stream=stream())
+    o, lse = attend_batch(w, batch, q, hq)
+    r = R.attention(w.now(), w.table, w.length, w.off, f64(q))
+    got, got_lse = f64(o), f64(lse)
+    score = d * 2 * F32 * r["size"] + 2.0 ** -20
+    # scores are fp32 in units of log 2: 448 * 2^120 times a query above 3 is 6.0e38 * 3 / 8 * 1.44 = 3.3e38 or more, and fp32 ends at
+    # 3.4e38; what such a row gets is not defined
+    held = r["size"] * math.log2(math.e) < 3.4e38
+    assert held.mean() > 0.99
+    assert not np.isnan(got[held]).any() and not np.isnan(got_lse[held]).any()
+    assert np.all((np.abs(got_lse - r["lse"]) <= score + 4 * F32 * np.abs(r["lse"]))[held])
+    bound = BF16 * np.abs(r["o"]) + (BF16 + 2 * score[..., None]) * r["spread"] * (1 + BF16) + 1e-30
+    # a number beyond bf16, 448 * 2^120 or 127 * 2^122 at most, counts as the largest bf16, 2^128: 1 / 1.99 of it or more; a sum may be infinite
+    great = r["spread"] > 1e30
+    assert np.all((np.abs(got - r["o"]) <= bound)[held[..., None] & ~great])
+    assert np.all((np.sign(got) == np.sign(r["o"]))[great]) and np.all((np.abs(got) >= 0.49 * np.abs(r["o"]) - bound)[great])
+    for b, j in at.items():                                       # the rows in front of it know nothing of it
+        assert not great[w.off[b]:w.off[b] + j].any() and held[w.off[b]:w.off[b] + j].all()
+    assert great[w.off[0] + at[0]:w.off[1]].any() and great[w.off[1] + at[1]:w.off[2]].any()
