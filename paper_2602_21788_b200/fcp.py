@@ -333,6 +333,7 @@ class RopeTable:
         config = FcpRopeConfig(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), _named(ROPE_LAYOUTS, layout),
                                _named(ROPE_SCALINGS, scaling), float(base), float(factor), float(original_length), float(low),
                                float(high), float(magnitude))
+        _torch_types()
         self.struct = FcpRopeTable()
         _check(lib().fcp_rope_init(C.byref(config), C.byref(self.struct)))
         self.ref, self.head_dim = C.byref(self.struct), self.struct.head_dim
@@ -352,14 +353,30 @@ def _named(names: dict, value) -> int:
     return int(value)
 
 
-# The checks below stand in front of kernels of a few microseconds: one look at shape and strides per tensor, no conversions.
+# The checks below stand in front of kernels of a few microseconds: one look at type, shape and strides per tensor, no conversions.
+# A tensor of another type would be read as what it is not.
+_BF16 = _F32 = _I32 = None
+
+
+def _torch_types():
+    """Called where a table, a cache or a batch is made: PyTorch need not be there for the planner's calls."""
+    global _BF16, _F32, _I32
+    if _BF16 is None:
+        import torch
+        _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
 def _heads(x, head_dim, name):
-    """Rows, heads, row stride and address of a tensor [rows][heads][head_dim] whose heads are contiguous."""
+    """Rows, heads, row stride and address of a bf16 tensor [rows][heads][head_dim] whose heads are contiguous."""
     rows, heads, d = x.shape
     s0, s1, s2 = x.stride()
-    if d != head_dim or s2 != 1 or (s1 != d and heads > 1) or x.element_size() != 2:
+    if d != head_dim or s2 != 1 or (s1 != d and heads > 1) or x.dtype is not _BF16:
         raise ValueError(f"{name}: a bf16 tensor [rows][heads][{head_dim}] with contiguous heads is wanted")
-    return rows, heads, s0 if rows > 1 else heads * d, x.data_ptr()
+    if rows <= 1:
+        s0 = heads * d
+    elif s0 < heads * d:                           # an expanded tensor: its stride 0 means heads * head_dim to the library
+        raise ValueError(f"{name}: rows that share memory (row stride {s0}); a row of its own for each is wanted, see Tensor.contiguous")
+    return rows, heads, s0, x.data_ptr()
 
 
 _NO_HEADS = (None, 0, 0, None)
@@ -369,7 +386,7 @@ def _i32_ptr(x, n, name):
     """Address of a contiguous int32 device tensor of n entries (None: NULL)."""
     if x is None:
         return None
-    if x.element_size() != 4 or x.numel() != n or x.is_floating_point() or not x.is_contiguous():
+    if x.dtype is not _I32 or x.numel() != n or not x.is_contiguous():
         raise ValueError(f"{name}: a contiguous int32 tensor of {n} entries is wanted")
     return x.data_ptr()
 
@@ -414,15 +431,16 @@ class Cache:
     k_scale, v_scale fp32 [n_pages][hkv], status int32 [4] (zeroed), weight fp32 [n_pages][hkv][page_tokens] or None."""
 
     def __init__(self, k, v, k_scale, v_scale, status, weight=None, kind=None):
+        _torch_types()
         n_pages, hkv, page_tokens, head_dim = k.shape
         if kind is None:
             kind = {"torch.float8_e4m3fn": "e4m3", "torch.int8": "int8"}.get(str(k.dtype))
             if kind is None:
                 raise ValueError(f"pages of {k.dtype}: say which kind of code they hold")
-        for x, shape, size in ((k, k.shape, 1), (v, k.shape, 1), (k_scale, (n_pages, hkv), 4), (v_scale, (n_pages, hkv), 4),
-                               (weight, (n_pages, hkv, page_tokens), 4), (status, (4,), 4)):
-            if x is not None and (tuple(x.shape) != tuple(shape) or x.dtype.itemsize != size or not x.is_contiguous()):
-                raise ValueError(f"a contiguous tensor {tuple(shape)} of {size}-byte values is wanted, not {tuple(x.shape)} {x.dtype}")
+        for x, shape, dtype in ((k, k.shape, None), (v, k.shape, None), (k_scale, (n_pages, hkv), _F32), (v_scale, (n_pages, hkv), _F32),
+                                (weight, (n_pages, hkv, page_tokens), _F32), (status, (4,), _I32)):
+            if x is not None and (tuple(x.shape) != tuple(shape) or not x.is_contiguous() or not (x.dtype is dtype if dtype else x.dtype.itemsize == 1)):
+                raise ValueError(f"a contiguous tensor {tuple(shape)} of {dtype or '1-byte values'} is wanted, not {tuple(x.shape)} {x.dtype}")
         self.hkv, self.head_dim, self.page_tokens, self.n_pages = hkv, head_dim, page_tokens, n_pages
         self.tensors = (k, v, k_scale, v_scale, status, weight)          # the pages live as long as the handle
         ptr = [None if x is None else x.data_ptr() for x in (k, v, k_scale, v_scale, weight, status)]
@@ -447,6 +465,7 @@ class CacheBatch:
     (device tensors, read when the call runs); rows and max_new bound them (default for max_new: rows)."""
 
     def __init__(self, page_table, length, row_offset=None, rows=0, max_new=None):
+        _torch_types()
         B, width = page_table.shape
         self.tensors = (page_table, length, row_offset)
         self.B, self.rows = B, int(rows)
@@ -477,8 +496,10 @@ def fcp_cache_attn(cache: Cache, batch: CacheBatch, q, o, lse, workspace, worksp
     o_rows, o_heads, _, op = _heads(o, cache.head_dim, "o")
     if rows != batch.rows or o_rows != rows or o_heads != hq or not o.is_contiguous():
         raise ValueError(f"q, o: {batch.rows} rows of the same heads are wanted, o contiguous")
-    if lse.numel() != rows * hq or lse.element_size() != 4 or not lse.is_contiguous():
+    if lse.numel() != rows * hq or lse.dtype is not _F32 or not lse.is_contiguous():
         raise ValueError("lse: a contiguous fp32 tensor [rows][hq] is wanted")
+    if workspace is not None and (workspace.nbytes < workspace_bytes or not workspace.is_contiguous()):
+        raise ValueError(f"workspace: contiguous, of at least the {workspace_bytes} bytes that the call names")
     rc = lib().fcp_cache_attn(cache.handle, batch.ref, qp, qs, hq, scale, op, lse.data_ptr(), 1 if accumulate else 0,
                               None if workspace is None else workspace.data_ptr(), workspace_bytes, stream)
     if rc:

@@ -194,6 +194,51 @@ def test_binding_checks_shapes():
         fcp.fcp_cache_evict(cache, batch, 1, 1, 1, table, length, z(2, 2, 4, t=torch.int32))
 
 
+
+def test_binding_refuses_types_and_rows_that_share_memory():
+    """Expanded tensors (row stride 0, which the library takes for dense rows), other 2-byte and 4-byte types."""
+    t = fcp.RopeTable(64)
+    cache, batch, x, lse = _host_cache()
+    one = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    wide = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    overlapping = torch.zeros(1000, dtype=torch.bfloat16).as_strided((2, 2, 64), (64, 64, 1))
+    off = torch.tensor([0, 2], dtype=torch.int32)
+    for bad in (one.expand(2, 2, 64), overlapping, x.half(), x.view(torch.int16)):
+        for call in (fcp.fcp_rope_fwd, fcp.fcp_rope_bwd):
+            for args in [(bad, None, x, None), (x, None, bad, None), (None, bad, None, x), (None, x, None, bad)]:
+                with pytest.raises(ValueError, match="bf16|share memory"):
+                    call(t, *args, row_offset=off)
+        for args in [(bad, x), (x, bad)]:
+            with pytest.raises(ValueError, match="bf16|share memory"):
+                fcp.fcp_cache_append(cache, batch, *args)
+        for q, o in [(bad, x), (x, bad)]:
+            with pytest.raises(ValueError, match="bf16|share memory|contiguous"):
+                fcp.fcp_cache_attn(cache, batch, q, o, lse, None, 0)
+    assert fcp._heads(wide[:, :2], 64, "q")[2] == 256 and fcp._heads(one.expand(1, 2, 64), 64, "q")[2] == 128        # slices, single rows
+    for bad in (lse.int(), lse.double(), lse.half()):
+        with pytest.raises(ValueError, match="fp32"):
+            fcp.fcp_cache_attn(cache, batch, x, x, bad, None, 0)
+    with pytest.raises(ValueError, match="workspace"):
+        fcp.fcp_cache_attn(cache, batch, x, x, lse, torch.zeros(10, dtype=torch.uint8), 11)
+    k, v, ks, vs, status, weight = (torch.zeros(s, dtype=d) for s, d in (((3, 2, 16, 64), torch.int8), ((3, 2, 16, 64), torch.int8), ((3, 2), torch.float32),
+                                    ((3, 2), torch.float32), (4, torch.int32), ((3, 2, 16), torch.float32)))
+    for args in [(k, v, ks.int(), vs, status, weight), (k, v, ks, vs.int(), status, weight), (k, v, ks, vs, status.float(), weight), (k, v, ks, vs, status, weight.int())]:
+        with pytest.raises(ValueError):
+            fcp.Cache(*args)
+    table = torch.zeros(2, 3, dtype=torch.int32)
+    for bad in (table.float(), table.bool(), table.short()):
+        with pytest.raises(ValueError, match="int32"):
+            fcp.CacheBatch(bad, batch.tensors[1])
+
+
+def _host_cache():
+    """A cache, a batch of two rows and tensors of its calls, all in host memory."""
+    k = torch.zeros(3, 2, 16, 64, dtype=torch.int8)
+    cache = fcp.Cache(k, k.clone(), torch.ones(3, 2), torch.ones(3, 2), torch.zeros(4, dtype=torch.int32), weight=torch.zeros(3, 2, 16))
+    batch = fcp.CacheBatch(torch.zeros(2, 3, dtype=torch.int32), torch.ones(2, dtype=torch.int32), torch.tensor([0, 1, 2], dtype=torch.int32), rows=2)
+    return cache, batch, torch.zeros(2, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 2)
+
+
 # ------------------------------------------------------------------------------------------ index arithmetic
 INDEX_MAIN = r"""
 #include <cstdio>
