@@ -353,8 +353,8 @@ def _named(names: dict, value) -> int:
     return int(value)
 
 
-# The checks below stand in front of kernels of a few microseconds: one look at type, shape and strides per tensor, no conversions.
-# A tensor of another type would be read as what it is not.
+# The checks below stand in front of kernels of a few microseconds: one look at type, shape, strides and device per tensor, no
+# conversions.  A tensor of another type would be read as what it is not, and one of another place is no address on this GPU.
 _BF16 = _F32 = _I32 = None
 
 
@@ -367,7 +367,7 @@ def _torch_types():
 
 
 def _heads(x, head_dim, name):
-    """Rows, heads, row stride and address of a bf16 tensor [rows][heads][head_dim] whose heads are contiguous."""
+    """Rows, heads, row stride, address and device of a bf16 tensor [rows][heads][head_dim] whose heads are contiguous."""
     rows, heads, d = x.shape
     s0, s1, s2 = x.stride()
     if d != head_dim or s2 != 1 or (s1 != d and heads > 1) or x.dtype is not _BF16:
@@ -376,33 +376,58 @@ def _heads(x, head_dim, name):
         s0 = heads * d
     elif s0 < heads * d:                           # an expanded tensor: its stride 0 means heads * head_dim to the library
         raise ValueError(f"{name}: rows that share memory (row stride {s0}); a row of its own for each is wanted, see Tensor.contiguous")
-    return rows, heads, s0, x.data_ptr()
+    return rows, heads, s0, x.data_ptr(), x.get_device()
 
 
-_NO_HEADS = (None, 0, 0, None)
+_NO_HEADS = (None, 0, 0, None, None)
 
 
-def _i32_ptr(x, n, name):
-    """Address of a contiguous int32 device tensor of n entries (None: NULL)."""
+def _i32_ptr(x, n, name, device=None):
+    """Address of a contiguous int32 device tensor of n entries (None: NULL), of that device if one is given."""
     if x is None:
         return None
     if x.dtype is not _I32 or x.numel() != n or not x.is_contiguous():
         raise ValueError(f"{name}: a contiguous int32 tensor of {n} entries is wanted")
+    if device is not None and x.get_device() != device:
+        _elsewhere(device)
     return x.data_ptr()
+
+
+def _elsewhere(device):
+    raise ValueError("the tensors of a call are wanted on one GPU" + (f", here cuda:{device}" if device >= 0 else ""))
+
+
+_ONE_DEVICE = None                                 # whether there is one GPU only; not known yet
+
+
+def _not_current(device) -> bool:
+    global _ONE_DEVICE
+    import torch
+    if _ONE_DEVICE is None:
+        _ONE_DEVICE = torch.cuda.device_count() == 1
+    return not _ONE_DEVICE and device != torch.cuda.current_device()
 
 
 def _rope(call, table, q, k, q_out, k_out, positions, row_offset, length, stream):
     d = table.head_dim
-    rows, hq, qs, qp = _NO_HEADS if q is None else _heads(q, d, "q")
-    k_rows, hkv, ks, kp = _NO_HEADS if k is None else _heads(k, d, "k")
-    q_out_rows, hq_out, qos, qop = _NO_HEADS if q_out is None else _heads(q_out, d, "q_out")
-    k_out_rows, hkv_out, kos, kop = _NO_HEADS if k_out is None else _heads(k_out, d, "k_out")
+    rows, hq, qs, qp, qd = _NO_HEADS if q is None else _heads(q, d, "q")
+    k_rows, hkv, ks, kp, kd = _NO_HEADS if k is None else _heads(k, d, "k")
+    q_out_rows, hq_out, qos, qop, qod = _NO_HEADS if q_out is None else _heads(q_out, d, "q_out")
+    k_out_rows, hkv_out, kos, kop, kod = _NO_HEADS if k_out is None else _heads(k_out, d, "k_out")
     if hq_out != hq or hkv_out != hkv or q_out_rows != rows or k_out_rows != k_rows or (q is not None and k is not None and k_rows != rows):
         raise ValueError("q, k, q_out, k_out differ in rows or heads")
     T = rows or k_rows or 0
     B = 0 if row_offset is None else row_offset.numel() - 1
-    rc = call(table.ref, T, qp, qs, hq, kp, ks, hkv, qop, qos, kop, kos, _i32_ptr(positions, T, "positions"),
-              _i32_ptr(row_offset, B + 1, "row_offset"), _i32_ptr(length, B, "length"), B, stream)
+    device = None
+    if T:
+        device = kd if qd is None else qd
+        if device < 0 or qod != qd or kod != kd or (qd is not None and kd is not None and kd != qd):
+            _elsewhere(device)
+    positions, row_offset, length = (_i32_ptr(positions, T, "positions", device), _i32_ptr(row_offset, B + 1, "row_offset", device),
+                                     _i32_ptr(length, B, "length", device))
+    if T and not _ONE_DEVICE and _not_current(device):
+        raise ValueError(f"the tensors lie on cuda:{device}, which is not the current device")
+    rc = call(table.ref, T, qp, qs, hq, kp, ks, hkv, qop, qos, kop, kos, positions, row_offset, length, B, stream)
     if rc:
         _check(rc)
 
@@ -441,6 +466,9 @@ class Cache:
                                 (weight, (n_pages, hkv, page_tokens), _F32), (status, (4,), _I32)):
             if x is not None and (tuple(x.shape) != tuple(shape) or not x.is_contiguous() or not (x.dtype is dtype if dtype else x.dtype.itemsize == 1)):
                 raise ValueError(f"a contiguous tensor {tuple(shape)} of {dtype or '1-byte values'} is wanted, not {tuple(x.shape)} {x.dtype}")
+        self.device = k.get_device()                 # -1: host memory, which the library's calls refuse
+        if any(x is not None and x.get_device() != self.device for x in (v, k_scale, v_scale, status, weight)):
+            raise ValueError("the tensors of a cache lie on different devices")
         self.hkv, self.head_dim, self.page_tokens, self.n_pages = hkv, head_dim, page_tokens, n_pages
         self.tensors = (k, v, k_scale, v_scale, status, weight)          # the pages live as long as the handle
         ptr = [None if x is None else x.data_ptr() for x in (k, v, k_scale, v_scale, weight, status)]
@@ -468,6 +496,9 @@ class CacheBatch:
         _torch_types()
         B, width = page_table.shape
         self.tensors = (page_table, length, row_offset)
+        self.device = page_table.get_device()
+        if any(x is not None and x.get_device() != self.device for x in (length, row_offset)):
+            raise ValueError("the tensors of a batch lie on different devices")
         self.B, self.rows = B, int(rows)
         self.struct = FcpCacheBatch(B, self.rows, int(rows if max_new is None else max_new), width,
                                     _i32_ptr(page_table, B * width, "page_table"), _i32_ptr(length, B, "length"),
@@ -475,11 +506,23 @@ class CacheBatch:
         self.ref = C.byref(self.struct)
 
 
+def _on_cache(cache: Cache, batch: CacheBatch, *devices):
+    """Everything where the pages are.  (Pages in host memory are left to the library, which refuses them.)"""
+    device = cache.device
+    if device >= 0:
+        if batch.device != device:
+            raise ValueError(f"the cache lies on cuda:{device}, the batch does not")
+        for d in devices:
+            if d != device:
+                _elsewhere(device)
+
+
 def fcp_cache_append(cache: Cache, batch: CacheBatch, k, v, stream=0):
-    k_rows, k_heads, ks, kp = _heads(k, cache.head_dim, "k")
-    v_rows, v_heads, vs, vp = _heads(v, cache.head_dim, "v")
+    k_rows, k_heads, ks, kp, kd = _heads(k, cache.head_dim, "k")
+    v_rows, v_heads, vs, vp, vd = _heads(v, cache.head_dim, "v")
     if k_rows != batch.rows or v_rows != batch.rows or k_heads != cache.hkv or v_heads != cache.hkv:
         raise ValueError(f"k, v: {batch.rows} rows of {cache.hkv} heads are wanted")
+    _on_cache(cache, batch, kd, vd)
     rc = lib().fcp_cache_append(cache.handle, batch.ref, kp, ks, vp, vs, stream)
     if rc:
         _check(rc)
@@ -492,14 +535,16 @@ def fcp_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, hq) -> int:
 
 
 def fcp_cache_attn(cache: Cache, batch: CacheBatch, q, o, lse, workspace, workspace_bytes, scale=0.0, accumulate=False, stream=0):
-    rows, hq, qs, qp = _heads(q, cache.head_dim, "q")
-    o_rows, o_heads, _, op = _heads(o, cache.head_dim, "o")
+    rows, hq, qs, qp, qd = _heads(q, cache.head_dim, "q")
+    o_rows, o_heads, _, op, od = _heads(o, cache.head_dim, "o")
     if rows != batch.rows or o_rows != rows or o_heads != hq or not o.is_contiguous():
         raise ValueError(f"q, o: {batch.rows} rows of the same heads are wanted, o contiguous")
     if lse.numel() != rows * hq or lse.dtype is not _F32 or not lse.is_contiguous():
         raise ValueError("lse: a contiguous fp32 tensor [rows][hq] is wanted")
+    wd = cache.device if workspace is None else workspace.get_device()
     if workspace is not None and (workspace.nbytes < workspace_bytes or not workspace.is_contiguous()):
         raise ValueError(f"workspace: contiguous, of at least the {workspace_bytes} bytes that the call names")
+    _on_cache(cache, batch, qd, od, lse.get_device(), wd)
     rc = lib().fcp_cache_attn(cache.handle, batch.ref, qp, qs, hq, scale, op, lse.data_ptr(), 1 if accumulate else 0,
                               None if workspace is None else workspace.data_ptr(), workspace_bytes, stream)
     if rc:
@@ -511,6 +556,7 @@ def fcp_cache_evict(cache: Cache, batch: CacheBatch, n_sink, n_heavy, n_recent, 
     if B != batch.B:
         raise ValueError("dst_table and the batch differ in their number of sequences")
     keep = int(n_sink) + int(n_heavy) + int(n_recent)
+    _on_cache(cache, batch, dst_table.get_device(), new_length.get_device(), kept.get_device())
     _check(lib().fcp_cache_evict(cache.handle, batch.ref, int(n_sink), int(n_heavy), int(n_recent),
                                  _i32_ptr(dst_table, B * width, "dst_table"), width, _i32_ptr(new_length, B, "new_length"),
                                  _i32_ptr(kept, B * cache.hkv * keep, "kept"), stream))

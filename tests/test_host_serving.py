@@ -239,6 +239,60 @@ def _host_cache():
     return cache, batch, torch.zeros(2, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 2)
 
 
+class _Elsewhere:
+    """A tensor of host memory that says it lies on a GPU."""
+
+    def __init__(self, x, device):
+        self.x, self.device_number = x, device
+
+    def get_device(self):
+        return self.device_number
+
+    def __getattr__(self, name):
+        return getattr(self.x, name)
+
+
+def test_binding_refuses_tensors_of_other_devices():
+    t, x = fcp.RopeTable(64), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    off = torch.tensor([0, 2], dtype=torch.int32)
+    for args in [(x, None, x, None), (None, x, None, x), (x, x, x, x)]:
+        with pytest.raises(ValueError, match="one GPU"):
+            fcp.fcp_rope_fwd(t, *args, row_offset=off)
+    here = lambda y: _Elsewhere(y, 0)
+    for args in [(here(x), None, x, None), (here(x), None, _Elsewhere(x, 1), None), (here(x), here(x), here(x), x)]:
+        with pytest.raises(ValueError, match="one GPU"):
+            fcp.fcp_rope_fwd(t, *args, row_offset=here(off))
+    with pytest.raises(ValueError, match="one GPU"):
+        fcp.fcp_rope_fwd(t, here(x), None, here(x), None, row_offset=off)
+    cache, batch, x, lse = _host_cache()
+    k, v, ks, vs, status, weight = cache.tensors
+    for i in range(6):
+        parts = [here(y) for y in (k, v, ks, vs, status, weight)]
+        parts[i] = parts[i].x
+        with pytest.raises(ValueError, match="different devices"):
+            fcp.Cache(*parts, kind="int8")
+    table, length, row_offset = batch.tensors
+    for args in [(here(table), length, here(row_offset)), (here(table), here(length), row_offset)]:
+        with pytest.raises(ValueError, match="different devices"):
+            fcp.CacheBatch(*args, rows=2)
+    cache.device = 0                                              # as if its pages were there
+    for b in (batch, fcp.CacheBatch(_Elsewhere(table, 1), _Elsewhere(length, 1), _Elsewhere(row_offset, 1), rows=2)):
+        with pytest.raises(ValueError, match="batch does not"):
+            fcp.fcp_cache_append(cache, b, here(x), here(x))
+    there = fcp.CacheBatch(here(table), here(length), here(row_offset), rows=2)
+    for args in [(x, here(x)), (here(x), x), (here(x), _Elsewhere(x, 1))]:
+        with pytest.raises(ValueError, match="one GPU"):
+            fcp.fcp_cache_append(cache, there, *args)
+    ws = torch.zeros(16, dtype=torch.uint8)
+    for args in [(x, here(x), here(lse), here(ws)), (here(x), x, here(lse), here(ws)), (here(x), here(x), lse, here(ws)), (here(x), here(x), here(lse), ws)]:
+        with pytest.raises(ValueError, match="one GPU"):
+            fcp.fcp_cache_attn(cache, there, *args, 16)
+    kept = torch.zeros(2, 2, 3, dtype=torch.int32)
+    for args in [(table, here(length), here(kept)), (here(table), length, here(kept)), (here(table), here(length), kept)]:
+        with pytest.raises(ValueError, match="one GPU"):
+            fcp.fcp_cache_evict(cache, there, 1, 1, 1, *args)
+
+
 # ------------------------------------------------------------------------------------------ index arithmetic
 INDEX_MAIN = r"""
 #include <cstdio>
