@@ -387,7 +387,8 @@ int fcp_rope_init(const fcp_rope_config* config, fcp_rope_table* table);
  * length[b] - (row_offset[b+1] - row_offset[b]) + t - row_offset[b], i.e. the rows are the last ones of sequences of those
  * lengths, as in the calls on a cache below.  Rows outside [row_offset[0], row_offset[B]) are left as they were.
  * Arithmetic in fp32, one rounding to bf16.  Asynchronous on `stream`; no workspace.
- * Errors: INVALID_ARG (NULL, T < 0 or >= 2^31, B < 0, a stride below heads * D, head counts < 0).
+ * Errors: INVALID_ARG (NULL, T < 0 or >= 2^31 - 8, B < 0 or >= 2^31 - 256, a stride below heads * D, head counts < 0 or above 65536
+ * together).
  */
 int fcp_rope_fwd(const fcp_rope_table* table, int64_t T, const void* q, int64_t q_stride, int32_t hq, const void* k,
                  int64_t k_stride, int32_t hkv, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
@@ -495,7 +496,7 @@ int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const v
  * among the batch's source pages: codes, weights, and per page and head the largest scale among the pages its tokens came
  * from (codes are rounded again where their own was smaller).  new_length [B], kept [B][hkv][n_sink+n_heavy+n_recent] (position
  * of each kept token, -1 behind the last) are written.  The cache needs weights.  row_offset, rows and max_new of the batch
- * are not used.  new_length is 0 for an absent sequence.  A token on an absent source page is kept as zeros.
+ * are not used.  n_sink + n_heavy + n_recent is 1 .. 2^31 - 8192.  new_length is 0 for an absent sequence.  A token on an absent source page is kept as zeros.
  */
 int fcp_cache_evict(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t n_sink, int32_t n_heavy, int32_t n_recent,
                     const int32_t* dst_table, int32_t dst_width, int32_t* new_length, int32_t* kept, void* stream);

@@ -451,7 +451,8 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const fcp_cache_batch* ba
     fcp_set_error("%s: the cache has no weights", call);
     return FCP_ERR_INVALID_ARG;
   }
-  if (n_sink < 0 || n_heavy < 0 || n_recent < 0 || keep < 1 || keep >= int64_t(1) << 31 || dst_width < 1 ||
+  // positions of kept tokens are gone through in steps of up to SELECT_BLOCKS * SELECT_THREADS, in 32 bits
+  if (n_sink < 0 || n_heavy < 0 || n_recent < 0 || keep < 1 || keep > (int64_t(1) << 31) - SELECT_BLOCKS * SELECT_THREADS || dst_width < 1 ||
       (int64_t)dst_width * c.page_tokens < keep) {
     fcp_set_error("%s: %d + %d + %d tokens to keep on %d pages of %d", call, n_sink, n_heavy, n_recent, dst_width, c.page_tokens);
     return FCP_ERR_INVALID_ARG;

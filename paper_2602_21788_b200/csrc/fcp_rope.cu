@@ -240,7 +240,8 @@ __global__ void __launch_bounds__(ROPE_THREADS, ROPE_RESIDENT) rope_kernel(const
 int rope(const char* call, float sign, const fcp_rope_table* table, int64_t T, const void* q, int64_t q_stride, int32_t hq,
          const void* k, int64_t k_stride, int32_t hkv, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
          const int32_t* positions, const int32_t* row_offset, const int32_t* length, int32_t B, void* stream) {
-  if (!table || T < 0 || T >= (int64_t(1) << 31) - 8 || hq < 0 || hkv < 0 || B < 0 || (int64_t)hq + hkv > 65536 ||
+  // the search for a row's sequence looks up to a block's threads behind the last one
+  if (!table || T < 0 || T >= (int64_t(1) << 31) - 8 || hq < 0 || hkv < 0 || B < 0 || B >= (int64_t(1) << 31) - ROPE_THREADS || (int64_t)hq + hkv > 65536 ||
       (T > 0 && ((hq > 0 && (!q || !q_out)) || (hkv > 0 && (!k || !k_out)) || (!positions && !row_offset)))) {
     fcp_set_error("%s: NULL buffer or invalid size", call);
     return FCP_ERR_INVALID_ARG;

@@ -195,6 +195,25 @@ def test_binding_checks_shapes():
 
 
 
+def test_sizes_next_to_2_to_the_31_are_refused():
+    """Where the kernels' 32-bit loops would pass the end: 2^31 - 8192 kept tokens are the most, 2^31 - 257 sequences of rotary calls."""
+    L, t = fcp.lib(), fcp.RopeTable(64)
+    buf, c = _config()
+    h = C.c_void_p()
+    assert L.fcp_cache_create(C.byref(c), C.byref(h)) == 0
+    p = c.k
+    batch = C.byref(fcp.FcpCacheBatch(0, 0, 0, 3, p, p, p))          # no sequences: what is not refused does nothing
+    evict = lambda *keep: L.fcp_cache_evict(h, batch, *keep, p, 1 << 27, p, p, None)
+    assert evict(4, (1 << 31) - 8192 - 20, 16) == evict((1 << 31) - 8192, 0, 0) == 0
+    for keep in ((4, (1 << 31) - 8191 - 20, 16), ((1 << 31) - 8191, 0, 0), (0, 0, (1 << 31) - 1), (0, (1 << 31) - 1, 0)):
+        assert evict(*keep) == fcp.FCP_ERR_INVALID_ARG, keep
+    assert L.fcp_cache_destroy(h) == 0
+    for f in (L.fcp_rope_fwd, L.fcp_rope_bwd):
+        rope = lambda B: f(t.ref, 0, p, 0, 1, None, 0, 0, p, 0, None, 0, None, p, None, B, None)
+        assert rope((1 << 31) - 257) == 0
+        assert rope((1 << 31) - 256) == rope((1 << 31) - 1) == fcp.FCP_ERR_INVALID_ARG
+
+
 def test_binding_refuses_types_and_rows_that_share_memory():
     """Expanded tensors (row stride 0, which the library takes for dense rows), other 2-byte and 4-byte types."""
     t = fcp.RopeTable(64)
