@@ -417,7 +417,8 @@ int fcp_rope_bwd(const fcp_rope_table* table, int64_t T, const void* dq, int64_t
  * fall, leave [0, rows] or span more than max_new rows, counts as absent (its rows are not written); tokens on a page
  * outside [0, n_pages) or, in fcp_cache_attn and fcp_cache_evict, on a page whose scale is not in
  * [FCP_CACHE_MIN_SCALE, FCP_CACHE_MAX_SCALE], count as absent.  status then holds FCP_ERR_INVALID_ARG, one of the
- * FCP_CACHE_BAD_* codes and the sequence (first failure, sticky); FCP_ERR_TIMEOUT as everywhere.
+ * FCP_CACHE_BAD_* codes and the sequence (first failure, sticky); FCP_ERR_TIMEOUT as everywhere.  Where row offsets fall, fcp_cache_append
+ * may leave out new tokens of the sequences beside the bad one too.
  * The calls write nothing but what is listed, whatever the tables hold.
  * Two calls on one cache must be stream-ordered if one of them writes what the other uses.  The device that holds the cache must be
  * the current one.  The first compute call of a handle looks up the device and sets the kernels up; make it outside any capture.

@@ -170,6 +170,12 @@ __global__ void __launch_bounds__(append_threads(WARPS)) cache_append_kernel(con
       hi = min(hi, lo + step - 1);
     }
     b = lo;
+    // offsets that fall can keep the search from a sequence, so one block looks at them all
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+      for (int i = threadIdx.x; i < a.s.B; i += THREADS) {
+        const int32_t bad = load_seq(a.s, i).bad;
+        if (bad) mark_bad(a.c.status, bad, i);
+      }
   }
   if (h >= a.c.hkv) return;
   const SeqView sv = load_seq(a.s, b);

@@ -1085,3 +1085,23 @@ def test_chunks_with_values_beyond_bf16(kind, d):
     for b, j in at.items():                                       # the rows in front of it know nothing of it
         assert not great[w.off[b]:w.off[b] + j].any() and held[w.off[b]:w.off[b] + j].all()
     assert great[w.off[0] + at[0]:w.off[1]].any() and great[w.off[1] + at[1]:w.off[2]].any()
+
+
+@pytest.mark.parametrize("page,rows,off", [(64, 240, [17, 187, 31, 80, 161, 236, 239]), (16, 160, [29, 30, 59, 124, 82, 141]), (128, 341, [46, 54, 282, 68, 149, 161, 173, 289]),
+                                           (16, 55, [8, 24, 28, 32, 41, 3, 45, 48]), (32, 190, [19, 61, 72, 5, 93, 119, 186]), (16, 40, [0, 20, 41])])
+def test_append_reports_offsets_that_fall(page, rows, off):
+    """Whichever sequences the search for a page's sequence finds: the bad one is reported, and only pages of the batch are written."""
+    B = len(off) - 1
+    w = World(87, "int8", page, 2, 64, [400] * B).up()
+    was = w.now()
+    k = bf16(w.rng, rows, 2, 64).cuda()
+    fcp.fcp_cache_append(w.cache, fcp.CacheBatch(dev(w.table), dev(w.length), dev(off), rows=rows), k, k, stream=stream())
+    bad = [b for b in range(B) if off[b + 1] < off[b] or off[b + 1] > rows]
+    st = w.cache.device_status().tolist()
+    assert st[:2] == [fcp.FCP_ERR_INVALID_ARG, fcp.FCP_CACHE_BAD_ROWS] and st[2] in bad
+    now = w.now()
+    good = [b for b in range(B) if b not in bad]
+    touched = {int(w.table[b][p // page]) for b in good for p in range(400 - (off[b + 1] - off[b]), 400)}
+    for p in range(w.n_pages):
+        if p not in touched:
+            assert np.array_equal(now["k"][p], was["k"][p], equal_nan=True) and np.array_equal(now["v_scale"][p], was["v_scale"][p])
