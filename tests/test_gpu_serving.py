@@ -1105,3 +1105,63 @@ def test_append_reports_offsets_that_fall(page, rows, off):
     for p in range(w.n_pages):
         if p not in touched:
             assert np.array_equal(now["k"][p], was["k"][p], equal_nan=True) and np.array_equal(now["v_scale"][p], was["v_scale"][p])
+
+
+def check_weights(w, was, new, hq, r):
+    """Every weight against the definition: a score's fp32 error three times (score, and the log-sum-exp's own), and the sum over rows."""
+    want, tol = was.copy(), F32 * 4 * np.abs(was) + 1e-30
+    score = w.d * 2 * F32 * r["size"].max() + 2.0 ** -20
+    for b, t in enumerate(w.length):
+        rows = new[b] * hq // w.hkv
+        for p in range(t):
+            page_id, slot = w.table[b][p // w.page], p % w.page
+            want[page_id, :, slot] += r["weights"][b][:, p]
+            tol[page_id, :, slot] += r["weights"][b][:, p] * (3 * score + (64 + rows / 4) * F32)
+    now = w.now()["weight"]
+    assert np.all(np.abs(now - want) <= tol), np.max(np.abs(now - want) / tol)
+
+
+@pytest.mark.parametrize("kind,page,d", [("e4m3", 16, 64), ("int8", 16, 128), ("int8", 64, 64), ("e4m3", 128, 128)])
+@pytest.mark.parametrize("hkv,group,new,before", [(8, 8, [300], [0]), (8, 8, [257, 0, 1], [70, 300, 5]), (8, 6, [300, 40, 257], [129, 0, 300])])
+def test_weights_that_long_chunks_leave(kind, page, d, hkv, group, new, before):
+    w = World(88, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    assert goes_by_copies(w, new, hkv * group)
+    state, was = w.state(), w.now()["weight"]
+    q, o, lse, rows = attend(w, new, hkv * group, accumulate=True)
+    r = R.attention(state, w.table, w.length, w.off, f64(q)[:rows])
+    check_weights(w, was, new, hkv * group, r)
+
+
+@pytest.mark.parametrize("kind,page,hkv,d", [("e4m3", 16, 2, 64), ("int8", 128, 2, 128)])
+@pytest.mark.parametrize("group,new,before", [(1, [33, 0, 128], [0, 40, 500]), (4, [9, 1, 31, 0], [1500, 3, 130, 64]), (2, [200], [500]), (8, [16, 16, 1], [127, 5, 2000])])
+def test_weights_that_many_rows_leave(kind, page, hkv, d, group, new, before):
+    w = World(89, kind, page, hkv, d, [a + n for a, n in zip(before, new)]).fill().up()
+    assert not goes_by_copies(w, new, hkv * group)
+    state, was = w.state(), w.now()["weight"]
+    q, o, lse, rows = attend(w, new, hkv * group, accumulate=True)
+    r = R.attention(state, w.table, w.length, w.off, f64(q)[:rows])
+    check_weights(w, was, new, hkv * group, r)
+
+
+def test_weights_of_a_chunk_with_sequences_that_need_care():
+    """Tokens on a page that does not exist get none; a sequence with more rows than tokens leaves those of its tokens."""
+    new, hkv, group = [140, 150, 133], 4, 8
+    w = World(90, "int8", 16, hkv, 64, [300, 90, 200]).fill()
+    good, table = w.state(), w.table.copy()
+    w.table[2, 1] = w.n_pages + 5
+    w.up()
+    assert goes_by_copies(w, new, hkv * group)
+    was = w.now()["weight"]
+    q, o, lse, rows = attend(w, new, hkv * group, accumulate=True, spare=0)
+    r = R.attention(good, table, w.length, w.off, f64(q))
+    added = w.now()["weight"] - was
+    sums = added[table[0][:19]].sum(axis=(0, 2)), added[table[1][:6]].sum(axis=(0, 2)), added[table[2][:13]].sum(axis=(0, 2))
+    for got, n in zip(sums, (140, 90, 133)):
+        assert np.allclose(got, n * group, rtol=1e-4)
+    assert np.all(added[table[2][1]] == 0)
+    score = 64 * 2 * F32 * r["size"].max() + 2.0 ** -20
+    for b in (0, 1):
+        for p in range(w.length[b]):
+            want = r["weights"][b][:, p]
+            got = added[table[b][p // 16], :, p % 16]
+            assert np.all(np.abs(got - want) <= want * (3 * score + 400 * F32) + 8 * F32)
