@@ -1165,3 +1165,24 @@ def test_weights_of_a_chunk_with_sequences_that_need_care():
             want = r["weights"][b][:, p]
             got = added[table[b][p // 16], :, p % 16]
             assert np.all(np.abs(got - want) <= want * (3 * score + 400 * F32) + 8 * F32)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunks_with_nan_keys_among_the_new_tokens(d):
+    """By copies: a NaN key of a new token reaches the rows that see it and no others, and no other sequence; stale NaN codes behind the length none."""
+    new, hkv, group = [200, 150, 133], 4, 8
+    w = World(91, "e4m3", 16, hkv, d, [300, 150, 200]).fill()
+    w.codes["k"][w.table[0][230 // 16], 1, 230 % 16, 3] = 0x7f
+    w.codes["k"][w.table[1][149 // 16], 2, 149 % 16, 0] = 0xff
+    w.up()
+    assert goes_by_copies(w, new, hkv * group)
+    q, o, lse, rows = attend(w, new, hkv * group, spare=0)
+    with np.errstate(invalid="ignore"):
+        r = R.attention(w.state(), w.table, w.length, w.off, f64(q))
+    got, got_lse = f64(o), f64(lse)
+    bad = np.isnan(r["lse"])
+    assert bad[130:200, 8:16].all() and bad[349, 16:24].all() and bad.sum() == 70 * 8 + 8
+    assert np.array_equal(np.isnan(got_lse), bad) and np.isnan(got[bad]).all()
+    score = d * 2 * F32 * np.nan_to_num(r["size"]) + 2.0 ** -20
+    bound = BF16 * np.abs(r["o"]) + (BF16 + 2 * score[..., None]) * r["spread"] * (1 + BF16) + 1e-30
+    assert np.all((np.abs(got - r["o"]) <= bound)[~bad])
