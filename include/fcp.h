@@ -385,7 +385,8 @@ int fcp_rope_init(const fcp_rope_config* config, fcp_rope_table* table);
  * Positions: `positions` [T] (device), or, if NULL, from row_offset [B+1] (device), the packed batch's offsets: token t
  * of sequence b stands at t - row_offset[b], with length [B] (device; NULL: not used) at
  * length[b] - (row_offset[b+1] - row_offset[b]) + t - row_offset[b], i.e. the rows are the last ones of sequences of those
- * lengths, as in the calls on a cache below.  Rows outside [row_offset[0], row_offset[B]) are left as they were.
+ * lengths, as in the calls on a cache below.  (Not after fcp_cache_evict: the lengths are smaller then, but the kept keys keep the turn of
+ * their old positions, so `positions` has to say where new tokens stand.)  Rows outside [row_offset[0], row_offset[B]) are left as they were.
  * Arithmetic in fp32, one rounding to bf16.  Asynchronous on `stream`; no workspace.
  * Errors: INVALID_ARG (NULL, T < 0 or >= 2^31 - 8, B < 0 or >= 2^31 - 256, a stride below heads * D, head counts < 0 or above 65536
  * together).
@@ -412,6 +413,9 @@ int fcp_rope_bwd(const fcp_rope_table* table, int64_t T, const void* dq, int64_t
  * row_offset[b] .. row_offset[b+1]-1 are the last tokens of sequence b, whose length includes them.  row_offset, length
  * and page_table are read on the device, so a captured call can be replayed with new contents; rows, max_new and
  * table_width bound them on the host.  Rows behind row_offset[B] are neither read nor written.
+ * fcp_cache_attn chooses its kernels, and the size of its workspace, as if every sequence had max_new new tokens and a full row of the
+ * page table.  So max_new and table_width should be no larger than the batch needs, and a chunk of a prompt beside sequences with
+ * single tokens is faster, and takes a smaller workspace, as two calls.
  *
  * What the kernels check: a sequence with a length outside [0, table_width * page_tokens], or with row offsets that
  * fall, leave [0, rows] or span more than max_new rows, counts as absent (its rows are not written); tokens on a page
@@ -446,7 +450,7 @@ typedef struct fcp_cache_config {
 typedef struct fcp_cache_batch {
   int32_t B;                         /* sequences                                              */
   int32_t rows;                      /* rows of the call's tensors                             */
-  int32_t max_new;                   /* no sequence has more new tokens than this              */
+  int32_t max_new;                   /* no sequence has more new tokens than this; 1 for single tokens */
   int32_t table_width;               /* columns of page_table; times page_tokens <= 2^31 - 256 */
   const int32_t* page_table;         /* device [B][table_width]                                */
   const int32_t* length;             /* device [B]                                             */
@@ -465,7 +469,7 @@ int fcp_cache_device_status(const fcp_cache* cache, int32_t* status);
  * x / scale rounded to the nearest (ties to even), infinities the largest code, NaN the NaN code (int8: 0); where the scale
  * grew, the earlier codes are code * (old / scale), rounded.  Powers of two keep a floating code exact through that, as
  * long as it is not subnormal.  weight, if there is one, is set to 0 at the new tokens.
- * A page that takes new tokens must belong to one sequence only.  Calling again with the same arguments changes nothing.
+ * A page that takes new tokens must belong to one sequence only, and stand in its row of the table once.  Calling again with the same arguments changes nothing.
  */
 int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const void* k, int64_t k_stride, const void* v,
                      int64_t v_stride, void* stream);
@@ -474,7 +478,8 @@ int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const
  * a sequence of length L sees the keys at positions <= L - n + j,
  *     o = softmax(q k^T * scale) v,   lse = natural log of the sum of exp(scaled scores)
  * q bf16 [rows][hq][D] with q_stride, o bf16 [rows][hq][D], lse fp32 [rows][hq]; hq % hkv == 0; scale <= 0 means
- * 1/sqrt(D).  A row that sees nothing gets o = 0 and lse = -infinity.  Pages may be shared by sequences.
+ * 1/sqrt(D).  A row that sees nothing gets o = 0 and lse = -infinity.  Pages may be shared by sequences.  The outputs and the workspace
+ * must not overlap the inputs or one another.
  * accumulate != 0: weight of every cached token += its attention weight, summed over the sequence's new tokens and the
  * query heads of its KV head (what fcp_cache_evict goes by).
  * workspace: device, 256-byte aligned, of at least fcp_cache_attn_workspace_bytes; its contents need not be initialised; two calls
@@ -483,8 +488,8 @@ int fcp_cache_append(const fcp_cache* cache, const fcp_cache_batch* batch, const
  * 2^-33 of the row's largest: a page with an infinite value leaves next to nothing of the others' for the rows that see any of its
  * tokens), and in calls with many new tokens, which go through bf16 copies of the codes in the workspace (up to 8 GB, where that is
  * faster), to bf16, as is code * scale where a scale is no power of two; beyond the largest bf16 it counts as that.  A row with a score of
- * 2^128 log 2 or more (in calls by copies 2^30) has no defined result.  The same call gives the same bits again, unless sequences of one
- * call share a page and accumulate.
+ * 2^128 log 2 or more (in calls by copies 2^30) has no defined result.  The same call gives the same bits again, unless it accumulates
+ * and a page stands in its tables more than once.
  */
 int fcp_cache_attn_workspace_bytes(const fcp_cache* cache, const fcp_cache_batch* batch, int32_t hq, int64_t* bytes);
 int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const void* q, int64_t q_stride, int32_t hq,
@@ -494,7 +499,7 @@ int fcp_cache_attn(const fcp_cache* cache, const fcp_cache_batch* batch, const v
 /* fcp_cache_evict — device.  Cuts sequences to n_sink + n_heavy + n_recent tokens per KV head: the first n_sink, the last
  * n_recent, and of those between the n_heavy of largest weight (equal ones: the earlier; NaN: last); a sequence that has no more
  * is kept whole.  The kept tokens go, in their order, to the pages dst_table [B][dst_width] (device), which must not be
- * among the batch's source pages: codes, weights, and per page and head the largest scale among the pages its tokens came
+ * among the batch's source pages and stand in dst_table once each: codes, weights, and per page and head the largest scale among the pages its tokens came
  * from (codes are rounded again where their own was smaller).  new_length [B], kept [B][hkv][n_sink+n_heavy+n_recent] (position
  * of each kept token, -1 behind the last) are written.  The cache needs weights.  row_offset, rows and max_new of the batch
  * are not used.  n_sink + n_heavy + n_recent is 1 .. 2^31 - 8192.  new_length is 0 for an absent sequence.  A token on an absent source page is kept as zeros.

@@ -23,7 +23,7 @@ namespace {
 
 // Row tiles in blocks of 8 rows: the smallest that holds a KV head's rows.  1, 2 and 4 blocks go by cache_attn_kernel, whose time grows
 // with the rows, 16 by cache_tile_kernel, whose time does not.  16 sequences of 4K to 32K tokens, 40/8 heads, int8, us, the one against the
-// other: 25 rows per KV head 189, 218; 35 rows (8 blocks) 323, 224; 100 rows (16 blocks) 599, 239.
+// other: 25 rows per KV head 178, 220; 35 rows (in tiles of 32) 325, 224; 100 rows 645, 237; e4m3 156, 214; 286, 218; 569, 235.
 constexpr int kWeights = 0;
 int row_blocks(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 ? 4 : TILE_ROWS / 8; }
 
@@ -172,8 +172,9 @@ int64_t chunk_stride(const fcp_cache_config& c, const fcp_cache_batch& b) {
 // take, in clk of the device per tile of 128 keys.  cache_tile_kernel: 4800 per KV head and 128 rows, spread over all SMs.  The other way:
 // 5900 per KV head for the copies; fcp_fwd_kernel takes 1700 per query head and tile of 128 new tokens, 1270 where two run beside
 // each other, and no item is cut along the keys.  4 sequences of 6K to 12K tokens, 32/8 heads, int8, us, copies against not: 512 new
-// tokens 294, 541; 256 235, 291; 192 244, 229 (goes by copies); 128 188, 171; 64 196, 110; one sequence, 256 165, 128.  The copies may
-// take up to 8 GB.
+// tokens 319, 535; 256 237, 291; 192 242, 228 (the rule takes the copies there, 6 % slower); 128 186, 174; 64 195, 110; one sequence, 256
+// 163, 128.  The copies may take up to 8 GB; beyond that calls go without.  Every sequence counts as having max_new new tokens, and the
+// copies are laid out for the table's width: one chunk beside single tokens is better two calls, as the header says.
 constexpr int64_t kChunkBytes = int64_t(8) << 30;
 bool in_chunks(const fcp_cache_config& c, const fcp_cache_batch& b, int32_t hq) {
   const int64_t tokens = b.B * chunk_stride(c, b), units = (int64_t)b.B * ((b.max_new + FCP_FWD_UNIT_ROWS - 1) / FCP_FWD_UNIT_ROWS);

@@ -402,7 +402,7 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) { return h2_bi
 
 // How the tiles of a batch lie in a row: sequence after sequence, its KV heads, their row tiles, their key tiles.
 // A group counts for GROUP_COST tiles more than it has, for what its queries and its end take.  64 sequences of 300 to 8K tokens, 8 KV heads,
-// us: 0 tiles 105, 1 tile 84, 2 tiles 73, 4 tiles 70 with pages of 128; 112, 92, 94, 99 with pages of 16.
+// us: 0 tiles 114, 1 tile 90, 2 tiles 78, 4 tiles 72 with pages of 128; 114, 90, 79, 82 with pages of 16.
 struct TileOrder {
   static constexpr int GROUP_COST = 2;
   int32_t rows_per_tile, group, hkv;
@@ -1224,9 +1224,9 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant_
 // all rows, S = Q K^T and O += P V run on 128 rows whether they are all there or not (1024 clk per tile of 128 keys, D = 128), and
 // sixteen warps keep the softmax, a quarter of a row per thread, with P and O in tensor memory.  A tile takes about 4400 clk, neither
 // the products' nor the bytes' time: codes to halves (2000 to 3000 clk), the softmax warps' way from S to P (of it 1000 for the
-// exponentials) and the products wait for one another.  16 sequences of 4K to 32K tokens, 40/8 heads, us: 224 for 35 rows, 239 for 100 rows
-// per KV head with int8, 228 with e4m3; cache_attn_kernel took 323 and 599 with int8.
-// Tried, with eight softmax warps: as it stands, 222, 236 and 247 us; V's halves in one buffer 253 for 35 rows; masking rows that do not
+// exponentials) and the products wait for one another.  16 sequences of 4K to 32K tokens, 40/8 heads, us: 224 for 35 rows, 237 for 100 rows
+// per KV head with int8, 218 and 235 with e4m3; cache_attn_kernel takes 325 and 645, 286 and 569.
+// Tried, with eight softmax warps: 222, 236 with int8 and 247 for 100 rows with e4m3; V's halves in one buffer 253 for 35 rows; masking rows that do not
 // exist 245; the next scores fetched before P is handed over 232; even and odd tiles to four softmax warps each, with an output of
 // their own, 264; polling in front of waits 228; halves made before their place is free 221, e4m3 249.  Four converting warps for K
 // and four for V took 142 against 111 (4 sequences, 64 new tokens).
@@ -1751,7 +1751,9 @@ __global__ void __launch_bounds__(MERGE_THREADS) cache_merge_kernel(const __grid
 // ---------------------------------------------------------------------------------------------
 // With many new tokens the products decide, and those of whole tiles of 128 tokens belong to tcgen05: the cached keys and values
 // are written out as bf16 once (exactly, where the scale is a power of two), [sequence][capacity][hkv][D], and the packed
-// attention of this library (fcp_fwd_kernel) runs over them, with work units and row limits made on the device.
+// attention of this library (fcp_fwd_kernel) runs over them, with work units and row limits made on the device.  Its weights are bf16, so
+// that keys and values of any size meet them: 2.3e-3 from 64 bits in the mean over 4 chunks of 512 tokens, of which the rounding of o is
+// 1.7e-3; the kernels above, with halves, stay at 1.7e-3.
 //
 // Sequences that this cannot serve exactly are marked and left to cache_attn_kernel or cache_tile_kernel: tokens on pages that do not
 // exist, more new rows than tokens, a NaN value among the new tokens (it would meet zero weights of rows that do not see it), key

@@ -286,7 +286,7 @@ int rope(const char* call, float sign, const fcp_rope_table* table, int64_t T, c
   const int64_t strides = a.q_stride | a.k_stride | a.q_out_stride | a.k_out_stride;
   const bool wide = a.rotary % 16 == 0 && (bases & 15) == 0 && strides % 8 == 0;
   // As many tokens per block as let all blocks run at once, up to ROPE_SLOTS slots: finding the sequence and the angles costs a
-  // thread as much as three slots.  16K tokens of 12/4 heads of 64: 14 tokens 15.4 us, 10 16.4, 16 (1.4 rounds) 17.1; 4000: 4
+  // thread as much as three slots.  16K tokens of 12/4 heads of 64: 14 tokens (0.99 rounds) 15.4 us, 10 (1.4) 16.4, 16 (0.87) 17.1; 4000: 4
   // tokens 6.4, 13 9.2; 64K tokens of 32/8 heads of 128: 4 tokens 211, 1 token 284.
   const int64_t per_token = (hq + hkv) * (wide ? a.D / 16 : a.D / 2), at_once = ROPE_RESIDENT * FCP_PLAN_SMS;
   a.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({ROPE_TOKENS, ROPE_SLOTS / per_token, (T + at_once - 1) / at_once}));

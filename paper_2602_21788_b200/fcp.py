@@ -434,7 +434,8 @@ def _rope(call, table, q, k, q_out, k_out, positions, row_offset, length, stream
 
 def fcp_rope_fwd(table: RopeTable, q, k, q_out, k_out, positions=None, row_offset=None, length=None, stream=0):
     """q, k and their outputs: bf16 [T][heads][head_dim] (slices of wider rows are fine; outputs may be the inputs); either
-    pair may be None.  Positions are given, or follow from the batch's row_offset (and the sequences' lengths)."""
+    pair may be None.  Positions are given, or follow from the batch's row_offset (and the sequences' lengths; not after an eviction,
+    which shortens them and leaves the kept keys' positions as they were)."""
     _rope(lib().fcp_rope_fwd, table, q, k, q_out, k_out, positions, row_offset, length, stream)
 
 
@@ -490,7 +491,8 @@ class Cache:
 
 class CacheBatch:
     """The sequences a call works on: page_table int32 [B][width], length int32 [B] (new tokens included), row_offset int32 [B+1]
-    (device tensors, read when the call runs); rows and max_new bound them (default for max_new: rows)."""
+    (device tensors, read when the call runs); rows and max_new bound them.  max_new defaults to rows, which is right for one sequence
+    only: the kernels of fcp_cache_attn are chosen by it, so a step of single tokens passes max_new=1."""
 
     def __init__(self, page_table, length, row_offset=None, rows=0, max_new=None):
         _torch_types()
