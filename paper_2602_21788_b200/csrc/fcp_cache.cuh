@@ -317,6 +317,8 @@ __device__ __forceinline__ float exp2_approx(float x) {
 //   - from the first tiles of a group on that hold keys whose y is 60 from another's, tiles are marked ST_APART, and from its first key with
 //     y >= 60 on ST_HUGE besides: their probabilities get exponentials of their own, because the weights may vanish where the
 //     probabilities do not.
+// Against sums taken from the weights alone, us: one token of 64 sequences of 300 to 8K 76.8 -> 79.1, of one of 384K 129.9 -> 130.8; 25 rows
+// per KV head 189 -> 178 (the step compiled twice, the marked form apart).  A running top scale in every step took 80.3 for the first and 4 % more for the second.
 constexpr int CT_APART = 60, CT_HUGE = 60;
 constexpr float CT_SHIFT = -40.f, CT_SHIFT_HUGE = 20.f, CT_UNIT = 0x1p-40f, CT_UNIT_HUGE = 0x1p20f;
 // l times 2^e, for -250 < e < 250 where the result is in range; 0 stays 0
